@@ -422,6 +422,102 @@ MDI_API mdi_status mdi_partition_info(const mdi_partition *part, uint32_t what, 
 MDI_API mdi_status mdi_partition_trace(mdi_partition *part, void *trace);
 
 /*
+ * A key/value cache in 8 bits, in pages like a partition's own ("rotating KV
+ * caches", Sec. III-D; what a node's memory holds of them, Sec. IV-C): half the
+ * bytes of a bf16 cache, so a node holds twice as many positions and a token's
+ * attention reads half as much.
+ *
+ * A row - one position of one kv head, its key or its value - is head_dim codes
+ * of 8 bits and one scale: with top = max |x| over the row, scale = top / 127 and
+ * c = 127 / top, each rounded to binary32, a code is the whole number nearest to
+ * x * c (ties to even; the product is not rounded before) and stands for code *
+ * scale, at most half a scale from x.  A row with top < 2^-100 is stored as
+ * zeros; of a row with an infinity or NaN the scale is NaN, so that all of it
+ * reads back as NaN.
+ *
+ * codes and scales are device memory of the caller, 16-byte aligned, laid out as
+ * [n_pages][n_kv_head][2: key, value][page_tokens][head_dim] and
+ * [n_pages][n_kv_head][2][page_tokens].  tables: device int32
+ * [n_tables][table_stride], a sample's pages in the order of its positions;
+ * entries that no position reaches may hold anything.  What a page holds behind a
+ * sample's newest position is never used, whatever it is (NaN included).
+ * Limits: head_dim a multiple of 8, at most 256; n_kv_head at most 1024;
+ * table_stride * page_tokens^2 < 2^32.
+ * err: device int32 or NULL; a kernel that meets a page number outside
+ * [0, n_pages), a table row outside [0, n_tables) or a position outside
+ * [0, max_ctx) sets it to 2 (nothing clears it).  Nothing is read or written out
+ * of bounds then, but the results that depend on it mean nothing.
+ */
+typedef struct mdi_kv8 {
+  int8_t *codes;
+  float *scales;
+  const int32_t *tables;
+  int32_t *err;
+  uint32_t n_pages, n_kv_head, head_dim, page_tokens, n_tables, table_stride;
+} mdi_kv8;
+
+/*
+ * The rows of a call: n samples, packed one after the other.  start: device
+ * int32 [n + 1], sample i's rows are start[i] .. start[i + 1] - 1 of the call's
+ * buffers (start[0] = 0, never falling, at most n_rows; a sample may have none);
+ * NULL: one row per sample, row i is sample i's (then n_rows = n).  pos: device
+ * int32 [n], the position of a sample's first row (its others follow); below 0:
+ * the sample takes no part.  table: device int32 [n], the row of mdi_kv8.tables
+ * that is the sample's; NULL: row i.  n_rows: rows of the buffers, at most 2^24;
+ * those from start[n] on belong to nobody and are left as they are.  max_ctx:
+ * host's bound of pos + rows over all samples, at most table_stride *
+ * page_tokens; it decides how the work is divided, so a call that is captured
+ * into a graph and replayed with later positions names the last of them.
+ */
+typedef struct mdi_kv8_rows {
+  const int32_t *table, *start, *pos;
+  uint32_t n, n_rows, max_ctx;
+} mdi_kv8_rows;
+
+/*
+ * Quantise rows into the cache: k and v are device arrays of dtype (MDI_F32 or
+ * MDI_BF16), element (row, kv head, channel) at row * row_stride + head *
+ * head_stride + channel - the parts of a fused QKV product as they stand, for
+ * instance.  Both 16-byte aligned, strides multiples of 16 bytes.  No two rows of
+ * a call may go to the same position of the same page.  The call enqueues on
+ * hip_stream (NULL: the default stream), whose device has to be current, and
+ * returns; the library keeps nothing.  The same holds for the calls below.
+ * Errors: MDI_ERR_ARG for what the descriptions exclude; n = 0 does nothing.
+ */
+MDI_API mdi_status mdi_kv8_write(const mdi_kv8 *cache, const mdi_kv8_rows *rows, const void *k, const void *v,
+                         uint32_t dtype, uint64_t row_stride, uint64_t head_stride, void *hip_stream);
+
+/*
+ * The values that cached rows stand for, back into arrays laid out as in
+ * mdi_kv8_write (code * scale in binary32, rounded once more for MDI_BF16).
+ */
+MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, void *k, void *v,
+                        uint32_t dtype, uint64_t row_stride, uint64_t head_stride, void *hip_stream);
+
+/*
+ * Attention of the call's rows over their samples' caches: the row at position p
+ * attends to positions 0 .. p (which have been written, its own among them) with
+ * weights softmax(scale * q . k), query head i with kv head i / (n_head /
+ * n_kv_head).  With start = NULL that is one new token per sample; otherwise whole
+ * prompts, or the next pieces of prompts, of samples of different lengths.  q and
+ * out: device bf16 [n_rows][n_head][head_dim], rows q_stride / out_stride elements
+ * apart, 16-byte aligned, strides multiples of 8; they must not overlap.
+ * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
+ * binary32.  n_head: a multiple of n_kv_head, at most 4096.
+ * workspace: mdi_kv8_attn_bytes() bytes of device memory, 16-byte aligned (0 bytes:
+ * may be NULL); it carries nothing from one call to the next, and calls that can
+ * run at the same time need one each.  Results do not depend on timing.
+ * Errors: MDI_ERR_ARG; MDI_ERR_NOMEM if the workspace is too small.
+ */
+MDI_API mdi_status mdi_kv8_attn(const mdi_kv8 *cache, const mdi_kv8_rows *rows, const void *q, uint64_t q_stride,
+                        uint32_t n_head, float scale, void *out, uint64_t out_stride, void *workspace,
+                        size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace that mdi_kv8_attn needs for these rows (host only; the device arrays are not read). */
+MDI_API mdi_status mdi_kv8_attn_bytes(const mdi_kv8 *cache, const mdi_kv8_rows *rows, uint32_t n_head,
+                              size_t *workspace_bytes);
+
+/*
  * The node leaves the ring (the starter's stop message of Sec. III-A ends a
  * secondary's loop, Alg. 2): frees the host object.  Nothing is enqueued and
  * nothing waited for: the caller drains the partition's stream first

@@ -1,0 +1,49 @@
+// Key/value cache in 8 bits (mdi_kv8_* of mdi.h): what its entry points, the partition and the kernels share.
+//
+// A row - one position of one kv head, its key or its value - is kept as head_dim codes of 8 bits and one scale:
+//   top = max |x|, c = 127 / top and scale = top / 127 (each rounded to fp32),
+//   code = the whole number nearest to x c, ties to even, value = code * scale.
+// A value is off by at most half a scale.  One scale a row, because it then stands outside both sums of the attention: a score is
+// scale_k (q . codes_k), the weighted sum takes (weight * scale_v) codes_v, and codes are exact in bf16, so the matrix
+// cores multiply what the cache holds without another rounding.
+#pragma once
+
+#include "mdi_internal.h"
+
+namespace mdi {
+
+struct Kv8Cache {                    // mdi_kv8 as the kernels take it
+  int8_t* codes; float* scales;      // [n_pages][K][2][pt][h], [n_pages][K][2][pt]
+  const int32_t* tables; int32_t* err;
+  int n_pages, K, h, pt;
+  int pt_sh; unsigned pt_magic;      // page of a position: pos >> pt_sh, or with pt_sh < 0 the high word of pos * pt_magic
+  int n_tables, table_stride;
+};
+struct Kv8Rows {                     // mdi_kv8_rows
+  const int32_t *table, *start, *pos;
+  int n, n_rows, max_ctx;            // max_ctx <= table_stride * pt
+};
+
+struct Kv8RowsIO {                   // rows in or out: element (row, kv head, channel) at row * row_stride + head * head_stride + channel
+  void *k, *v; long row_stride, head_stride;
+};
+void launch_kv8_write(hipStream_t s, int dtype, const Kv8Cache& c, const Kv8Rows& r, const Kv8RowsIO& io);
+void launch_kv8_read(hipStream_t s, int dtype, const Kv8Cache& c, const Kv8Rows& r, const Kv8RowsIO& io);
+
+// How an attention call is divided: a row's visible positions go to workgroups in pieces of `chunk`, at most `splits` of them.
+// A row with one piece is finished where it is computed; of the others, every piece leaves its sums at part[((row * H +
+// head) * splits + piece) * (h + 4)]: h weighted sums, the reference, the sum of weights; a second launch adds them.
+struct Kv8Plan { int chunk, splits; };
+Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H);
+inline size_t kv8_part_bytes(const Kv8Plan& p, const Kv8Cache& c, const Kv8Rows& r, int H) {
+  return p.splits > 1 ? (size_t)r.n_rows * H * p.splits * (c.h + 4) * sizeof(float) : 0;
+}
+struct Kv8Attn {
+  const bf16_t* q; long q_stride;    // [n_rows][H][h], rows q_stride elements apart
+  bf16_t* out; long out_stride;
+  int H; float scale;                // scores are scale * (q . k) in powers of two: the softmax's scale times log2 e
+  float* part; Kv8Plan plan;
+};
+void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
+
+}  // namespace mdi

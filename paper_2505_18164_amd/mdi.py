@@ -20,7 +20,8 @@ MDI_HAS_EMBED, MDI_HAS_HEAD = 1, 2
 
 EXPORTS = ["mdi_partition_bytes", "mdi_partition_create", "mdi_prefill", "mdi_prefill_chunk", "mdi_decode_step", "mdi_decode_steps", "mdi_decode_batch",
            "mdi_sample_greedy", "mdi_sample_topk", "mdi_sample_topk_static", "mdi_sample_batch", "mdi_partition_sync", "mdi_seq_reset", "mdi_seq_len", "mdi_step_bytes", "mdi_time_kernel",
-           "mdi_partition_info", "mdi_partition_trace", "mdi_partition_destroy", "mdi_strerror"]
+           "mdi_partition_info", "mdi_partition_trace", "mdi_partition_destroy", "mdi_strerror",
+           "mdi_kv8_write", "mdi_kv8_read", "mdi_kv8_attn", "mdi_kv8_attn_bytes"]
 
 
 class MdiConfig(C.Structure):
@@ -42,6 +43,15 @@ class MdiLayerWeights(C.Structure):
 class MdiWeights(C.Structure):
     _fields_ = [("wte", C.c_void_p), ("wpe", C.c_void_p), ("lnf_g", C.c_void_p), ("lnf_b", C.c_void_p),
                 ("lm_head", C.c_void_p), ("layers", C.POINTER(MdiLayerWeights))]
+
+
+class MdiKv8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales", "tables", "err")] + \
+               [(n, C.c_uint32) for n in ("n_pages", "n_kv_head", "head_dim", "page_tokens", "n_tables", "table_stride")]
+
+
+class MdiKv8Rows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "start", "pos")] + [(n, C.c_uint32) for n in ("n", "n_rows", "max_ctx")]
 
 
 class MdiError(RuntimeError):
@@ -83,8 +93,14 @@ def lib():
         L.mdi_partition_destroy.restype = None
         L.mdi_strerror.argtypes = [C.c_int]
         L.mdi_strerror.restype = C.c_char_p
-        for name in EXPORTS[:18]:
-            getattr(L, name).restype = C.c_int
+        kv8, rows, u64 = C.POINTER(MdiKv8), C.POINTER(MdiKv8Rows), C.c_uint64
+        L.mdi_kv8_write.argtypes = [kv8, rows, vp, vp, u32, u64, u64, vp]
+        L.mdi_kv8_read.argtypes = [kv8, rows, vp, vp, u32, u64, u64, vp]
+        L.mdi_kv8_attn.argtypes = [kv8, rows, vp, u64, u32, C.c_float, vp, u64, vp, C.c_size_t, vp]
+        L.mdi_kv8_attn_bytes.argtypes = [kv8, rows, u32, C.POINTER(C.c_size_t)]
+        for name in EXPORTS:
+            if name not in ("mdi_partition_destroy", "mdi_strerror"):
+                getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
 
@@ -348,3 +364,116 @@ class Partition:
             self.close()
         except Exception:
             pass
+
+
+def _stride(t, dim, alone):
+    """Elements between neighbours along `dim`; a dimension of one has none, whatever the tensor says: `alone`."""
+    return t.stride(dim) if t.shape[dim] > 1 else alone
+
+
+class Kv8Rows:
+    """The rows of a call (mdi_kv8_rows), made by Kv8Cache.rows; keeps its device arrays alive."""
+
+    def __init__(self, keep, struct, n_rows):
+        self._keep, self._c, self.n_rows = keep, struct, n_rows
+        self._ref = C.byref(struct)
+
+
+class Kv8Cache:
+    """A key/value cache in 8 bits (mdi_kv8): codes int8 [pages, kv heads, 2, page tokens, head_dim], scales float32
+    [pages, kv heads, 2, page tokens], tables int32 [samples, pages of a sample], all contiguous on one GPU; err: int32 [1]
+    or None, see check().  Calls enqueue on the current stream of that GPU."""
+
+    def __init__(self, codes, scales, tables, err=None):
+        if codes.dim() != 5 or codes.shape[2] != 2 or scales.shape != codes.shape[:4] or tables.dim() != 2:
+            raise ValueError("codes [pages, kv heads, 2, page tokens, head_dim], scales [pages, kv heads, 2, page tokens], tables [samples, pages]")
+        self.device = codes.device
+        self._tensor(codes, torch.int8, "codes")
+        self._tensor(scales, torch.float32, "scales")
+        self._tensor(tables, torch.int32, "tables")
+        if err is not None:
+            self._tensor(err, torch.int32, "err")
+        self.codes, self.scales, self.tables, self.err = codes, scales, tables, err
+        self.n_pages, self.K, _, self.page_tokens, self.h = codes.shape
+        self._c = MdiKv8(_ptr(codes), _ptr(scales), _ptr(tables), _ptr(err), self.n_pages, self.K, self.h, self.page_tokens,
+                         tables.shape[0], tables.shape[1])
+        self._ref = C.byref(self._c)
+
+    def _tensor(self, t, dtype, what, contiguous=True):
+        if t.dtype != dtype or t.device != self.device or (contiguous and not t.is_contiguous()):
+            raise ValueError(f"{what}: expected a {'contiguous ' if contiguous else ''}{dtype} tensor on {self.device}")
+
+    def _call(self, what, *args):
+        """A C entry point, on the current stream of the cache's GPU, with that GPU current."""
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        if self.device.index == torch.cuda.current_device():
+            st = getattr(lib(), what)(*args, stream)
+        else:
+            with torch.cuda.device(self.device):
+                st = getattr(lib(), what)(*args, stream)
+        if st != MDI_OK:
+            raise MdiError(st, what)
+
+    def rows(self, pos, start=None, table=None, n_rows=None, max_ctx=None):
+        """pos int32 [n]; start int32 [n + 1] (None: one row per sample), table int32 [n] (None: row i of the tables); n_rows:
+        rows of the call's buffers (needed with start); max_ctx: no sample gets longer (default: what the tables hold)."""
+        n = pos.shape[0]
+        self._tensor(pos, torch.int32, "pos")
+        for t, size, what in ((start, n + 1, "start"), (table, n, "table")):
+            if t is not None:
+                self._tensor(t, torch.int32, what)
+                if t.shape != (size,):
+                    raise ValueError(f"{what}: expected {size} entries")
+        if start is not None and n_rows is None:
+            raise ValueError("n_rows: the rows of the buffers are not read from the device")
+        n_rows = n if n_rows is None else n_rows
+        max_ctx = self.tables.shape[1] * self.page_tokens if max_ctx is None else max_ctx
+        return Kv8Rows((pos, start, table), MdiKv8Rows(_ptr(table), _ptr(start), _ptr(pos), n, n_rows, max_ctx), n_rows)
+
+    def _rows_io(self, rows, k, v, what):
+        if k.shape != (rows.n_rows, self.K, self.h) or v.shape != k.shape or v.dtype != k.dtype or v.device != k.device \
+                or k.stride() != v.stride() or k.stride(2) != 1:
+            raise ValueError(f"{what}: k and v [rows, kv heads, head_dim] of one type and layout, channels next to each other")
+        if k.device != self.device or k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"{what}: bfloat16 or float32 on {self.device}")
+        return (k.data_ptr(), v.data_ptr(), MDI_BF16 if k.dtype == torch.bfloat16 else MDI_F32, _stride(k, 0, self.K * self.h),
+                _stride(k, 1, self.h))
+
+    def write(self, rows, k, v):
+        """Quantise rows k, v [rows, kv heads, head_dim] (bfloat16 or float32, any row and head stride) into the cache."""
+        self._call("mdi_kv8_write", self._ref, rows._ref, *self._rows_io(rows, k, v, "write"))
+
+    def read(self, rows, k, v):
+        """The values the cached rows stand for, into k, v; returns (k, v)."""
+        self._call("mdi_kv8_read", self._ref, rows._ref, *self._rows_io(rows, k, v, "read"))
+        return k, v
+
+    def workspace(self, rows, n_head):
+        """A workspace for attn calls on these rows (None when none is needed)."""
+        n = C.c_size_t(0)
+        st = lib().mdi_kv8_attn_bytes(self._ref, rows._ref, n_head, C.byref(n))
+        if st != MDI_OK:
+            raise MdiError(st, "mdi_kv8_attn_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device) if n.value else None
+
+    def attn(self, rows, q, scale=None, out=None, workspace=None):
+        """Attention of rows q [rows, heads, head_dim] (bfloat16) over their samples' caches; scale: head_dim ** -0.5.
+        workspace: as made by workspace() (None: taken from the allocator for this call)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        for t in (q, out):
+            if t.dim() != 3 or t.shape[0] != rows.n_rows or t.shape[2] != self.h or t.dtype != torch.bfloat16 or t.device != self.device \
+                    or t.stride(2) != 1 or _stride(t, 1, self.h) != self.h or t.shape != q.shape:
+                raise ValueError(f"attn: q and out bfloat16 [rows, heads, {self.h}] on {self.device}, heads next to each other")
+        if workspace is None:
+            workspace = self.workspace(rows, q.shape[1])
+        self._call("mdi_kv8_attn", self._ref, rows._ref, q.data_ptr(), _stride(q, 0, q.shape[1] * self.h), q.shape[1],
+                   self.h ** -0.5 if scale is None else scale, out.data_ptr(), _stride(out, 0, q.shape[1] * self.h), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+        return out
+
+    def check(self):
+        """Wait for the current stream and report what only the device can detect (needs err): an MdiError for a page, table
+        row or position outside the cache."""
+        torch.cuda.current_stream(self.device).synchronize()
+        if self.err is not None and int(self.err.item()):
+            raise MdiError(MDI_ERR_ARG, "mdi_kv8")

@@ -1,0 +1,72 @@
+"""What the 8-bit cache's entry points refuse on the host, before anything reaches a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from kv8_cases import quantise
+from paper_2505_18164_amd import mdi
+
+GOOD = dict(codes=4096, scales=8192, tables=64, err=None, n_pages=8, n_kv_head=2, head_dim=64, page_tokens=16, n_tables=2, table_stride=4)
+ROWS = dict(table=None, start=16, pos=32, n=2, n_rows=9, max_ctx=64)
+
+
+def cache(**over):
+    f = dict(GOOD, **over)
+    return mdi.MdiKv8(*[f[n] for n, _ in mdi.MdiKv8._fields_])
+
+
+def rows(**over):
+    f = dict(ROWS, **over)
+    return mdi.MdiKv8Rows(*[f[n] for n, _ in mdi.MdiKv8Rows._fields_])
+
+
+def bytes_of(c, r, heads=4):
+    n = C.c_size_t(77)
+    return mdi.lib().mdi_kv8_attn_bytes(C.byref(c) if c else None, C.byref(r) if r else None, heads, C.byref(n)), n.value
+
+
+def test_sizes():
+    assert C.sizeof(mdi.MdiKv8) == 4 * 8 + 6 * 4 and C.sizeof(mdi.MdiKv8Rows) == 3 * 8 + 3 * 4 + 4
+    assert bytes_of(cache(), rows()) == (mdi.MDI_OK, 0)                        # short samples are not divided
+    st, n = bytes_of(cache(table_stride=1000), rows(n_rows=2, max_ctx=16000, start=None))
+    assert st == mdi.MDI_OK and n >= 2 * 4 * 2 * 68 * 4
+
+
+@pytest.mark.parametrize("over", [dict(codes=None), dict(scales=None), dict(tables=None), dict(codes=4100), dict(scales=8196), dict(n_pages=0), dict(n_kv_head=0),
+                                  dict(n_kv_head=1025), dict(head_dim=0), dict(head_dim=60), dict(head_dim=264), dict(page_tokens=0), dict(n_tables=0), dict(table_stride=0),
+                                  dict(n_pages=1 << 31), dict(page_tokens=1 << 14, table_stride=16), dict(page_tokens=1, table_stride=1 << 31)])
+def test_caches_that_are_refused(over):
+    assert bytes_of(cache(**over), rows(max_ctx=1))[0] == mdi.MDI_ERR_ARG
+
+
+@pytest.mark.parametrize("over", [dict(pos=None), dict(start=None), dict(max_ctx=0), dict(max_ctx=65), dict(n_rows=(1 << 24) + 1), dict(n=1 << 31)])
+def test_rows_that_are_refused(over):
+    assert bytes_of(cache(), rows(**over))[0] == mdi.MDI_ERR_ARG
+
+
+def test_calls_that_are_refused():
+    L, c, r = mdi.lib(), cache(), rows()
+    assert bytes_of(None, r)[0] == bytes_of(c, None)[0] == mdi.MDI_ERR_ARG
+    for heads in (0, 3, 4098):
+        assert bytes_of(c, r, heads)[0] == mdi.MDI_ERR_ARG
+    assert L.mdi_kv8_attn_bytes(C.byref(c), C.byref(r), 4, None) == mdi.MDI_ERR_ARG
+    for call in (L.mdi_kv8_write, L.mdi_kv8_read):
+        for a in ((None, 16, 1, 128, 64), (16, None, 1, 128, 64), (16, 16, 2, 128, 64), (8, 16, 1, 128, 64), (16, 24, 1, 128, 64), (16, 16, 1, 4, 64), (16, 16, 1, 128, 4),
+                  (16, 16, 0, 2, 64), (16, 16, 1, 1 << 39, 64)):
+            assert call(C.byref(c), C.byref(r), *a, None) == mdi.MDI_ERR_ARG, a
+        assert call(None, C.byref(r), 16, 16, 1, 128, 64, None) == mdi.MDI_ERR_ARG
+        assert call(C.byref(c), C.byref(rows(n=0, n_rows=0, pos=None)), None, None, 1, 128, 64, None) == mdi.MDI_OK      # nothing to do
+    for a in ((None, 256, 4, .1, 16, 256), (16, 256, 4, .1, None, 256), (24, 256, 4, .1, 16, 256), (16, 256, 4, .1, 24, 256), (16, 248, 4, .1, 16, 256), (16, 256, 4, .1, 16, 248),
+              (16, 260, 4, .1, 16, 256), (16, 256, 3, .1, 16, 256), (16, 256, 4, float("nan"), 16, 256), (16, 256, 4, float("inf"), 16, 256)):
+        assert L.mdi_kv8_attn(C.byref(c), C.byref(r), *a, None, 0, None) == mdi.MDI_ERR_ARG, a
+    c, r = cache(table_stride=1000), rows(n_rows=2, max_ctx=16000, start=None)
+    assert L.mdi_kv8_attn(C.byref(c), C.byref(r), 16, 256, 4, .1, 16, 256, None, 1 << 30, None) == mdi.MDI_ERR_ARG
+    assert L.mdi_kv8_attn(C.byref(c), C.byref(r), 16, 256, 4, .1, 16, 256, 8, 1 << 30, None) == mdi.MDI_ERR_ARG
+    assert L.mdi_kv8_attn(C.byref(c), C.byref(r), 16, 256, 4, .1, 16, 256, 16, bytes_of(c, r)[1] - 1, None) == mdi.MDI_ERR_NOMEM
+
+
+def test_the_formula():
+    code, scale = quantise(np.array([[1.0, -1.0, 0.5, 0.0], [0, 0, 0, 0], [2.0 ** -101, 0, 0, 0], [1, np.inf, 0, 0], [127, 0.5, 1.5, -2.5]]))
+    assert code.tolist() == [[127, -127, 64, 0], [0] * 4, [0] * 4, [0] * 4, [127, 0, 2, -2]]     # ties to even: 63.5 is 64
+    assert scale[1] == scale[2] == 0 and np.isnan(scale[3]) and scale[4] == 1
