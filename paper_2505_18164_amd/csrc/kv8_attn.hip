@@ -106,6 +106,7 @@ __global__ __launch_bounds__(kBlock) void k_kv8_join(Kv8Cache c, Kv8Rows r, Kv8A
 }  // namespace
 
 Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
+  if (kv8_decode_supported(c, r)) return kv8_decode_plan(c, r, H);
   const long items = (long)r.n_rows * H;
   const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / items));
   int chunk = std::max(256, ((r.max_ctx + want - 1) / want + 63) / 64 * 64);
@@ -113,9 +114,13 @@ Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
 }
 
 void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  int L = 1;
-  while (8 * L < c.h) L *= 2;
-  hipLaunchKernelGGL(k_kv8_attn, dim3((unsigned)(r.n_rows * a.H), a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
+  if (kv8_decode_supported(c, r)) {
+    launch_kv8_decode(s, c, r, a);
+  } else {
+    int L = 1;
+    while (8 * L < c.h) L *= 2;
+    hipLaunchKernelGGL(k_kv8_attn, dim3((unsigned)(r.n_rows * a.H), a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
+  }
   if (a.plan.splits > 1)
     hipLaunchKernelGGL(k_kv8_join, dim3((unsigned)(((long)r.n_rows * a.H + 3) / 4)), dim3(kBlock), 0, s, c, r, a);
 }

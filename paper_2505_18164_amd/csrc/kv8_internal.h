@@ -44,6 +44,10 @@ struct Kv8Attn {
   int H; float scale;                // scores are scale * (q . k) in powers of two: the softmax's scale times log2 e
   float* part; Kv8Plan plan;
 };
+// One new token per sample with heads of 64 or 128: on the matrix cores (kv8_decode.hip).
+bool kv8_decode_supported(const Kv8Cache& c, const Kv8Rows& r);
+Kv8Plan kv8_decode_plan(const Kv8Cache& c, const Kv8Rows& r, int H);
+void launch_kv8_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
 void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
 
 }  // namespace mdi
