@@ -12,11 +12,10 @@ mdi_status take_cache(const mdi_kv8* k, Kv8Cache* c) {
   if (!k->n_pages || !k->n_kv_head || !k->head_dim || !k->page_tokens || !k->n_tables || !k->table_stride) return MDI_ERR_ARG;
   if (k->head_dim % 8 || k->head_dim > 256 || k->n_kv_head > 1024 || k->n_pages > INT32_MAX || k->n_tables > INT32_MAX) return MDI_ERR_ARG;
   // a position is divided by the page size with one multiplication, exact below this bound
-  if ((uint64_t)k->table_stride * k->page_tokens > INT32_MAX || (uint64_t)k->table_stride * k->page_tokens * k->page_tokens >= (1ull << 32)) return MDI_ERR_ARG;
+  if ((uint64_t)k->table_stride * k->page_tokens > 1u << 30 || (uint64_t)k->table_stride * k->page_tokens * k->page_tokens >= (1ull << 32)) return MDI_ERR_ARG;
   const int pt = (int)k->page_tokens;
-  const bool pow2 = (pt & (pt - 1)) == 0;
   *c = Kv8Cache{k->codes, k->scales, k->tables, k->err, (int)k->n_pages, (int)k->n_kv_head, (int)k->head_dim, pt,
-                pow2 ? __builtin_ctz((unsigned)pt) : -1, pow2 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u, (int)k->n_tables, (int)k->table_stride};
+                pt == 1 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u, (int)k->n_tables, (int)k->table_stride};
   return MDI_OK;
 }
 
@@ -35,7 +34,8 @@ mdi_status take(const mdi_kv8* k, const mdi_kv8_rows* g, Kv8Cache* c, Kv8Rows* r
 
 // Query rows of the call: heads that the kv heads divide, rows of 16-byte pieces.
 bool good_heads(const Kv8Cache& c, const Kv8Rows& r, uint32_t n_head) {
-  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 31);
+  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 31) &&
+         (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 1) < (1ull << 31);   // tiles of all units are counted in 32 bits
 }
 
 mdi_status hip_status() { return hipGetLastError() == hipSuccess ? MDI_OK : MDI_ERR_HIP; }

@@ -1,13 +1,21 @@
 // Attention of one new token per sample over the 8-bit cache, on the matrix cores.
 //
-// A workgroup takes one kv head of one sample, up to sixteen of its query heads and a piece of its positions; its four wavefronts
-// take tiles of 32 positions in turn, straight from the pages into registers.  Both products are computed transposed:
+// A workgroup takes one kv head of one sample and up to sixteen of its query heads (a unit), or a piece of its positions; its
+// four wavefronts take 32 positions in turn, straight from the pages into registers.  Both products are computed transposed:
 // S^T = K Q^T leaves, with v_mfma_f32_16x16x32_bf16, positions 4 g + r (g = lane / 16) of query lane % 16 in a lane, and two
-// tiles of 16 positions side by side are just what O^T = V^T P^T takes as its second operand, if the sixteen positions that lane
+// tiles of 16 positions side by side are just what O^T = V^T P^T takes as its second operand, if the positions that lane
 // group g contracts are named 4 g .. 4 g + 3 of either tile.  The sum over positions is in no order, so any naming does; likewise
 // the channels of K and Q.  So a key's codes are read 16 bytes a lane (four lanes a row, 64 bytes of it next to each other),
-// a value's HD / 16 bytes a lane (sixteen lanes a row), and the transposition of V costs nothing: a code becomes bf16 by itself, whichever byte
-// of whichever row's word it is.
+// a value's HD / 16 bytes a lane (sixteen lanes a row), and nothing has to be transposed: a code becomes bf16 by itself,
+// whichever byte of whichever row's word it is (one conversion, and one byte permutation for two of them).
+//
+// What bounds it: memory.  A code takes 1.5 vector instructions, a score about ten; a wavefront spends 0.7 us on 32 positions,
+// 40 % of the time that twelve of them on a compute unit have until the memory has answered.  Nothing is fetched ahead inside a
+// wavefront: a second tile of registers (217 of them, two workgroups a compute unit) only made every load wait longer, the first ones of
+// a unit - page numbers, query - included (8 samples of the 7B shape 42 us, 16 of the 8B shape 55).
+// Shares instead of pieces of one length: 8 samples of 1 .. 4096 positions 41 -> 29.8 us (a piece is as long as the longest
+// sample's, and few of them are); what a unit costs to begin has to count, or 32 short ones after the other are one workgroup's (69 us).
+// 16 samples of 8100 positions of the 8B shape: 53 us = 5.2 TB/s of codes and scales, 8 of the 7B shape 4.5 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,211 +35,238 @@ template <int HD> struct Tile {      // 32 positions of a wavefront
 
 // kWhole16: pages of a multiple of 16 positions, so 16 aligned positions lie in one page, next to each other.
 template <int HD, bool kWhole16>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_kv8_decode(Kv8Cache c, Kv8Rows r, Kv8Attn a, int groups) {
+__global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Rows r, Kv8Attn a, int groups) {
   constexpr int KI = HD / 64, VB = HD / 16;                      // 16-byte units of a key a lane has; bytes of a value (= channel blocks)
   constexpr int OS = HD + 4;
   __shared__ __attribute__((aligned(16))) float fold[kWaves * 16 * OS];
   __shared__ float fold_m[kWaves][16], fold_l[kWaves][16];
-  int* pages = (int*)fold;                                       // (done with before the fold begins)
-  static_assert(kPages <= kWaves * 16 * OS, "page numbers fit");
+  __shared__ int pages[kPages];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-  const int piece = blockIdx.x % a.plan.splits, unit = blockIdx.x / a.plan.splits;
-  const int sample = unit / (c.K * groups), kvg = unit - sample * (c.K * groups), kv = kvg / groups, G = a.H / c.K;
-  const int head0 = kv * G + 16 * (kvg - kv * groups), heads = min(16, kv * G + G - head0);
-  const Kv8View view = kv8_view(c, r, sample);
-  const int lo = piece * a.plan.chunk, hi = min(view.seen, lo + a.plan.chunk);
-  if (lo >= hi && piece > 0) return;
-  const int32_t* table = view.seen ? kv8_table(c, r, sample) : nullptr;
-  bf16_t* out = a.out + (long)sample * a.out_stride + (long)head0 * HD;
-  if (!table) {
-    if (piece == 0) for (int e = threadIdx.x; e < heads * HD; e += 64 * kWaves) out[e] = 0;
-    return;
+  const unsigned k_off = col * HD + 16 * g, v_off = 4 * g * HD + VB * col, s_off = 16 * g;
+  const int units = c.K * groups, G = a.H / c.K;                  // units of a sample: a kv head's sixteen query heads
+  int x0 = blockIdx.x, x1 = x0 + 1, per = 1, seen64 = 0;
+  if (a.plan.wgs) {
+    seen64 = kv8_seen(c, r, lane);
+    const Kv8Stream all = kv8_stream(c, r, a.plan, units, 0, seen64);
+    per = all.per;
+    x0 = min(x0 * per, all.cost * units);
+    x1 = min(x0 + per, all.cost * units);
   }
-
-  const int at0 = kv8_page_of(c, lo), n_at = kv8_page_of(c, hi - 1) - at0 + 1;
-  for (int i = threadIdx.x; i < n_at; i += 64 * kWaves) pages[i] = kv8_checked_page(c, table[at0 + i]);
-  // this lane's query: channels 64 i + 16 g + 8 s + 0..7 for steps 2 i + s, as the keys' units have them
-  bf16x8 qf[2 * KI];
-  {
-    const bf16_t* q = a.q + (long)sample * a.q_stride + (long)(head0 + min(col, heads - 1)) * HD + 16 * g;
-#pragma unroll
-    for (int i = 0; i < KI; ++i)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) qf[2 * i + s] = *reinterpret_cast<const bf16x8*>(q + 64 * i + 8 * s);
-  }
-  f32x4 o[VB];
-#pragma unroll
-  for (int b = 0; b < VB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = kKv8None, l = 0.f;
-  __syncthreads();
-
-  auto row_of = [&](int pos) __attribute__((always_inline)) {     // the key's row; the value's is pt further
-    const int at = kv8_page_of(c, pos);
-    return ((long)pages[at - at0] * c.K + kv) * 2 * c.pt + (pos - at * c.pt);
-  };
-  auto fetch = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if constexpr (kWhole16) {
-        const int p16 = min(base + 16 * u, (hi - 1) & ~15), at = kv8_page_of(c, p16);
-        const int page = __builtin_amdgcn_readfirstlane(pages[at - at0]);
-        const long row = ((long)page * c.K + kv) * 2 * c.pt + (p16 - at * c.pt);
-        const int8_t* kp = c.codes + row * HD;
-        const int8_t* vp = kp + (long)c.pt * HD;
-#pragma unroll
-        for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + col * HD + 64 * i + 16 * g);
-        const float* sp = c.scales + row + 4 * g;
-        t.ks[u] = *reinterpret_cast<const f32x4*>(sp);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(vp + (4 * g + j) * HD + VB * col);
-          if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
-          else t.v[u][j][0] = *w;
-        }
-        t.vs[u] = *reinterpret_cast<const f32x4*>(sp + c.pt);
-      } else {
-        const int8_t* kp = c.codes + row_of(min(base + 16 * u + col, hi - 1)) * HD;
-#pragma unroll
-        for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + 64 * i + 16 * g);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const long row = row_of(min(base + 16 * u + 4 * g + j, hi - 1));
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(c.codes + (row + c.pt) * HD + VB * col);
-          if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
-          else t.v[u][j][0] = *w;
-          t.ks[u][j] = c.scales[row];
-          t.vs[u][j] = c.scales[row + c.pt];
-        }
-      }
+  while (x0 < x1) {
+    int sample, unit, seen, piece = 0, pieces = 1, lo = 0, end;
+    if (a.plan.wgs) {
+      const Kv8Found f = kv8_find(c, r, x0 / units, seen64);
+      sample = f.sample;
+      seen = f.seen;
+      const int tiles = kv8_tiles(seen), cost = tiles + kKv8Begin, in = x0 - f.start * units;
+      unit = in / cost;
+      // this share has x0 .. next - 1, the unit's tiles are from .. from + tiles - 1
+      const int start = f.start * units + unit * cost, from = start + kKv8Begin, next = min(x1, start + cost), first_wg = from / per;
+      lo = max(x0 - from, 0) * kKv8Tile;
+      end = min(seen, max(next - from, 0) * kKv8Tile);
+      piece = (int)blockIdx.x - first_wg;
+      pieces = max(from + tiles - 1, from) / per - first_wg + 1;
+      x0 = next;
+      if (seen && lo >= end) continue;                           // only what it costs to begin: the tiles are another share's
+    } else {
+      sample = x0 / units;
+      unit = x0 - sample * units;
+      seen = end = __builtin_amdgcn_readfirstlane(kv8_seen(c, r, sample));
+      x0 = x1;
     }
-  };
-  auto use = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
-    f32x4 s[2];
-    float p[2][4];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int kv = unit / groups, head0 = kv * G + 16 * (unit - kv * groups), heads = min(16, kv * G + G - head0);
+    const int which = __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample));
+    const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
+    int at0 = kv8_page_of(c, lo);
+    const int first = at0 + (int)threadIdx.x < c.table_stride ? table[at0 + threadIdx.x] : 0;
+    bf16_t* out = a.out + (long)sample * a.out_stride + (long)head0 * HD;
+    if (!seen || which < 0) {
+      if (piece <= 0) for (int e = threadIdx.x; e < heads * HD; e += 64 * kWaves) out[e] = 0;
+      continue;
+    }
+    // this lane's query: channels 64 i + 16 g + 8 s + 0..7 for steps 2 i + s, as the keys' units have them
+    bf16x8 qf[2 * KI];
+    {
+      const bf16_t* q = a.q + (long)sample * a.q_stride + (long)(head0 + min(col, heads - 1)) * HD + 16 * g;
 #pragma unroll
       for (int i = 0; i < KI; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t a0 = t.k[u][i][2 * h], a1 = t.k[u][i][2 * h + 1];
-          const u32x4 f = {high_halves(code_of<0>(a0), code_of<1>(a0)), high_halves(code_of<2>(a0), code_of<3>(a0)),
-                           high_halves(code_of<0>(a1), code_of<1>(a1)), high_halves(code_of<2>(a1), code_of<3>(a1))};
-          s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[2 * i + h], s[u], 0, 0, 0);
-        }
-      t.ks[u] *= a.scale;
+        for (int s = 0; s < 2; ++s) qf[2 * i + s] = *reinterpret_cast<const bf16x8*>(q + 64 * i + 8 * s);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (base + 32 > hi) {                                        // what lies behind the last position counts for nothing, whatever it holds
+    f32x4 o[VB];
+#pragma unroll
+    for (int b = 0; b < VB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kKv8None, l = 0.f;
+    int hi = lo;
+
+    auto row_of = [&](int pos) __attribute__((always_inline)) {     // the key's row; the value's is pt further
+      const int at = kv8_page_of(c, pos);
+      return ((long)pages[at - at0] * c.K + kv) * 2 * c.pt + (pos - at * c.pt);
+    };
+    auto fetch = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (kWhole16) {
+          const int p16 = min(base + 16 * u, (hi - 1) & ~15), at = kv8_page_of(c, p16);
+          const int page = __builtin_amdgcn_readfirstlane(pages[at - at0]);
+          const long row = ((long)page * c.K + kv) * 2 * c.pt + (p16 - at * c.pt);
+          // one uniform address each and 32-bit offsets of the lanes
+          const char* kp = (const char*)c.codes + row * HD;
+          const char* vp = kp + (long)c.pt * HD;
+          const char* sk = (const char*)(c.scales + row);
+          const char* sv = sk + 4l * c.pt;
+#pragma unroll
+          for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + (k_off + 64u * i));
+          t.ks[u] = *reinterpret_cast<const f32x4*>(sk + s_off);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const char* w = vp + (v_off + (unsigned)(j * HD));
+            if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
+            else t.v[u][j][0] = *reinterpret_cast<const uint32_t*>(w);
+          }
+          t.vs[u] = *reinterpret_cast<const f32x4*>(sv + s_off);
+        } else {
+          const int8_t* kp = c.codes + row_of(min(base + 16 * u + col, hi - 1)) * HD;
+#pragma unroll
+          for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + 64 * i + 16 * g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const long row = row_of(min(base + 16 * u + 4 * g + j, hi - 1));
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(c.codes + (row + c.pt) * HD + VB * col);
+            if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
+            else t.v[u][j][0] = *w;
+            t.ks[u][j] = c.scales[row];
+            t.vs[u][j] = c.scales[row + c.pt];
+          }
+        }
+      }
+    };
+    auto use = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
+      f32x4 s[2];
+      float p[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KI; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t a0 = t.k[u][i][2 * h], a1 = t.k[u][i][2 * h + 1];
+            const u32x4 f = {high_halves(code_of<0>(a0), code_of<1>(a0)), high_halves(code_of<2>(a0), code_of<3>(a0)),
+                             high_halves(code_of<0>(a1), code_of<1>(a1)), high_halves(code_of<2>(a1), code_of<3>(a1))};
+            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[2 * i + h], s[u], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);                     // (else every step's operands are made first, and spilled)
+          }
+        t.ks[u] *= a.scale;
+      }
+      if (base + 32 > hi) {                                        // what lies behind the last position counts for nothing, whatever it holds
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (base + 16 * u + 4 * g + j >= hi) { s[u][j] = -INFINITY; t.ks[u][j] = 1.f; t.vs[u][j] = 0.f; }
+      }
+      float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (base + 16 * u + 4 * g + j >= hi) { s[u][j] = -INFINITY; t.ks[u][j] = 1.f; t.vs[u][j] = 0.f; }
-    }
-    float top = -INFINITY;
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, s[u][j] * t.ks[u][j]);
+      // Weights are relative to m, which is raised - for all four lanes of a query alike - only when a score exceeds it by
+      // 2^kKv8Raise: the sum is divided out at the end, so any reference near the largest score does.
+      if (__any(top > m + kKv8Raise)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = fmaxf(m, top), alpha = exp2_raw(m - to);
+        m = to;
+        l *= alpha;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, s[u][j] * t.ks[u][j]);
-    // Weights are relative to m, which is raised - for all four lanes of a query alike - only when a score exceeds it by
-    // 2^kKv8Raise: the sum is divided out at the end, so any reference near the largest score does.
-    if (__any(top > m + kKv8Raise)) {
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float to = fmaxf(m, top), alpha = exp2_raw(m - to);
-      m = to;
-      l *= alpha;
-#pragma unroll
-      for (int b = 0; b < VB; ++b) o[b] *= alpha;
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        p[u][j] = exp2_raw(fmaf(s[u][j], t.ks[u][j], -m));
-        l += p[u][j];
-        p[u][j] *= t.vs[u][j];
+        for (int b = 0; b < VB; ++b) o[b] *= alpha;
       }
-    bf16x8 pf;                                                   // the one rounding of a weight: to the matrix cores' operand
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) pf[4 * u + j] = (__bf16)p[u][j];
+        for (int j = 0; j < 4; ++j) {
+          p[u][j] = exp2_raw(fmaf(s[u][j], t.ks[u][j], -m));
+          l += p[u][j];
+          p[u][j] *= t.vs[u][j];
+        }
+      bf16x8 pf;                                                   // the one rounding of a weight: to the matrix cores' operand
 #pragma unroll
-    for (int w = 0; w < KI; ++w) {
-      auto block = [&](auto byte) __attribute__((always_inline)) {
-        constexpr int N = decltype(byte)::value;
-        const u32x4 f = {high_halves(code_of<N>(t.v[0][0][w]), code_of<N>(t.v[0][1][w])), high_halves(code_of<N>(t.v[0][2][w]), code_of<N>(t.v[0][3][w])),
-                         high_halves(code_of<N>(t.v[1][0][w]), code_of<N>(t.v[1][1][w])), high_halves(code_of<N>(t.v[1][2][w]), code_of<N>(t.v[1][3][w]))};
-        o[4 * w + N] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pf, o[4 * w + N], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);                       // (else every block's operands are made first, and spilled)
-      };
-      block(std::integral_constant<int, 0>());
-      block(std::integral_constant<int, 1>());
-      block(std::integral_constant<int, 2>());
-      block(std::integral_constant<int, 3>());
-    }
-  };
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pf[4 * u + j] = (__bf16)p[u][j];
+#pragma unroll
+      for (int w = 0; w < KI; ++w) {
+        auto block = [&](auto byte) __attribute__((always_inline)) {
+          constexpr int N = decltype(byte)::value;
+          const u32x4 f = {high_halves(code_of<N>(t.v[0][0][w]), code_of<N>(t.v[0][1][w])), high_halves(code_of<N>(t.v[0][2][w]), code_of<N>(t.v[0][3][w])),
+                           high_halves(code_of<N>(t.v[1][0][w]), code_of<N>(t.v[1][1][w])), high_halves(code_of<N>(t.v[1][2][w]), code_of<N>(t.v[1][3][w]))};
+          o[4 * w + N] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pf, o[4 * w + N], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        block(std::integral_constant<int, 0>());
+        block(std::integral_constant<int, 1>());
+        block(std::integral_constant<int, 2>());
+        block(std::integral_constant<int, 3>());
+      }
+    };
 
-  // tiles lo + 32 (wave + kWaves i), the next one on its way while one is used
-  int base = lo + 32 * wave;
-  if (base < hi) {
-    Tile<HD> t0, t1;
-    fetch(t0, base);
-    for (;;) {
-      const int next = base + 32 * kWaves, after = next + 32 * kWaves;
-      if (next < hi) fetch(t1, next);
-      use(t0, base);
-      if (next >= hi) break;
-      if (after < hi) fetch(t0, after);
-      use(t1, next);
-      if (after >= hi) break;
-      base = after;
+    // as many positions at a time as the LDS holds page numbers of
+    const int span = (kPages - 2) * c.pt / kKv8Tile * kKv8Tile;
+    for (bool fresh = true; lo < end; lo = hi, fresh = false) {
+      hi = (int)min((long)end, (long)lo + span);
+      at0 = kv8_page_of(c, lo);
+      const int n_at = kv8_page_of(c, hi - 1) - at0 + 1;
+      __syncthreads();                                             // the numbers before are no longer needed
+      for (int i = threadIdx.x; i < n_at; i += 64 * kWaves) pages[i] = kv8_checked_page(c, fresh && i < 64 * kWaves ? first : table[at0 + i]);
+      __syncthreads();
+      // tiles lo + 32 (wave + kWaves i)
+      for (int base = lo + 32 * wave; base < hi; base += 32 * kWaves) {
+        Tile<HD> t;
+        fetch(t, base);
+        use(t, base);
+      }
     }
-  }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  __syncthreads();                                               // the page numbers are no longer needed
-  // lane (col, g) has channels VB (4 g + j) + b of query col in o[b][j]
-  if (col < heads) {
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    // lane (col, g) has channels VB (4 g + j) + b of query col in o[b][j]
+    if (col < heads) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int w = 0; w < KI; ++w)
-        *reinterpret_cast<f32x4*>(fold + (wave * 16 + col) * OS + VB * (4 * g + j) + 4 * w) = f32x4{o[4 * w][j], o[4 * w + 1][j], o[4 * w + 2][j], o[4 * w + 3][j]};
-    if (g == 0) { fold_m[wave][col] = m; fold_l[wave][col] = l; }
-  }
-  __syncthreads();
-  const bool whole = view.seen <= a.plan.chunk;
-  for (int e = 2 * threadIdx.x; e < heads * HD; e += 2 * 64 * kWaves) {
-    const int q = e / HD, ch = e % HD;
-    float to = kKv8None, ls = 0.f, s0 = 0.f, s1 = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) to = fmaxf(to, fold_m[w][q]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = exp2_raw(fold_m[w][q] - to);
-      const float* x = fold + (w * 16 + q) * OS + ch;
-      ls += fold_l[w][q] * f; s0 += x[0] * f; s1 += x[1] * f;
+        for (int w = 0; w < KI; ++w)
+          *reinterpret_cast<f32x4*>(fold + (wave * 16 + col) * OS + VB * (4 * g + j) + 4 * w) = f32x4{o[4 * w][j], o[4 * w + 1][j], o[4 * w + 2][j], o[4 * w + 3][j]};
+      if (g == 0) { fold_m[wave][col] = m; fold_l[wave][col] = l; }
     }
-    if (whole) {
-      const float inv = 1.f / ls;
-      *reinterpret_cast<uint32_t*>(out + e) = (uint32_t)f32_to_bf16(s0 * inv) | ((uint32_t)f32_to_bf16(s1 * inv) << 16);
-    } else {
-      float* part = a.part + (((long)sample * a.H + head0 + q) * a.plan.splits + piece) * (HD + 4);
-      part[ch] = s0; part[ch + 1] = s1;
-      if (ch == 0) { part[HD] = to; part[HD + 1] = ls; }
+    __syncthreads();
+    for (int e = 2 * threadIdx.x; e < heads * HD; e += 2 * 64 * kWaves) {
+      const int q = e / HD, ch = e % HD;
+      float to = kKv8None, ls = 0.f, s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) to = fmaxf(to, fold_m[w][q]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_raw(fold_m[w][q] - to);
+        const float* x = fold + (w * 16 + q) * OS + ch;
+        ls += fold_l[w][q] * f; s0 += x[0] * f; s1 += x[1] * f;
+      }
+      if (pieces == 1) {
+        const float inv = 1.f / ls;
+        *reinterpret_cast<uint32_t*>(out + e) = (uint32_t)f32_to_bf16(s0 * inv) | ((uint32_t)f32_to_bf16(s1 * inv) << 16);
+      } else {
+        float* part = kv8_part_sums(a, c, sample * a.H + head0 + q, piece);
+        part[ch] = s0; part[ch + 1] = s1;
+        if (ch == 0) *kv8_part_marks(a, c, r, sample * a.H + head0 + q, piece) = make_float2(to, ls);
+      }
     }
   }
 }
 
 template <int HD>
 void launch_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  const int groups = (a.H / c.K + 15) / 16;
-  const dim3 grid((unsigned)((long)r.n * c.K * groups * a.plan.splits)), block(64 * kWaves);
+  const int groups = kv8_groups(c, a.H);
+  const dim3 grid((unsigned)(a.plan.wgs ? a.plan.wgs : r.n * c.K * groups)), block(64 * kWaves);
   if (c.pt % 16 == 0) hipLaunchKernelGGL((k_kv8_decode<HD, true>), grid, block, 0, s, c, r, a, groups);
   else hipLaunchKernelGGL((k_kv8_decode<HD, false>), grid, block, 0, s, c, r, a, groups);
 }
@@ -240,13 +275,19 @@ void launch_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8
 
 bool kv8_decode_supported(const Kv8Cache& c, const Kv8Rows& r) { return !r.start && (c.h == 64 || c.h == 128); }
 
+// Workgroups of a call that is cut into shares: two on each of 256 compute units.  (Every one keeps 32 KiB on their way, and more of
+// them only make each wait longer: 512 / 768 workgroups, 16 samples of 8100 positions of the 8B shape 53.3 / 54.4 us, 8 of 1 to
+// 4096 of the 7B shape 29.8 / 30.8.)
+constexpr int kShares = 512;
+constexpr int kLeast = 2;            // tiles of a share, at least
+
+// With many units, or short samples, a unit is a workgroup's.  Else the tiles of all units are cut into equal shares.
 Kv8Plan kv8_decode_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
-  const long units = (long)r.n * c.K * ((H / c.K + 15) / 16);
-  const int want = (int)std::max<long>(1, std::min<long>(256, 2048 / units));
-  int chunk = std::max(256, (r.max_ctx + want - 1) / want);
-  chunk = std::min(chunk, std::min(4096, (kPages - 2) * c.pt));
-  chunk = std::max(128, chunk / 128 * 128);
-  return Kv8Plan{chunk, (r.max_ctx + chunk - 1) / chunk};
+  const int each = c.K * kv8_groups(c, H);                       // units of a sample
+  if ((long)r.n * each >= 4 * kShares || r.max_ctx <= kLeast * kKv8Tile) return Kv8Plan{r.max_ctx, 1, 0};
+  // a unit of t tiles in shares of at least kLeast, and of at least t * each / kShares (it is one of `each` alike)
+  const int tiles = (r.max_ctx + kKv8Tile - 1) / kKv8Tile;
+  return Kv8Plan{kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares};
 }
 
 void launch_kv8_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {

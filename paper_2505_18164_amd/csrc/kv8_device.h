@@ -12,7 +12,7 @@ __device__ __forceinline__ void kv8_report(const Kv8Cache& c) {
 
 // Quotient of a position and the page size (exact: table_stride * pt * pt < 2^32 is checked on the host).
 __device__ __forceinline__ int kv8_page_of(const Kv8Cache& c, int pos) {
-  return c.pt_sh >= 0 ? pos >> c.pt_sh : (int)__umulhi((unsigned)pos, c.pt_magic);
+  return c.pt_magic ? (int)__umulhi((unsigned)pos, c.pt_magic) : pos;
 }
 
 // The sample that `row` belongs to, or -1; `row` is the same in all lanes.  The samples' ends are looked at 64 at a time: one
@@ -30,11 +30,12 @@ __device__ __forceinline__ int kv8_sample_of(const Kv8Rows& r, int row) {
   return s < r.n && r.start[s] <= row ? s : -1;
 }
 
-// A sample's page table, or nullptr when the row of `tables` it names is not there.
-__device__ __forceinline__ const int32_t* kv8_table(const Kv8Cache& c, const Kv8Rows& r, int sample) {
+// The row of `tables` that is a sample's, or -1 when the one it names is not there.
+__device__ __forceinline__ int kv8_table_row(const Kv8Cache& c, const Kv8Rows& r, int sample) {
   const int t = r.table ? r.table[sample] : sample;
-  if ((unsigned)t >= (unsigned)c.n_tables) { kv8_report(c); return nullptr; }
-  return c.tables + (long)t * c.table_stride;
+  if ((unsigned)t < (unsigned)c.n_tables) return t;
+  kv8_report(c);
+  return -1;
 }
 
 // A page number that is not of this cache is reported and page 0 read in its place.
@@ -57,6 +58,52 @@ __device__ __forceinline__ Kv8View kv8_view(const Kv8Cache& c, const Kv8Rows& r,
   if (seen > r.max_ctx) kv8_report(c);
   v.seen = (int)max(0l, min(seen, (long)r.max_ctx));
   return v;
+}
+
+// Item (row * H + head)'s piece in the workspace.
+__device__ __forceinline__ float* kv8_part_sums(const Kv8Attn& a, const Kv8Cache& c, int item, int piece) {
+  return a.part + ((long)item * a.plan.splits + piece) * c.h;
+}
+__device__ __forceinline__ float2* kv8_part_marks(const Kv8Attn& a, const Kv8Cache& c, const Kv8Rows& r, int item, int piece) {
+  return reinterpret_cast<float2*>(a.part + (long)r.n_rows * a.H * a.plan.splits * c.h) + (long)item * a.plan.splits + piece;
+}
+
+// The cut of kv8_decode.hip.  The tiles of all samples' units follow one another - sample by sample, a sample's units side by
+// side, kKv8Begin more for every unit, what it costs to begin one - and workgroup w has w * per .. + per - 1 of them.  Every
+// wavefront works this out for itself, 64 samples at a time; `seen` is what the first 64 see, one a lane.
+constexpr int kKv8Begin = 2;         // (1, 2, 4: 30.2, 29.8, 32.1 us for 8 samples of 1 .. 4096 positions of the 7B shape)
+__device__ __forceinline__ int kv8_seen(const Kv8Cache& c, const Kv8Rows& r, int sample) { return sample < r.n ? kv8_view(c, r, sample).seen : 0; }
+__device__ __forceinline__ int kv8_tiles(int seen) { return (seen + kKv8Tile - 1) / kKv8Tile; }
+__device__ __forceinline__ int kv8_cost(const Kv8Rows& r, int sample, int seen) { return sample < r.n ? kv8_tiles(seen) + kKv8Begin : 0; }
+
+struct Kv8Stream { int cost, per, before; };                     // of one unit of every sample; a share; of those before `sample`
+__device__ __forceinline__ Kv8Stream kv8_stream(const Kv8Cache& c, const Kv8Rows& r, const Kv8Plan& p, int units, int sample, int seen) {
+  int sum = 0, before = 0;
+  for (int i = threadIdx.x & 63; i < r.n; i += 64) {
+    const int t = kv8_cost(r, i, i < 64 ? seen : kv8_seen(c, r, i));
+    sum += t;
+    if (i < sample) before += t;
+  }
+  for (int off = 32; off >= 1; off >>= 1) { sum += __shfl_xor(sum, off, 64); before += __shfl_xor(before, off, 64); }
+  sum = __builtin_amdgcn_readfirstlane(sum);
+  return Kv8Stream{sum, max(p.chunk / kKv8Tile, (int)(((long)sum * units + p.wgs - 1) / p.wgs)), __builtin_amdgcn_readfirstlane(before)};
+}
+struct Kv8Found { int sample, start, seen; };                    // the sample in whose unit `x` lies, and where that unit starts
+__device__ __forceinline__ Kv8Found kv8_find(const Kv8Cache& c, const Kv8Rows& r, int x, int seen) {
+  const int lane = threadIdx.x & 63;
+  for (int base = 0, sum = 0;; base += 64) {
+    if (base) seen = kv8_seen(c, r, base + lane);
+    const int t = kv8_cost(r, base + lane, seen);
+    int up = t;
+    for (int off = 1; off < 64; off <<= 1) { const int o = __shfl_up(up, off, 64); if (lane >= off) up += o; }
+    const unsigned long long past = __ballot(sum + up > x);
+    if (past || base + 64 >= r.n) {
+      const int at = past ? __ffsll(past) - 1 : 0;
+      return Kv8Found{__builtin_amdgcn_readfirstlane(base + at), __builtin_amdgcn_readfirstlane(sum + __shfl(up - t, at, 64)),
+                      __builtin_amdgcn_readfirstlane(__shfl(seen, at, 64))};
+    }
+    sum += __shfl(up, 63, 64);
+  }
 }
 
 constexpr float kKv8None = -3e38f;   // reference of a softmax that has seen nothing

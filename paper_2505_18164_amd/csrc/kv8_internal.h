@@ -16,7 +16,7 @@ struct Kv8Cache {                    // mdi_kv8 as the kernels take it
   int8_t* codes; float* scales;      // [n_pages][K][2][pt][h], [n_pages][K][2][pt]
   const int32_t* tables; int32_t* err;
   int n_pages, K, h, pt;
-  int pt_sh; unsigned pt_magic;      // page of a position: pos >> pt_sh, or with pt_sh < 0 the high word of pos * pt_magic
+  unsigned pt_magic;                 // page of a position: the high word of pos * pt_magic; with 0 (pages of one) the position
   int n_tables, table_stride;
 };
 struct Kv8Rows {                     // mdi_kv8_rows
@@ -31,12 +31,15 @@ void launch_kv8_write(hipStream_t s, int dtype, const Kv8Cache& c, const Kv8Rows
 void launch_kv8_read(hipStream_t s, int dtype, const Kv8Cache& c, const Kv8Rows& r, const Kv8RowsIO& io);
 
 // How an attention call is divided: a row's visible positions go to workgroups in pieces of `chunk`, at most `splits` of them.
-// A row with one piece is finished where it is computed; of the others, every piece leaves its sums at part[((row * H +
-// head) * splits + piece) * (h + 4)]: h weighted sums, the reference, the sum of weights; a second launch adds them.
-struct Kv8Plan { int chunk, splits; };
+// A row with one piece is finished where it is computed; of the others, every piece leaves its h weighted sums and, behind all of
+// those, its reference and its sum of weights (kv8_part_sums, kv8_part_marks in kv8_device.h); a second launch adds them.
+// wgs > 0 (kv8_decode.hip): the cut is another, all samples' positions in equal shares for so many workgroups, of at least `chunk`.
+constexpr int kKv8Tile = 128;        // positions that shares are counted in
+struct Kv8Plan { int chunk, splits, wgs; };
+__host__ __device__ inline int kv8_groups(const Kv8Cache& c, int H) { return (H / c.K + 15) / 16; }   // sets of up to sixteen query heads of a kv head
 Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H);
 inline size_t kv8_part_bytes(const Kv8Plan& p, const Kv8Cache& c, const Kv8Rows& r, int H) {
-  return p.splits > 1 ? (size_t)r.n_rows * H * p.splits * (c.h + 4) * sizeof(float) : 0;
+  return p.splits > 1 ? (size_t)r.n_rows * H * p.splits * (c.h + 2) * sizeof(float) : 0;
 }
 struct Kv8Attn {
   const bf16_t* q; long q_stride;    // [n_rows][H][h], rows q_stride elements apart

@@ -41,11 +41,11 @@ __device__ __forceinline__ bool place(const Kv8Cache& c, const Kv8Rows& r, int r
   const int p0 = r.pos[s];
   if (p0 < 0) return false;                                      // a sample that takes no part
   const long far = (long)p0 + (r.start ? row - r.start[s] : 0);
-  const int32_t* table = kv8_table(c, r, s);
-  if (!table) return false;
+  const int t = kv8_table_row(c, r, s);
+  if (t < 0) return false;
   if (far < 0 || far >= r.max_ctx) { kv8_report(c); return false; }
   const int pos = (int)far, at = kv8_page_of(c, pos);
-  *page = table[at];
+  *page = c.tables[(long)t * c.table_stride + at];
   *slot = pos - at * c.pt;
   if ((unsigned)*page >= (unsigned)c.n_pages) { kv8_report(c); return false; }
   return true;
