@@ -503,8 +503,8 @@ MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, 
  * out: device bf16 [n_rows][n_head][head_dim], rows q_stride / out_stride elements
  * apart, 16-byte aligned, strides multiples of 8; they must not overlap.
  * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
- * binary32.  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head, and
- * n * n_head * (max_ctx / 128 + 1), below 2^31.
+ * binary32.  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
+ * 2^30, n * n_head * (max_ctx / 128 + 1) below 2^31.
  * workspace: mdi_kv8_attn_bytes() bytes of device memory, 16-byte aligned (0 bytes:
  * may be NULL); it carries nothing from one call to the next, and calls that can
  * run at the same time need one each.  Results do not depend on timing.

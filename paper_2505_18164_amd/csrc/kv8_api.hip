@@ -1,5 +1,6 @@
 // The entry points of the 8-bit cache (mdi_kv8_* of mdi.h): checks on the host, then one or two launches.
 #include "kv8_internal.h"
+#include "once_per_device.h"
 
 using namespace mdi;
 
@@ -34,9 +35,11 @@ mdi_status take(const mdi_kv8* k, const mdi_kv8_rows* g, Kv8Cache* c, Kv8Rows* r
 
 // Query rows of the call: heads that the kv heads divide, rows of 16-byte pieces.
 bool good_heads(const Kv8Cache& c, const Kv8Rows& r, uint32_t n_head) {
-  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 31) &&
+  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 30) &&
          (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 1) < (1ull << 31);   // tiles of all units are counted in 32 bits
 }
+
+OncePerDevice g_prompt_lds;          // the kernels that use more than 64 KiB of LDS
 
 mdi_status hip_status() { return hipGetLastError() == hipSuccess ? MDI_OK : MDI_ERR_HIP; }
 
@@ -98,6 +101,10 @@ mdi_status mdi_kv8_attn(const mdi_kv8* cache, const mdi_kv8_rows* rows, const vo
   const size_t need = kv8_part_bytes(plan, c, r, (int)n_head);
   if (need && (!workspace || !aligned16(workspace))) return MDI_ERR_ARG;
   if (need > workspace_bytes) return MDI_ERR_NOMEM;
+  if (kv8_prompt_supported(c, r)) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || !g_prompt_lds.run(dev, kv8_prompt_allow_lds)) return MDI_ERR_HIP;
+  }
   launch_kv8_attn((hipStream_t)hip_stream, c, r,
                   Kv8Attn{(const bf16_t*)q, (long)q_stride, (bf16_t*)out, (long)out_stride, (int)n_head, scale * 1.44269504f, (float*)workspace, plan});
   return hip_status();

@@ -145,6 +145,7 @@ __global__ __launch_bounds__(kBlock) void k_kv8_join(Kv8Cache c, Kv8Rows r, Kv8A
 
 Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
   if (kv8_decode_supported(c, r)) return kv8_decode_plan(c, r, H);
+  if (kv8_prompt_supported(c, r)) return kv8_prompt_plan(c, r, H);
   const long items = (long)r.n_rows * H;
   const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / items));
   int chunk = std::max(256, ((r.max_ctx + want - 1) / want + 63) / 64 * 64);
@@ -154,6 +155,8 @@ Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
 void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
   if (kv8_decode_supported(c, r)) {
     launch_kv8_decode(s, c, r, a);
+  } else if (kv8_prompt_supported(c, r)) {
+    launch_kv8_prompt(s, c, r, a);
   } else {
     int L = 1;
     while (8 * L < c.h) L *= 2;

@@ -51,6 +51,11 @@ struct Kv8Attn {
 bool kv8_decode_supported(const Kv8Cache& c, const Kv8Rows& r);
 Kv8Plan kv8_decode_plan(const Kv8Cache& c, const Kv8Rows& r, int H);
 void launch_kv8_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
+// Packed rows with heads of 64 or 128: on the matrix cores (kv8_prompt.hip).  kv8_prompt_allow_lds: once per device, with it current.
+bool kv8_prompt_supported(const Kv8Cache& c, const Kv8Rows& r);
+bool kv8_prompt_allow_lds();
+Kv8Plan kv8_prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H);
+void launch_kv8_prompt(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
 void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a);
 
 }  // namespace mdi
