@@ -16,7 +16,7 @@ mdi_status take_cache(const mdi_kv8* k, Kv8Cache* c) {
   if ((uint64_t)k->table_stride * k->page_tokens > 1u << 30 || (uint64_t)k->table_stride * k->page_tokens * k->page_tokens >= (1ull << 32)) return MDI_ERR_ARG;
   const int pt = (int)k->page_tokens;
   *c = Kv8Cache{k->codes, k->scales, k->tables, k->err, (int)k->n_pages, (int)k->n_kv_head, (int)k->head_dim, pt,
-                pt == 1 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u, (int)k->n_tables, (int)k->table_stride};
+                pt == 1 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u, pt == 1 ? ~0u : 0u, (int)k->n_tables, (int)k->table_stride};
   return MDI_OK;
 }
 

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kBlock) void k_kv8_attn(Kv8Cache c, Kv8Rows r, Kv8A
   float m = kKv8None, l = 0.f;
   for (int t0 = lo + wave * tpw; t0 < hi; t0 += 4 * tpw) {
     const int pos = min(t0 + sub, hi - 1), at = kv8_page_of(c, pos);
-    const long rk = ((long)kv8_checked_page(c, table[at]) * c.K + kv) * 2 * c.pt + (pos - at * c.pt), rv = rk + c.pt;
+    const long rk = kv8_row(c, kv8_checked_page(c, table[at]), kv, pos), rv = rk + c.pt;
     const uint2 kc = live ? *reinterpret_cast<const uint2*>(c.codes + rk * h + ch) : make_uint2(0, 0);
     const uint2 vc = live ? *reinterpret_cast<const uint2*>(c.codes + rv * h + ch) : make_uint2(0, 0);
     const float ks = c.scales[rk], vs = c.scales[rv];

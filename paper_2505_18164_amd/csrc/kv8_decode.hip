@@ -101,16 +101,14 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
     int hi = lo;
 
     auto row_of = [&](int pos) __attribute__((always_inline)) {     // the key's row; the value's is pt further
-      const int at = kv8_page_of(c, pos);
-      return ((long)pages[at - at0] * c.K + kv) * 2 * c.pt + (pos - at * c.pt);
+      return kv8_row(c, pages[kv8_page_of(c, pos) - at0], kv, pos);
     };
     auto fetch = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         if constexpr (kWhole16) {
-          const int p16 = min(base + 16 * u, (hi - 1) & ~15), at = kv8_page_of(c, p16);
-          const int page = __builtin_amdgcn_readfirstlane(pages[at - at0]);
-          const long row = ((long)page * c.K + kv) * 2 * c.pt + (p16 - at * c.pt);
+          const int p16 = min(base + 16 * u, (hi - 1) & ~15);
+          const long row = kv8_row(c, __builtin_amdgcn_readfirstlane(pages[kv8_page_of(c, p16) - at0]), kv, p16);
           // one uniform address each and 32-bit offsets of the lanes
           const char* kp = (const char*)c.codes + row * HD;
           const char* vp = kp + (long)c.pt * HD;

@@ -12,7 +12,12 @@ __device__ __forceinline__ void kv8_report(const Kv8Cache& c) {
 
 // Quotient of a position and the page size (exact: table_stride * pt * pt < 2^32 is checked on the host).
 __device__ __forceinline__ int kv8_page_of(const Kv8Cache& c, int pos) {
-  return c.pt_magic ? (int)__umulhi((unsigned)pos, c.pt_magic) : pos;
+  return (int)(__umulhi((unsigned)pos, c.pt_magic) | ((unsigned)pos & c.pt_one));
+}
+
+// The key of position pos in `page`, as a row of codes or an index of scales; its value is c.pt further.
+__device__ __forceinline__ long kv8_row(const Kv8Cache& c, unsigned page, int kv, int pos) {
+  return (long)((uint64_t)page * (unsigned)(2 * c.K * c.pt) + (unsigned)(2 * kv * c.pt + pos - kv8_page_of(c, pos) * c.pt));
 }
 
 // The sample that `row` belongs to, or -1; `row` is the same in all lanes.  The samples' ends are looked at 64 at a time: one
@@ -30,12 +35,16 @@ __device__ __forceinline__ int kv8_sample_of(const Kv8Rows& r, int row) {
   return s < r.n && r.start[s] <= row ? s : -1;
 }
 
-// The row of `tables` that is a sample's, or -1 when the one it names is not there.
-__device__ __forceinline__ int kv8_table_row(const Kv8Cache& c, const Kv8Rows& r, int sample) {
-  const int t = r.table ? r.table[sample] : sample;
+// A row of `tables`, or -1 when it is not there.
+__device__ __forceinline__ int kv8_checked_row(const Kv8Cache& c, int t) {
   if ((unsigned)t < (unsigned)c.n_tables) return t;
   kv8_report(c);
   return -1;
+}
+
+// The row of `tables` that is a sample's, or -1 when the one it names is not there.
+__device__ __forceinline__ int kv8_table_row(const Kv8Cache& c, const Kv8Rows& r, int sample) {
+  return kv8_checked_row(c, r.table ? r.table[sample] : sample);
 }
 
 // A page number that is not of this cache is reported and page 0 read in its place.

@@ -16,7 +16,7 @@ struct Kv8Cache {                    // mdi_kv8 as the kernels take it
   int8_t* codes; float* scales;      // [n_pages][K][2][pt][h], [n_pages][K][2][pt]
   const int32_t* tables; int32_t* err;
   int n_pages, K, h, pt;
-  unsigned pt_magic;                 // page of a position: the high word of pos * pt_magic; with 0 (pages of one) the position
+  unsigned pt_magic, pt_one;         // page of a position: the high word of pos * pt_magic, or (pages of one) the position & pt_one
   int n_tables, table_stride;
 };
 struct Kv8Rows {                     // mdi_kv8_rows

@@ -1,7 +1,8 @@
 // Causal attention of packed rows - prompts, or the next pieces of prompts, of several samples - over the 8-bit cache, on the
 // matrix cores.
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
+#include <type_traits>
 
 #include "kv8_mfma.h"
 
@@ -25,12 +26,13 @@ __device__ __forceinline__ Span rows_of(const Kv8Rows& r, int i) {
 }
 
 // The sample that has block x, counting BP positions a block, and which of its blocks that is; sample < 0: there are fewer.
-struct BlockPlace { int sample, block, first, rows; };
+struct BlockPlace { int sample, block, first, rows, pos, table; };
 template <int BQ>
 __device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int g_sh) {
   const int lane = threadIdx.x & 63, bp = BQ >> g_sh;
   for (int base = 0, sum = 0; base < r.n; base += 64) {
-    const Span s = base + lane < r.n ? rows_of(r, base + lane) : Span{0, 0};
+    const int i = min(base + lane, r.n - 1), pos = r.pos[i], table = r.table ? r.table[i] : i;   // (asked for along with the rows)
+    const Span s = base + lane < r.n ? rows_of(r, i) : Span{0, 0};
     const int t = (s.end - s.first + bp - 1) / bp;
     int up = t;
     for (int off = 1; off < 64; off <<= 1) { const int o = __shfl_up(up, off, 64); if (lane >= off) up += o; }
@@ -38,38 +40,41 @@ __device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int g_sh
     if (past) {
       const int at = __ffsll(past) - 1;
       return BlockPlace{__builtin_amdgcn_readfirstlane(base + at), __builtin_amdgcn_readfirstlane(x - (sum + __shfl(up - t, at, 64))),
-                        __builtin_amdgcn_readfirstlane(__shfl(s.first, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(s.end - s.first, at, 64))};
+                        __builtin_amdgcn_readfirstlane(__shfl(s.first, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(s.end - s.first, at, 64)),
+                        __builtin_amdgcn_readfirstlane(__shfl(pos, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(table, at, 64))};
     }
     sum += __shfl(up, 63, 64);
   }
-  return BlockPlace{-1, 0, 0, 0};
+  return BlockPlace{-1, 0, 0, 0, 0, 0};
 }
 
 struct PromptGeo { int n_blocks, sets, g_sh; };                  // bound of the blocks of all samples; sets of 2^g_sh query heads
 
-template <int HD, int NG, int WQ>
-__global__ __launch_bounds__(WQ * 64 * NG, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv8Attn a, PromptGeo geo) {
-  constexpr int BQ = 32 * WQ, GT = 64 * WQ;                      // rows of a workgroup - (position, head) pairs -, threads of a group
+// A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
+// kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.
+template <int HD, int NG, bool kWhole>
+__global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv8Attn a, PromptGeo geo) {
+  constexpr int WQ = 8 / NG, BQ = 32 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
   constexpr int KS = HD + 8, VR = HD + 32, HT = HD / 32;
   constexpr int UB = 64 * HD / GT < 16 ? 64 * HD / GT : 16;      // codes a thread moves at a time
   constexpr int KU = 64 * HD / (GT * UB), PER = HD / UB;         // ... and how often; threads a key
-  constexpr int KV = BK * KS + BK * VR + 4 * BK;                 // bf16 elements of a buffer: keys, values, their scales
-  constexpr int NB = NG == 4 ? 1 : 2;
+  constexpr int NB = 2;                                          // buffers of keys, and of values
+  constexpr int KV = NB * BK * (KS + VR) + 8 * BK;               // bf16 elements of a group: keys, values, scales of four blocks of keys
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int tid = threadIdx.x & (GT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int grp = NG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GT);
-  bf16_t* bufs = (bf16_t*)smem + grp * NB * KV;
-  // Workgroups are handed to the eight compute dies in turn, each with an L2 of its own: a die takes sets that follow each
-  // other (sets share keys), a sample's longest rows first.
-  const int total = geo.n_blocks * geo.sets, per_die = (total + 7) >> 3, idx = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_die || idx >= total) return;
-  const int set = idx / geo.n_blocks;
-  const BlockPlace at = place_of<BQ>(r, idx - set * geo.n_blocks, geo.g_sh);
+  const int grp = NG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GT), late = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  bf16_t* const Kb = (bf16_t*)smem + grp * KV;
+  bf16_t* const Vb = Kb + NB * BK * KS;
+  float* const Sc = (float*)(Vb + NB * BK * VR);                 // [4][64]
+  // A sample's longest rows first, and of those all sets.  (Workgroups are handed to the eight compute dies, each with an L2 of its
+  // own, in turn: with a multiple of eight sets, a set stays on its die.)
+  const int block = blockIdx.x / geo.sets, set = blockIdx.x - block * geo.sets;
+  const BlockPlace at = place_of<BQ>(r, block, geo.g_sh);
   if (at.sample < 0) return;
   const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
   const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
-  const int which = __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, at.sample)), p0 = __builtin_amdgcn_readfirstlane(r.pos[at.sample]);
+  const int which = kv8_checked_row(c, at.table), p0 = at.pos;
   const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
   const int col = lane & 31, half = lane >> 5;
   const int row = q0 + ((32 * wave + col) >> g_sh), head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
@@ -101,160 +106,247 @@ __global__ __launch_bounds__(WQ * 64 * NG, 2) void k_kv8_prompt(Kv8Cache c, Kv8R
   for (int i = 0; i < HT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = kKv8None, l = 0.f;
+  float m = 0.f, l = 0.f;
+  bool first = true;                                             // no block yet: scores are counted from zero
   const int wave_pos = (int)min((long)p0 + q0 + ((32 * wave) >> g_sh), (long)r.max_ctx - 1);   // of the wavefront's first row
 
+  // Staging.  A thread moves UB channels of KU keys: those of block j along with the values of block j - 1.
   const int n_kb = (hi - lo + BK - 1) / BK, n_it = (n_kb + NG - 1) / NG;
   u32x4 kreg[KU], vreg[KU];
-  int pg[KU], pgs;
-  float sreg;
-  auto key_of = [&](int kb, int in) __attribute__((always_inline)) { return min(lo + kb * BK + in, hi - 1); };   // keys past the last repeat it
-  auto pages = [&](int kb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < KU; ++j) pg[j] = table[kv8_page_of(c, key_of(kb, (tid + j * GT) / PER))];
-    pgs = table[kv8_page_of(c, key_of(kb, tid & 63))];
+  float vs[KU], sk = 0.f, sv = 0.f;
+  unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
+  auto checked = [&](int page) __attribute__((always_inline)) {
+    worst = max(worst, (unsigned)page);
+    return min((unsigned)page, (unsigned)c.n_pages - 1);
   };
-  auto row_at = [&](int page, int key) __attribute__((always_inline)) {
-    return ((long)kv8_checked_page(c, page) * c.K + kv) * 2 * c.pt + (key - kv8_page_of(c, key) * c.pt);
+  auto block_at = [&](int j) __attribute__((always_inline)) { return lo + (NG * j + grp) * BK; };
+  auto take = [&](const char* codes, uint32_t off) __attribute__((always_inline)) {
+    if constexpr (UB == 16) return *reinterpret_cast<const u32x4*>(codes + off);
+    const u32x2 x = *reinterpret_cast<const u32x2*>(codes + off);
+    return u32x4{x.x, x.y, 0, 0};
   };
-  auto fetch = [&](int kb) __attribute__((always_inline)) {
+  // fetch(j) asks for block j's keys and block j - 1's values (whose places it was left by the one before) and for block j + 1's page numbers.
+  int pg[kWhole ? 1 : KU + 1];
+  long k_row[kWhole ? 1 : KU] = {};                              // rows of the cache
+  int k_last = 0;                                                // positions of the block but the first
+  auto pages = [&](int j) __attribute__((always_inline)) {
+    if constexpr (kWhole) {
+      int at = kv8_page_of(c, min(block_at(j), hi - 1));
+      asm volatile("" : "+v"(at));                               // a vector load: behind a scalar one every read of LDS would have to wait for it
+      pg[0] = table[at];
+    } else {
 #pragma unroll
-    for (int j = 0; j < KU; ++j) {
-      const int u = tid + j * GT;
-      const int8_t* kp = c.codes + row_at(pg[j], key_of(kb, u / PER)) * HD + UB * (u % PER);
-      const int8_t* vp = kp + (long)c.pt * HD;
-      if constexpr (UB == 16) {
-        kreg[j] = *reinterpret_cast<const u32x4*>(kp);
-        vreg[j] = *reinterpret_cast<const u32x4*>(vp);
-      } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(kp), y = *reinterpret_cast<const u32x2*>(vp);
-        kreg[j] = u32x4{x.x, x.y, 0, 0};
-        vreg[j] = u32x4{y.x, y.y, 0, 0};
+      for (int u = 0; u <= KU; ++u) pg[u] = table[kv8_page_of(c, min(block_at(j) + (u < KU ? (tid + u * GT) / PER : lane), hi - 1))];
+    }
+  };
+  auto fetch = [&](int j) __attribute__((always_inline)) {
+    const int k0 = min(block_at(j), hi - 1);                     // keys past the last repeat it
+    if constexpr (kWhole) {
+      const long v_row = k_row[0] + c.pt;
+      const int v_last = k_last;
+      k_row[0] = kv8_row(c, __builtin_amdgcn_readfirstlane((int)checked(pg[0])), kv, k0);
+      k_last = min(BK, hi - k0) - 1;
+      const char* const kp = (const char*)c.codes + k_row[0] * HD;
+      const char* const vp = (const char*)c.codes + v_row * HD;
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int at = tid + u * GT, key = at / PER, ch = UB * (at % PER);
+        kreg[u] = take(kp, (uint32_t)(min(key, k_last) * HD + ch));
+        if (j > 0) {
+          vreg[u] = take(vp, (uint32_t)(min(key, v_last) * HD + ch));
+          vs[u] = *reinterpret_cast<const float*>((const char*)(c.scales + v_row) + 4u * min(key, v_last));
+        }
+      }
+      if (wave == 0) {
+        const char* const sp = (const char*)(c.scales + k_row[0]);
+        const uint32_t off = 4u * min(lane, k_last);
+        sk = *reinterpret_cast<const float*>(sp + off);
+        sv = *reinterpret_cast<const float*>(sp + 4l * c.pt + off);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int at = tid + u * GT, ch = UB * (at % PER);
+        const long v_row = k_row[u] + c.pt;
+        k_row[u] = kv8_row(c, checked(pg[u]), kv, min(block_at(j) + at / PER, hi - 1));
+        kreg[u] = take((const char*)c.codes + k_row[u] * HD, ch);
+        if (j > 0) {
+          vreg[u] = take((const char*)c.codes + v_row * HD, ch);
+          vs[u] = c.scales[v_row];
+        }
+      }
+      if (wave == 0) {
+        const long row = kv8_row(c, checked(pg[KU]), kv, min(block_at(j) + lane, hi - 1));
+        sk = c.scales[row];
+        sv = c.scales[row + c.pt];
       }
     }
-    sreg = tid < 128 ? c.scales[row_at(pgs, key_of(kb, tid & 63)) + (tid < 64 ? 0 : c.pt)] : 0.f;
-    pages(kb + NG);
+    pages(j + 1);
   };
-  auto widen = [&](bf16_t* to, const u32x4& x) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < UB / 8; ++h) {
-      const uint32_t w0 = x[2 * h], w1 = x[2 * h + 1];
-      *reinterpret_cast<u32x4*>(to + 8 * h) = u32x4{high_halves(code_of<0>(w0), code_of<1>(w0)), high_halves(code_of<2>(w0), code_of<3>(w0)),
-                                                    high_halves(code_of<0>(w1), code_of<1>(w1)), high_halves(code_of<2>(w1), code_of<3>(w1))};
-    }
+  // What has been asked for is looked at here and not before: a shift that is moved up to the load waits for it there.
+  auto here = [](uint32_t w) __attribute__((always_inline)) { asm volatile("" : "+v"(w)); return w; };
+  constexpr int kUnits = UB / 8 * KU;                            // eight codes of a key each
+  auto stash_keys = [&](int j, int n) __attribute__((always_inline)) {
+    const int u = n / (UB / 8), h = n % (UB / 8), at = tid + u * GT;
+    const uint32_t w0 = here(kreg[u][2 * h]), w1 = here(kreg[u][2 * h + 1]);
+    *reinterpret_cast<u32x4*>(Kb + (j & 1) * BK * KS + at / PER * KS + UB * (at % PER) + 8 * h) =
+        u32x4{high_halves(code_of<0>(w0), code_of<1>(w0)), high_halves(code_of<2>(w0), code_of<3>(w0)),
+              high_halves(code_of<0>(w1), code_of<1>(w1)), high_halves(code_of<2>(w1), code_of<3>(w1))};
   };
-  auto stash = [&](bf16_t* Ks) __attribute__((always_inline)) {
-    bf16_t* Vs = Ks + BK * KS;
-    float* sc = (float*)(Vs + BK * VR);
-#pragma unroll
-    for (int j = 0; j < KU; ++j) {
-      const int u = tid + j * GT, key = u / PER, ch = UB * (u % PER);
-      widen(Ks + key * KS + ch, kreg[j]);
-      widen(Vs + key * VR + ch, vreg[j]);
-    }
-    if (tid < 128) sc[tid] = tid < 64 ? sreg * a.scale : sreg;
+  auto stash_values = [&](int j, int n) __attribute__((always_inline)) {
+    const int u = n / (UB / 8), h = n % (UB / 8), at = tid + u * GT;
+    const float f = __uint_as_float(here(__float_as_uint(vs[u]))), by = f - f == 0.f ? f : 0.f;
+    const uint32_t w0 = here(vreg[u][2 * h]), w1 = here(vreg[u][2 * h + 1]);
+    *reinterpret_cast<bf16x8*>(Vb + ((j - 1) & 1) * BK * VR + at / PER * VR + UB * (at % PER) + 8 * h) =
+        bf16x8{(__bf16)(code_of<0>(w0) * by), (__bf16)(code_of<1>(w0) * by), (__bf16)(code_of<2>(w0) * by), (__bf16)(code_of<3>(w0) * by),
+               (__bf16)(code_of<0>(w1) * by), (__bf16)(code_of<1>(w1) * by), (__bf16)(code_of<2>(w1) * by), (__bf16)(code_of<3>(w1) * by)};
+  };
+  auto stash_scales = [&](int j) __attribute__((always_inline)) {
+    const float v = __uint_as_float(here(__float_as_uint(sv)));
+    if (wave == 0) Sc[64 * (j & 3) + lane] = v - v == 0.f ? sk * a.scale : __uint_as_float(0x7FC00000u);   // a value that is not finite makes its weight NaN (and is staged as zeros)
   };
 
   const int v_lane = (4 * half + ((lane & 15) >> 2)) * VR + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  pages(grp);
-  fetch(grp);
-  stash(bufs);
-  __syncthreads();
-  for (int it = 0; it < n_it; ++it) {
-    const int kb = NG * it + grp;
-    const bf16_t* Ks = bufs + (NB == 2 ? it & 1 : 0) * KV;
-    const bf16_t* Vs = Ks + BK * KS;
-    const float* sc = (const float*)(Vs + BK * VR);
-    if (it + 1 < n_it) fetch(kb + NG);
-    const int k0 = lo + kb * BK;
-    const int last_pos = min(wave_pos + (31 >> g_sh), n_seen - 1);
-    if (kb < n_kb && k0 <= last_pos) {                           // else: no block, or this wavefront's rows see none of these keys
-      f32x16 s[2], x[2];
+  const int last_pos = min(wave_pos + (31 >> g_sh), n_seen - 1);
+  auto sees = [&](int j) __attribute__((always_inline)) { return NG * j + grp < n_kb && lo + (NG * j + grp) * BK <= last_pos; };   // some row of the wavefront, some key of the block
+  f32x16 s[2];
+  u32x4 pf[4] = {};                                              // weights, two a word
+  // The products of a step: the values of block j - 1 with its weights, the keys of block j with the queries.  Four operands are
+  // on their way from the LDS while the four before them are multiplied.
+  auto products = [&](int j, auto keys) __attribute__((always_inline)) {
+    constexpr int kSets = decltype(keys)::value ? 2 * HT : HT;   // sets of four operands: HT of values, HT of keys
+    const bf16_t* const V = Vb + ((j - 1) & 1) * BK * VR + v_lane;
+    const bf16_t* const K = Kb + (j & 1) * BK * KS + col * KS + 8 * half;
+    u32x4 f[2][4];
+    auto read = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-        const bf16_t* kr = Ks + (32 * t + col) * KS + 8 * half;
-#pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks)
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kr + 16 * ks), qf[ks], s[t], 0, 0, 0);
+      for (int x = 0; x < 4; ++x) {
+        if (n < HT) {
+          const bf16_t* const at = V + 16 * ((4 * n + x) / HT) * VR + 32 * (x % HT);
+          const u32x2 b0 = read_transposed(at), b1 = read_transposed(at + 8 * VR);
+          f[n & 1][x] = u32x4{b0.x, b0.y, b1.x, b1.y};
+        } else {
+          f[n & 1][x] = *reinterpret_cast<const u32x4*>(K + 32 * (x & 1) * KS + 16 * (2 * (n - HT) + (x >> 1)));
+        }
       }
-      const bool masked = k0 + BK - 1 > wave_pos || k0 + BK > hi;
-      auto count = [&]() __attribute__((always_inline)) {        // scores counted from m, and the largest
-        float top = -INFINITY;
+    };
+    read(0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < kSets; ++n) {
+      if (n + 1 < kSets) read(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 32 * t + 8 * g + 4 * half);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[t][4 * g + j] = fmaf(s[t][4 * g + j], ks[j], -m);
-          }
-        if (masked)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int key = k0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
-              if (key > pos || key >= hi) x[t][e] = -INFINITY;
-            }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmaxf(top, x[t][e]);
-        return top;
-      };
-      float top = count();
-      if (__any(top > kKv8Raise)) {
-        // the largest score itself, not counted from an m that may lie far from it
-        const float was = m;
-        m = 0.f;
-        top = count();
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        m = fmaxf(was, top);
-        const float alpha = exp2_raw(was - m);
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < HT; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-        count();
+      for (int x = 0; x < 4; ++x) {
+        const bf16x8 op = __builtin_bit_cast(bf16x8, f[n & 1][x]);
+        if (n < HT) {
+          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, __builtin_bit_cast(bf16x8, pf[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
+        } else {
+          const int k = 2 * (n - HT) + (x >> 1);
+          s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[k], k ? s[x & 1] : f32x16{}, 0, 0, 0);
+        }
       }
+      if constexpr (decltype(keys)::value) {                     // staging, in between
+        constexpr int kPer = (kUnits + HT - 1) / HT;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int x = n % HT * kPer + i;
+          if (x < kUnits) { if (n < HT) stash_keys(j + 1, x); else stash_values(j + 1, x); }
+        }
+        if (n == 2 * HT - 1) { stash_scales(j + 1); fetch(j + 2); }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // The weights of block j from its scores.  They are counted from m, the row's reference, which is the largest score of the first
+  // block and is raised - in both lanes of a row alike - when a score exceeds it by 2^kKv8Raise: the sum is divided out at
+  // the end, so any reference near the largest score does.  The sum takes the weights as they are multiplied, rounded to bf16.
+  float alpha = 1.f;
+  bool raised = false;
+  auto weigh = [&](int j, auto mask) __attribute__((always_inline)) {
+    constexpr bool kMask = decltype(mask)::value;                // some of these keys are not for some of the rows
+    const int pos_in = min(pos, hi - 1) - (lo + (NG * j + grp) * BK) - 4 * half;   // what the lane's row sees of the block
+    const float* const sc = Sc + 64 * (j & 3) + 4 * half;
+    float top = kKv8None;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 k = *reinterpret_cast<const f32x4*>(sc + 32 * t + 8 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 4 * g + i;
+          s[t][e] = fmaf(s[t][e], k[i], -m);
+          if (kMask && 32 * t + 8 * g + i > pos_in) s[t][e] = -INFINITY;
+          top = fmaxf(top, s[t][e]);
+        }
+      }
+    if (__builtin_expect(first || __any(top > kKv8Raise), 0)) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float by = first ? top : fmaxf(top, 0.f);
+      alpha = first ? 1.f : exp2_raw(-by);
+      raised = !first;
+      m += by;
+      first = false;
+      l *= alpha;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int pp = 0; pp < 2; ++pp) {
-          bf16x8 pf;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const f32x4 vs = *reinterpret_cast<const f32x4*>(sc + BK + 32 * t + 16 * pp + 8 * g + 4 * half);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int e = 8 * pp + 4 * g + j;
-              const float p = exp2_raw(x[t][e]);
-              l += p;
-              float w = p * vs[j];
-              if (masked) {
-                const int key = k0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
-                if (key > pos || key >= hi) w = 0.f;             // whatever its scale is
-              }
-              pf[4 * g + j] = (__bf16)w;
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < HT; ++i) {
-            const bf16_t* vr = Vs + v_lane + (32 * t + 16 * pp) * VR + 32 * i;
-            const u32x2 b0 = read_transposed(vr), b1 = read_transposed(vr + 8 * VR);
-            const u32x4 vf = {b0.x, b0.y, b1.x, b1.y};
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[i], 0, 0, 0);
-          }
-        }
+        for (int e = 0; e < 16; ++e) s[t][e] -= by;
     }
-    if (NB == 1) __syncthreads();
-    if (it + 1 < n_it) stash(bufs + (NB == 2 ? (it + 1) & 1 : 0) * KV);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const bf16x2 w = {(__bf16)exp2_raw(s[t][e]), (__bf16)exp2_raw(s[t][e + 1])};
+        l = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+        pf[2 * t + (e >> 3)][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+      }
+  };
+  auto soften = [&](int j) __attribute__((always_inline)) {
+    if (!sees(j)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) pf[t] = u32x4{0, 0, 0, 0};
+      return;
+    }
+    const int k0 = lo + (NG * j + grp) * BK;
+    if (k0 + BK - 1 > wave_pos || k0 + BK > hi) weigh(j, std::true_type()); else weigh(j, std::false_type());
+  };
+
+  // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies and stages, the other takes exponentials; so the later
+  // four are one turn behind.  Block j + 1's keys and block j's values, which both stage in turn j, go over blocks that both have left.
+  pages(0);
+  fetch(0);
+#pragma unroll
+  for (int n = 0; n < kUnits; ++n) stash_keys(0, n);
+  stash_scales(0);
+  fetch(1);
+  // (the first step has no values yet: its weights are zeros, and so is what they multiply)
+  for (int i = tid; i < BK * VR / 8; i += GT) *reinterpret_cast<u32x4*>(Vb + BK * VR + 8 * i) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+  if (late) __syncthreads();
+  for (int j = 0; j < n_it; ++j) {
+    products(j, std::true_type());
+    __syncthreads();
+    soften(j);
+    if (__builtin_expect(raised, 0)) {
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x = o[i][e] * alpha;
+          asm volatile("" : "+v"(x));                            // (one after the other, in place: else they are copied, and others spilled)
+          o[i][e] = x;
+        }
+      raised = false;
+    }
     __syncthreads();
   }
+  products(n_it, std::false_type());
+  if (!late) __syncthreads();
+  __syncthreads();
+  if (first) m = kKv8None;                                       // saw nothing
 
+  if (worst >= (unsigned)c.n_pages) kv8_report(c);
   if constexpr (NG > 1) {
     float* fold = (float*)smem + (grp > 0 ? grp - 1 : 0) * (HT * 16 + 2) * GT;
     if (grp > 0) {
@@ -303,19 +395,20 @@ __global__ __launch_bounds__(WQ * 64 * NG, 2) void k_kv8_prompt(Kv8Cache c, Kv8R
   }
 }
 
-template <int HD, int NG, int WQ>
+template <int HD, int NG>
 constexpr size_t prompt_lds() {
-  const size_t kv = (size_t)NG * (NG == 4 ? 1 : 2) * (BK * (HD + 8 + HD + 32) + 4 * BK) * sizeof(bf16_t);
-  const size_t fold = NG > 1 ? (size_t)(NG - 1) * (HD / 2 + 2) * 64 * WQ * sizeof(float) : 0;
+  const size_t kv = (size_t)NG * (2 * BK * (HD + 8 + HD + 32) + 8 * BK) * sizeof(bf16_t);
+  const size_t fold = (size_t)(NG - 1) * (HD / 2 + 2) * (512 / NG) * sizeof(float);
   return kv > fold ? kv : fold;
 }
-template <int HD, int NG, int WQ>
+template <int HD, int NG>
 bool allow_one() {                                               // 64 KiB is what a kernel gets by default
-  constexpr size_t lds = prompt_lds<HD, NG, WQ>();
-  return lds <= 64 * 1024 || hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, WQ>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
+  constexpr size_t lds = prompt_lds<HD, NG>();
+  return lds <= 64 * 1024 || (hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess &&
+                              hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess);
 }
 template <int HD>
-bool allow_heads() { return allow_one<HD, 1, 8>() && allow_one<HD, 2, 4>() && allow_one<HD, 4, 2>() && allow_one<HD, 1, 4>(); }
+bool allow_heads() { return allow_one<HD, 1>() && allow_one<HD, 2>(); }
 
 // Query heads of a kv head that a workgroup's rows take together: the largest power of two that divides their number, up to 32.
 int heads_shift(const Kv8Cache& c, int H) {
@@ -328,25 +421,43 @@ PromptGeo geo_of(const Kv8Cache& c, const Kv8Rows& r, int H, int WQ) {
   const int sh = heads_shift(c, H), bp = 32 * WQ >> sh;
   return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh};
 }
-struct Shape { int groups, waves; };
-Shape shape_of(const Kv8Cache& c, const Kv8Rows& r, int H) {
-  if (const char* e = getenv("KV8_SHAPE")) return Shape{e[0] - '0', e[1] - '0'};
-  return Shape{1, 8};
+// Groups of a workgroup and pieces of a row's positions.  A step of 64 NG keys takes `step` us, a workgroup six or seven more to begin
+// and end; what is divided is added by a second launch, whose workgroups - one per row and head - are most of what a division of
+// many rows costs.  How long the single samples are is on the device: they are taken for equal.  Measured, us, undivided with 1 / 2
+// groups: a prompt of 512, 1024, 2048 of the 7B shape 27.8/21.4, 45.3/33.0, 81.3/69.9, four of 512 31.6/39.8, sixteen of 64 20.0/23.0,
+// eight of 333 of TinyLlama 26.2/30.5, one of 1500 44.3/30.0; four pieces of 64 behind 8000 of the 8B shape 264/165, in 4 parts
+// 97/74, in 8 70/84; the prompt of 1024 in two parts 76/80.
+struct PromptPlan { int groups, splits; };
+PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
+  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
+  const double heads = (double)r.n_rows * H, seen = r.max_ctx - 0.5 * std::min(r.max_ctx, rows);   // what a row sees, on average
+  PromptPlan best{1, 1};
+  double best_us = 1e30;
+  for (int ng = 1; ng <= 2; ++ng) {
+    const int sh = heads_shift(c, H), bp = 256 / ng >> sh;
+    const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.15 : 2.65) : (ng == 1 ? 1.45 : 1.65);
+    for (int s = 1; s <= 32; s *= 2) {
+      if (s > 1 && r.max_ctx < 256 * s) break;
+      const double longest = std::ceil(r.max_ctx / (64. * ng * s)), all = items * seen / (64. * ng * 256);
+      double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
+      if (s > 1) us += 6 + heads / 800 + heads * s * c.h / 5e5;
+      if (us < best_us) { best_us = us; best = PromptPlan{ng, s}; }
+    }
+  }
+  return best;
 }
 
-template <int HD, int NG, int WQ>
-void launch_shape(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  const PromptGeo g = geo_of(c, r, a.H, WQ);
+template <int HD, int NG>
+void launch_groups(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
+  const PromptGeo g = geo_of(c, r, a.H, 8 / NG);
   const long total = (long)g.n_blocks * g.sets;
-  hipLaunchKernelGGL((k_kv8_prompt<HD, NG, WQ>), dim3((unsigned)(8 * ((total + 7) / 8)), a.plan.splits), dim3(64 * WQ * NG), (prompt_lds<HD, NG, WQ>()), s, c, r, a, g);
+  const dim3 grid((unsigned)total, a.plan.splits);
+  if (c.pt % BK == 0) hipLaunchKernelGGL((k_kv8_prompt<HD, NG, true>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+  else hipLaunchKernelGGL((k_kv8_prompt<HD, NG, false>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
 }
 template <int HD>
 void launch_heads(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  const Shape p = shape_of(c, r, a.H);
-  if (p.groups == 1 && p.waves == 8) launch_shape<HD, 1, 8>(s, c, r, a);
-  else if (p.groups == 1) launch_shape<HD, 1, 4>(s, c, r, a);
-  else if (p.groups == 2) launch_shape<HD, 2, 4>(s, c, r, a);
-  else launch_shape<HD, 4, 2>(s, c, r, a);
+  if (prompt_plan(c, r, a.H).groups == 1) launch_groups<HD, 1>(s, c, r, a); else launch_groups<HD, 2>(s, c, r, a);
 }
 
 }  // namespace
@@ -355,8 +466,7 @@ bool kv8_prompt_supported(const Kv8Cache& c, const Kv8Rows& r) { return r.start 
 bool kv8_prompt_allow_lds() { return allow_heads<64>() && allow_heads<128>(); }
 
 Kv8Plan kv8_prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
-  const char* e = getenv("KV8_SPLIT");
-  const int want = e ? atoi(e) : 1;
+  const int want = prompt_plan(c, r, H).splits;
   const int chunk = ((r.max_ctx + want - 1) / want + BK - 1) / BK * BK;
   return Kv8Plan{chunk, (r.max_ctx + chunk - 1) / chunk, 0};
 }
