@@ -366,9 +366,11 @@ class Partition:
             pass
 
 
-def _stride(t, dim, alone):
-    """Elements between neighbours along `dim`; a dimension of one has none, whatever the tensor says: `alone`."""
-    return t.stride(dim) if t.shape[dim] > 1 else alone
+# the current stream of a GPU as a number: torch's own way to it where there is one (a Stream object costs 2 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_KV8_TYPES = {torch.bfloat16: MDI_BF16, torch.float32: MDI_F32}
 
 
 class Kv8Rows:
@@ -405,12 +407,12 @@ class Kv8Cache:
 
     def _call(self, what, *args):
         """A C entry point, on the current stream of the cache's GPU, with that GPU current."""
-        stream = torch.cuda.current_stream(self.device).cuda_stream
-        if self.device.index == torch.cuda.current_device():
-            st = getattr(lib(), what)(*args, stream)
+        index = self.device.index
+        if index == torch.cuda.current_device():
+            st = getattr(lib(), what)(*args, _raw_stream(index))
         else:
-            with torch.cuda.device(self.device):
-                st = getattr(lib(), what)(*args, stream)
+            with torch.cuda.device(index):
+                st = getattr(lib(), what)(*args, _raw_stream(index))
         if st != MDI_OK:
             raise MdiError(st, what)
 
@@ -431,13 +433,12 @@ class Kv8Cache:
         return Kv8Rows((pos, start, table), MdiKv8Rows(_ptr(table), _ptr(start), _ptr(pos), n, n_rows, max_ctx), n_rows)
 
     def _rows_io(self, rows, k, v, what):
-        if k.shape != (rows.n_rows, self.K, self.h) or v.shape != k.shape or v.dtype != k.dtype or v.device != k.device \
-                or k.stride() != v.stride() or k.stride(2) != 1:
+        shape, stride, dtype = k.shape, k.stride(), k.dtype
+        if shape != (rows.n_rows, self.K, self.h) or stride[2] != 1 or v.shape != shape or v.stride() != stride or v.dtype != dtype:
             raise ValueError(f"{what}: k and v [rows, kv heads, head_dim] of one type and layout, channels next to each other")
-        if k.device != self.device or k.dtype not in (torch.bfloat16, torch.float32):
+        if dtype not in _KV8_TYPES or k.device != self.device or v.device != self.device:
             raise ValueError(f"{what}: bfloat16 or float32 on {self.device}")
-        return (k.data_ptr(), v.data_ptr(), MDI_BF16 if k.dtype == torch.bfloat16 else MDI_F32, _stride(k, 0, self.K * self.h),
-                _stride(k, 1, self.h))
+        return k.data_ptr(), v.data_ptr(), _KV8_TYPES[dtype], stride[0] if shape[0] > 1 else self.K * self.h, stride[1] if shape[1] > 1 else self.h
 
     def write(self, rows, k, v):
         """Quantise rows k, v [rows, kv heads, head_dim] (bfloat16 or float32, any row and head stride) into the cache."""
@@ -461,14 +462,17 @@ class Kv8Cache:
         workspace: as made by workspace() (None: taken from the allocator for this call)."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        for t in (q, out):
-            if t.dim() != 3 or t.shape[0] != rows.n_rows or t.shape[2] != self.h or t.dtype != torch.bfloat16 or t.device != self.device \
-                    or t.stride(2) != 1 or _stride(t, 1, self.h) != self.h or t.shape != q.shape:
-                raise ValueError(f"attn: q and out bfloat16 [rows, heads, {self.h}] on {self.device}, heads next to each other")
+        shape, qs, os, h = q.shape, q.stride(), out.stride(), self.h
+        if (len(shape) != 3 or shape[0] != rows.n_rows or shape[2] != h or out.shape != shape or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16
+                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or q.device != self.device or out.device != self.device):
+            raise ValueError(f"attn: q and out bfloat16 [rows, heads, {h}] on {self.device}, heads next to each other")
+        heads = shape[1]
         if workspace is None:
-            workspace = self.workspace(rows, q.shape[1])
-        self._call("mdi_kv8_attn", self._ref, rows._ref, q.data_ptr(), _stride(q, 0, q.shape[1] * self.h), q.shape[1],
-                   self.h ** -0.5 if scale is None else scale, out.data_ptr(), _stride(out, 0, q.shape[1] * self.h), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+            workspace = self.workspace(rows, heads)
+        alone = shape[0] < 2                                     # a lone row has no neighbours, whatever its stride says
+        self._call("mdi_kv8_attn", self._ref, rows._ref, q.data_ptr(), heads * h if alone else qs[0], heads, h ** -0.5 if scale is None else scale,
+                   out.data_ptr(), heads * h if alone else os[0], None if workspace is None else workspace.data_ptr(),
+                   0 if workspace is None else workspace.numel() * workspace.element_size())
         return out
 
     def check(self):
