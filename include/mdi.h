@@ -90,7 +90,7 @@ enum { MDI_NORM_LAYERNORM = 0, MDI_NORM_RMSNORM = 1 };
 enum { MDI_MLP_GELU_TANH = 0, MDI_MLP_GELU_ERF = 1, MDI_MLP_SWIGLU = 2 };
 enum { MDI_POS_LEARNED = 0, MDI_POS_ROPE = 1 };
 enum { MDI_F32 = 0, MDI_BF16 = 1 };
-enum { MDI_HAS_EMBED = 1u, MDI_HAS_HEAD = 2u };
+enum { MDI_HAS_EMBED = 1u, MDI_HAS_HEAD = 2u, MDI_KV8 = 4u };
 
 /*
  * Model and cache geometry.  Passed by pointer (host), copied at create.
@@ -173,6 +173,14 @@ MDI_API mdi_status mdi_partition_bytes(const mdi_config *cfg, uint32_t layer_lo,
  * MDI_HAS_HEAD = mdi_sample_greedy is available (starter's output portion).
  * layer_lo == layer_hi is legal only with MDI_HAS_HEAD and without
  * MDI_HAS_EMBED: an output portion without transformer blocks (Sec. III-E).
+ * MDI_KV8 = the KV caches are kept in 8 bits (see mdi_kv8): (head_dim + 4) bytes
+ * for a position's key or value of a kv head instead of 2 * head_dim, so the same
+ * memory holds nearly twice the samples or positions.  Needs blocks, MDI_BF16,
+ * max_ctx at most 2^24.  All positions - a first visit's own as well - are read
+ * as the cache holds them, so a prompt in pieces and in one gives the same keys
+ * and values.  Such a partition runs one kernel per operation; several samples
+ * share a pass over the weights in mdi_decode_batch and mdi_prefill_batch, up to
+ * 64 of them and max_prefill rows.
  *
  * The weights are copied, repacked, into `arena` (256-byte aligned device
  * memory of at least mdi_partition_bytes() bytes, owned by the caller and kept
@@ -210,6 +218,23 @@ MDI_API mdi_status mdi_prefill(mdi_partition *part, uint32_t seq_id, const void 
  */
 MDI_API mdi_status mdi_prefill_chunk(mdi_partition *part, uint32_t seq_id, const void *acts_in,
                              uint32_t T, void *acts_out);
+
+/*
+ * First visits, or their next pieces, of n different samples at once: sample
+ * seq_ids[i]'s next T[i] positions, which continue at its cache length (0 for a
+ * fresh sample).  acts_in and acts_out hold the samples' rows one after the other
+ * ([T[0] + .. + T[n - 1], d], or that many token ids).  With MDI_KV8 the rows of
+ * up to 64 samples, together at most max_prefill, go through the layers together,
+ * one pass over the weights for all of them: what many short prompts wait for is
+ * the weights.  Other partitions take the samples one after the other.  Each
+ * sample's result is that of mdi_prefill_chunk, up to the order in which partial
+ * sums are added; a sample that lives and has T[i] = 1 is decoded that way.
+ * seq_ids, T: host uint32[n], the samples pairwise different.
+ * Errors: as mdi_prefill_chunk, checked for all samples before the first is
+ * taken; MDI_ERR_ARG also when n == 0 or a sample occurs twice.
+ */
+MDI_API mdi_status mdi_prefill_batch(mdi_partition *part, uint32_t n, const uint32_t *seq_ids,
+                             const uint32_t *T, const void *acts_in, void *acts_out);
 
 /*
  * Later visit (Sec. III-D): forward only the newest position through the local
@@ -260,7 +285,9 @@ MDI_API mdi_status mdi_decode_steps(mdi_partition *part, uint32_t n, const uint3
  * (mdi_partition_info(4) tells).  Vectors between the matrix products are
  * rounded to bf16 here (as in a first visit), so a sample's result agrees with
  * mdi_decode_step's within the bf16 parity bar, not to the last bits; for a
- * given call pattern results are reproducible bit for bit.
+ * given call pattern results are reproducible bit for bit.  A partition with
+ * MDI_KV8 takes up to 64 messages a pass (at most max_prefill), by the products
+ * of a first visit.
  * Arguments and errors: as mdi_decode_steps.
  */
 MDI_API mdi_status mdi_decode_batch(mdi_partition *part, uint32_t n, const uint32_t *seq_ids,

@@ -1,6 +1,5 @@
 // The entry points of the 8-bit cache (mdi_kv8_* of mdi.h): checks on the host, then one or two launches.
 #include "kv8_internal.h"
-#include "once_per_device.h"
 
 using namespace mdi;
 
@@ -10,13 +9,8 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 mdi_status take_cache(const mdi_kv8* k, Kv8Cache* c) {
   if (!k || !k->codes || !k->scales || !k->tables || !aligned16(k->codes) || !aligned16(k->scales)) return MDI_ERR_ARG;
-  if (!k->n_pages || !k->n_kv_head || !k->head_dim || !k->page_tokens || !k->n_tables || !k->table_stride) return MDI_ERR_ARG;
-  if (k->head_dim % 8 || k->head_dim > 256 || k->n_kv_head > 1024 || k->n_pages > INT32_MAX || k->n_tables > INT32_MAX) return MDI_ERR_ARG;
-  // a position is divided by the page size with one multiplication, exact below this bound
-  if ((uint64_t)k->table_stride * k->page_tokens > 1u << 30 || (uint64_t)k->table_stride * k->page_tokens * k->page_tokens >= (1ull << 32)) return MDI_ERR_ARG;
-  const int pt = (int)k->page_tokens;
-  *c = Kv8Cache{k->codes, k->scales, k->tables, k->err, (int)k->n_pages, (int)k->n_kv_head, (int)k->head_dim, pt,
-                pt == 1 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u, pt == 1 ? ~0u : 0u, (int)k->n_tables, (int)k->table_stride};
+  if (!kv8_geometry(k->n_pages, k->n_kv_head, k->head_dim, k->page_tokens, k->n_tables, k->table_stride, c)) return MDI_ERR_ARG;
+  c->codes = k->codes; c->scales = k->scales; c->tables = k->tables; c->err = k->err;
   return MDI_OK;
 }
 
@@ -38,8 +32,6 @@ bool good_heads(const Kv8Cache& c, const Kv8Rows& r, uint32_t n_head) {
   return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 30) &&
          (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 1) < (1ull << 31);   // tiles of all units are counted in 32 bits
 }
-
-OncePerDevice g_prompt_lds;          // the kernels that use more than 64 KiB of LDS
 
 mdi_status hip_status() { return hipGetLastError() == hipSuccess ? MDI_OK : MDI_ERR_HIP; }
 
@@ -101,10 +93,7 @@ mdi_status mdi_kv8_attn(const mdi_kv8* cache, const mdi_kv8_rows* rows, const vo
   const size_t need = kv8_part_bytes(plan, c, r, (int)n_head);
   if (need && (!workspace || !aligned16(workspace))) return MDI_ERR_ARG;
   if (need > workspace_bytes) return MDI_ERR_NOMEM;
-  if (kv8_prompt_supported(c, r)) {
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || !g_prompt_lds.run(dev, kv8_prompt_allow_lds)) return MDI_ERR_HIP;
-  }
+  if (!kv8_allow_lds()) return MDI_ERR_HIP;
   launch_kv8_attn((hipStream_t)hip_stream, c, r,
                   Kv8Attn{(const bf16_t*)q, (long)q_stride, (bf16_t*)out, (long)out_stride, (int)n_head, scale * 1.44269504f, (float*)workspace, plan});
   return hip_status();

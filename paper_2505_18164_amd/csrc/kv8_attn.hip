@@ -143,13 +143,18 @@ __global__ __launch_bounds__(kBlock) void k_kv8_join(Kv8Cache c, Kv8Rows r, Kv8A
 
 }  // namespace
 
-Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
-  if (kv8_decode_supported(c, r)) return kv8_decode_plan(c, r, H);
-  if (kv8_prompt_supported(c, r)) return kv8_prompt_plan(c, r, H);
-  const long items = (long)r.n_rows * H;
-  const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / items));
-  int chunk = std::max(256, ((r.max_ctx + want - 1) / want + 63) / 64 * 64);
-  return Kv8Plan{chunk, (r.max_ctx + chunk - 1) / chunk, 0};
+Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_limit) {
+  Kv8Plan p{};
+  if (kv8_decode_supported(c, r)) {
+    p = kv8_decode_plan(c, r, H);
+  } else if (kv8_prompt_supported(c, r)) {
+    p = kv8_prompt_plan(c, r, H, part_limit);
+  } else {
+    const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / ((long)r.n_rows * H)));
+    p.chunk = std::max(256, ((r.max_ctx + want - 1) / want + 63) / 64 * 64);
+    p.splits = (r.max_ctx + p.chunk - 1) / p.chunk;
+  }
+  return kv8_part_bytes(p, c, r, H) <= part_limit ? p : Kv8Plan{r.max_ctx, 1, 0, 1};
 }
 
 void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {

@@ -282,10 +282,10 @@ constexpr int kLeast = 2;            // tiles of a share, at least
 // With many units, or short samples, a unit is a workgroup's.  Else the tiles of all units are cut into equal shares.
 Kv8Plan kv8_decode_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
   const int each = c.K * kv8_groups(c, H);                       // units of a sample
-  if ((long)r.n * each >= 4 * kShares || r.max_ctx <= kLeast * kKv8Tile) return Kv8Plan{r.max_ctx, 1, 0};
+  if ((long)r.n * each >= 4 * kShares || r.max_ctx <= kLeast * kKv8Tile) return Kv8Plan{r.max_ctx, 1, 0, 0};
   // a unit of t tiles in shares of at least kLeast, and of at least t * each / kShares (it is one of `each` alike)
   const int tiles = (r.max_ctx + kKv8Tile - 1) / kKv8Tile;
-  return Kv8Plan{kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares};
+  return Kv8Plan{kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares, 0};
 }
 
 void launch_kv8_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "kv8_mfma.h"
+#include "once_per_device.h"
 
 namespace mdi {
 namespace {
@@ -428,7 +429,7 @@ PromptGeo geo_of(const Kv8Cache& c, const Kv8Rows& r, int H, int WQ) {
 // eight of 333 of TinyLlama 26.2/30.5, one of 1500 44.3/30.0; four pieces of 64 behind 8000 of the 8B shape 264/165, in 4 parts
 // 97/74, in 8 70/84; the prompt of 1024 in two parts 76/80.
 struct PromptPlan { int groups, splits; };
-PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
+PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_limit) {
   const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
   const double heads = (double)r.n_rows * H, seen = r.max_ctx - 0.5 * std::min(r.max_ctx, rows);   // what a row sees, on average
   PromptPlan best{1, 1};
@@ -437,7 +438,7 @@ PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
     const int sh = heads_shift(c, H), bp = 256 / ng >> sh;
     const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.15 : 2.65) : (ng == 1 ? 1.45 : 1.65);
     for (int s = 1; s <= 32; s *= 2) {
-      if (s > 1 && r.max_ctx < 256 * s) break;
+      if (s > 1 && (r.max_ctx < 256 * s || kv8_part_bytes(Kv8Plan{0, s, 0, 0}, c, r, H) > part_limit)) break;
       const double longest = std::ceil(r.max_ctx / (64. * ng * s)), all = items * seen / (64. * ng * 256);
       double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
       if (s > 1) us += 6 + heads / 800 + heads * s * c.h / 5e5;
@@ -457,18 +458,22 @@ void launch_groups(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8
 }
 template <int HD>
 void launch_heads(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  if (prompt_plan(c, r, a.H).groups == 1) launch_groups<HD, 1>(s, c, r, a); else launch_groups<HD, 2>(s, c, r, a);
+  if (a.plan.groups == 1) launch_groups<HD, 1>(s, c, r, a); else launch_groups<HD, 2>(s, c, r, a);
 }
 
 }  // namespace
 
 bool kv8_prompt_supported(const Kv8Cache& c, const Kv8Rows& r) { return r.start && (c.h == 64 || c.h == 128); }
-bool kv8_prompt_allow_lds() { return allow_heads<64>() && allow_heads<128>(); }
+bool kv8_allow_lds() {
+  static OncePerDevice done;
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_heads<64>() && allow_heads<128>(); });
+}
 
-Kv8Plan kv8_prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
-  const int want = prompt_plan(c, r, H).splits;
-  const int chunk = ((r.max_ctx + want - 1) / want + BK - 1) / BK * BK;
-  return Kv8Plan{chunk, (r.max_ctx + chunk - 1) / chunk, 0};
+Kv8Plan kv8_prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_limit) {
+  const PromptPlan p = prompt_plan(c, r, H, part_limit);
+  const int chunk = ((r.max_ctx + p.splits - 1) / p.splits + BK - 1) / BK * BK;
+  return Kv8Plan{chunk, (r.max_ctx + chunk - 1) / chunk, 0, p.groups};
 }
 
 void launch_kv8_prompt(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {

@@ -8,6 +8,7 @@
 #include <new>
 #include <vector>
 
+#include "kv8_internal.h"
 #include "mdi_internal.h"
 #include "once_per_device.h"
 #include "visit_internal.h"
@@ -20,7 +21,8 @@ struct LayerPacked {
   const float *ln1_g = nullptr, *ln1_b = nullptr, *ln2_g = nullptr, *ln2_b = nullptr;
   const void *wqkv = nullptr, *wo = nullptr, *wup = nullptr, *wdown = nullptr;
   const float *bqkv = nullptr, *bo = nullptr, *bup = nullptr, *bdown = nullptr;
-  char* kv = nullptr;  // this layer's pages: [page][K][2][pt][h]
+  char* kv = nullptr;  // this layer's pages: [page][K][2][pt][h], in 8-bit caches (kv8_internal.h) of codes ...
+  float* kv_scales = nullptr;   // ... and [page][K][2][pt] scales
 };
 
 // Walks the arena in a fixed order; with base == nullptr it only measures.
@@ -73,6 +75,15 @@ struct mdi_partition {
   float* p_part = nullptr;       // partial results of products whose inner dimension is split
   size_t part_cap = 0;           // ... in floats
   bf16_t* p_qb = nullptr;        // queries of the matrix-core attention of a first visit
+  // 8-bit cache (MDI_KV8): rows of a pass as the QKV product leaves them - one page of Tm positions -, what launch_kv8_setup
+  // writes, inputs and outputs of single messages side by side, partial sums of the attention
+  bool kv8 = false;
+  bf16_t* p_kv = nullptr;
+  int32_t* p_rows = nullptr;
+  float2* p_rope = nullptr;
+  void *p_in = nullptr, *p_out = nullptr;
+  float* p_kv8_part = nullptr;
+  size_t kv8_part_cap = 0;       // ... in bytes
   // host bookkeeping
   std::vector<uint32_t> seq_len;
   std::vector<int32_t> host_tables;   // mirror of `tables`, source of the async page-table copies
@@ -136,11 +147,36 @@ mdi_status check_config(const mdi_config* c, uint32_t lo, uint32_t hi, uint32_t 
   if (c->max_prefill > c->max_ctx) return MDI_ERR_ARG;
   // the decode kernel divides a position by the page size with one multiplication, exact below this bound
   if ((uint64_t)c->max_ctx * (c->kv_page_tokens ? c->kv_page_tokens : 16) >= (1ull << 32)) return MDI_ERR_ARG;
-  if (flags & ~(uint32_t)(MDI_HAS_EMBED | MDI_HAS_HEAD)) return MDI_ERR_ARG;
+  if (flags & ~(uint32_t)(MDI_HAS_EMBED | MDI_HAS_HEAD | MDI_KV8)) return MDI_ERR_ARG;
   if (hi > c->n_layer || lo > hi) return MDI_ERR_ARG;
   if (lo == hi && ((flags & MDI_HAS_EMBED) || !(flags & MDI_HAS_HEAD))) return MDI_ERR_ARG;
   if ((flags & MDI_HAS_EMBED) && lo != 0) return MDI_ERR_ARG;  // token ids enter at layer 0 only
+  if (flags & MDI_KV8) {
+    Kv8Cache geometry;
+    const uint64_t pt = c->kv_page_tokens ? c->kv_page_tokens : 16, stride = (c->max_ctx + pt - 1) / pt;
+    if (lo == hi || c->dtype != MDI_BF16 || c->max_ctx > 1u << 24 || c->n_head > 4096 || c->max_seqs > 1u << 20) return MDI_ERR_ARG;
+    if (!kv8_geometry(c->kv_pages ? c->kv_pages : c->max_seqs * stride, c->n_kv_head, c->head_dim, pt, c->max_seqs, stride, &geometry)) return MDI_ERR_ARG;
+  }
   return MDI_OK;
+}
+
+// The 8-bit cache of a layer, and the samples and rows of a call (n one-row samples).
+Kv8Cache kv8_cache(const mdi_partition* p, const LayerPacked& L) {
+  Kv8Cache c{};
+  (void)kv8_geometry(p->n_pages, p->cfg.n_kv_head, p->cfg.head_dim, p->pt, p->cfg.max_seqs, p->pages_per_seq, &c);   // (checked with the configuration)
+  c.codes = (int8_t*)L.kv; c.scales = L.kv_scales; c.tables = p->tables; c.err = p->err;
+  return c;
+}
+// Room for the attention's partial sums: what any number of single tokens may need, and 16 MiB for pieces of prompts (kv8_plan
+// divides no further than fits).
+size_t kv8_part_room(const mdi_partition* p) {
+  const Kv8Cache c = kv8_cache(p, LayerPacked());
+  size_t most = 16u << 20;
+  for (int n = 1; n <= (int)std::min<uint32_t>(p->cfg.max_seqs, kMaxVisits); ++n) {
+    const Kv8Rows r{nullptr, nullptr, nullptr, n, n, (int)p->cfg.max_ctx};
+    most = std::max(most, kv8_part_bytes(kv8_plan(c, r, (int)p->cfg.n_head), c, r, (int)p->cfg.n_head));
+  }
+  return most;
 }
 
 // Lays the partition out in the arena.  Called with p->... unset pointers when measuring.
@@ -186,8 +222,11 @@ size_t carve(mdi_partition* p, void* arena) {
   p->counters = (unsigned*)cv.take((H + 2) * 4);
   if (p->n_local) {
     if (c.pos_kind == MDI_POS_ROPE) p->rope = (float2*)cv.take((size_t)c.max_ctx * (h / 2) * sizeof(float2));
-    const size_t layer_pool = (size_t)p->n_pages * K * 2 * p->pt * h * B;
-    for (auto& L : p->layers) L.kv = (char*)cv.take(layer_pool);
+    const size_t layer_rows = (size_t)p->n_pages * K * 2 * p->pt;
+    for (auto& L : p->layers) {
+      L.kv = (char*)cv.take(layer_rows * h * (p->kv8 ? 1 : B));
+      if (p->kv8) L.kv_scales = (float*)cv.take(layer_rows * 4);
+    }
     p->tables = (int32_t*)cv.take((size_t)c.max_seqs * p->pages_per_seq * 4);
     p->xres = (float*)cv.take(d * 4);
     p->q = (float*)cv.take(H * h * 4);
@@ -250,8 +289,17 @@ size_t carve(mdi_partition* p, void* arena) {
     // few positions are cut into up to kMaxKSplits pieces, more positions into fewer: 4096 rows of partial results
     p->part_cap = std::min<size_t>(T * kMaxKSplits, 4096) * d;
     p->p_part = (float*)cv.take(p->part_cap * 4);
-    if (flash_supported(c.dtype, (int)h)) p->p_qb = (bf16_t*)cv.take(T * H * h * 2);
+    if (p->kv8 || flash_supported(c.dtype, (int)h)) p->p_qb = (bf16_t*)cv.take(T * H * h * 2);
     else p->p_q = (float*)cv.take(T * H * h * 4);
+    if (p->kv8) {
+      p->p_kv = (bf16_t*)cv.take(T * 2 * K * h * 2);
+      p->p_rows = (int32_t*)cv.take((4 * kMaxVisits + T) * 4);
+      if (p->rope || c.pos_kind == MDI_POS_ROPE) p->p_rope = (float2*)cv.take(T * (h / 2) * sizeof(float2));
+      p->p_in = cv.take(kMaxVisits * std::max<size_t>(d * B, 4));
+      p->p_out = cv.take(kMaxVisits * d * B);
+      p->kv8_part_cap = kv8_part_room(p);
+      p->p_kv8_part = (float*)cv.take(p->kv8_part_cap);
+    }
   }
   return (cv.off + 255) & ~(size_t)255;
 }
@@ -259,6 +307,7 @@ size_t carve(mdi_partition* p, void* arena) {
 void init_geometry(mdi_partition* p, const mdi_config* cfg, uint32_t lo, uint32_t hi, uint32_t flags) {
   p->cfg = *cfg;
   p->lo = lo; p->hi = hi; p->flags = flags;
+  p->kv8 = flags & MDI_KV8;
   p->n_local = (int)(hi - lo);
   p->esz = cfg->dtype == MDI_BF16 ? 2 : 4;
   p->pt = cfg->kv_page_tokens ? (int)cfg->kv_page_tokens : 16;
@@ -271,7 +320,7 @@ void init_geometry(mdi_partition* p, const mdi_config* cfg, uint32_t lo, uint32_
 void plan_step(mdi_partition* p, int n_cu) {
   const mdi_config& c = p->cfg;
   p->use_step = false;
-  if (c.decode_path == 1 || !p->n_local || n_cu <= 0) return;
+  if (c.decode_path == 1 || !p->n_local || n_cu <= 0 || p->kv8) return;
   const int H = c.n_head, K = c.n_kv_head, h = c.head_dim, d = c.d_model, F = c.d_ff;
   const int group = H / K;
   // Query heads that take one pass over their kv head's cache together.  Measured (heads of 128, groups of 4 and 8):
@@ -438,6 +487,49 @@ void put_rows(mdi_partition* p, const void* src, const void* dst, size_t rows, s
 
 mdi_status hip_status() { return hipGetLastError() == hipSuccess ? MDI_OK : MDI_ERR_HIP; }
 
+// Takes T rows through the local layers: `src` is where they come from, acts_out where they go.  qkv(layer) says where a layer's
+// QKV product leaves its queries, keys and values, attend(layer) enqueues its attention, from there to p_o.
+template <typename Qkv, typename Attend>
+void run_layers(mdi_partition* p, uint32_t T, RowSource src, void* acts_out, Qkv&& qkv, Attend&& attend) {
+  const mdi_config& c = p->cfg;
+  hipStream_t s = p->stream;
+  const int d = c.d_model, H = c.n_head, K = c.n_kv_head, h = c.head_dim, F = c.d_ff;
+  const int ak = act_kind(c);
+  const bool swiglu = c.mlp_kind == MDI_MLP_SWIGLU;
+  const size_t four = 4 * p->esz;
+  // Residual products with few positions split their inner dimension; the norm that follows adds the partial results.
+  int pend_S = 1;
+  const float* pend_bias = nullptr;
+  auto norm = [&](const float* g, const float* b, void* out, void* hand_off) {
+    NormRowsArgs n{p->p_xres, (int)T, d, (int)c.norm_kind, g, b, c.norm_eps, out, ak, pend_S, p->p_part, (long)T * d, pend_bias, hand_off,
+                   (uintptr_t)hand_off % four == 0, src};
+    launch_norm_rows(s, n);
+    pend_S = 1;
+    src.in = nullptr;                        // the first norm has taken it
+  };
+  const int aligned = ((uintptr_t)acts_out & 15) == 0;
+  auto resid = [&](const void* A, const void* W, const float* bias, int Kd, void* hand_off) {
+    GemmArgs ga{A, W, bias, (int)T, d, Kd, 1, p->p_xres, hand_off, 0, aligned, {}};
+    const GemmPlan pl = plan_gemm(c.dtype, p->n_cu, (int)T, d, Kd, p->part_cap);
+    ga.S = pl.S;
+    if (pl.S > 1) { ga.out_f32 = p->p_part; ga.out_act = nullptr; pend_S = pl.S; pend_bias = bias; }
+    launch_gemm(s, c.dtype, pl.S > 1 ? GEPI_PART : GEPI_RESID, pl.shape, ga);
+    if (pl.S > 1 && hand_off) norm(nullptr, nullptr, nullptr, hand_off);
+  };
+  for (int i = 0; i < p->n_local; ++i) {
+    const LayerPacked& L = p->layers[i];
+    norm(L.ln1_g, L.ln1_b, p->p_xn, nullptr);
+    GemmArgs g1{p->p_xn, L.wqkv, L.bqkv, (int)T, (H + 2 * K) * h, d, 1, nullptr, nullptr, 0, 0, qkv(L)};
+    launch_gemm(s, c.dtype, GEPI_QKV, plan_gemm(c.dtype, p->n_cu, (int)T, g1.N, d, 0).shape, g1);
+    attend(L);
+    resid(p->p_o, L.wo, L.bo, H * h, nullptr);
+    norm(L.ln2_g, L.ln2_b, p->p_xn, nullptr);
+    GemmArgs g3{p->p_xn, L.wup, L.bup, (int)T, swiglu ? 2 * F : F, d, 1, nullptr, p->p_u, c.mlp_kind == MDI_MLP_GELU_TANH, 1, {}};
+    launch_gemm(s, c.dtype, swiglu ? GEPI_SWIGLU : GEPI_GELU, plan_gemm(c.dtype, p->n_cu, (int)T, g3.N, d, 0).shape, g3);
+    resid(p->p_u, L.wdown, L.bdown, F, i == p->n_local - 1 ? acts_out : nullptr);
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -541,7 +633,7 @@ mdi_status mdi_partition_create(const mdi_config* cfg, uint32_t layer_lo, uint32
     if (dev < 0 || dev >= kMaxDevices) { delete p; return MDI_ERR_ARG; }
     p->n_cu = n_cu;
     p->device = dev;
-    if (!g_prefill_lds.run(dev, []() { return allow_gemm_lds_bf16() && allow_gemm_lds_f32() && allow_flash_lds(); })) {
+    if (!g_prefill_lds.run(dev, []() { return allow_gemm_lds_bf16() && allow_gemm_lds_f32() && allow_flash_lds() && kv8_allow_lds(); })) {
       delete p;
       return MDI_ERR_HIP;
     }
@@ -640,75 +732,117 @@ mdi_status mdi_partition_create(const mdi_config* cfg, uint32_t layer_lo, uint32
 
 namespace {
 
+// Page of a position as the QKV product and the attention of first visits divide: see QkvOut.
+struct PageDivide { int sh; unsigned magic; };
+PageDivide page_divide(int pt) {
+  const bool pow2 = (pt & (pt - 1)) == 0;
+  return {pow2 ? __builtin_ctz((unsigned)pt) : -1, pow2 ? 0u : 0xFFFFFFFFu / (unsigned)pt + 1u};
+}
+int new_pages(const mdi_partition* p, uint32_t seq, uint32_t T) {
+  const int len = (int)p->seq_len[seq];
+  return (len + (int)T + p->pt - 1) / p->pt - (len + p->pt - 1) / p->pt;
+}
+
 // Forwards T positions of sample seq, starting at position pos0 = its current cache length (0: a first visit).
 mdi_status prefill_rows(mdi_partition* p, uint32_t seq, const void* acts_in, uint32_t T, void* acts_out) {
   const mdi_config& c = p->cfg;
   const int pos0 = (int)p->seq_len[seq];
   if ((uint32_t)pos0 + T > c.max_ctx) return MDI_ERR_CTX;
   if (T > (uint32_t)p->Tm) return MDI_ERR_ARG;
-  const int have = (pos0 + p->pt - 1) / p->pt;
-  const int need = (pos0 + (int)T + p->pt - 1) / p->pt - have;
+  const int have = (pos0 + p->pt - 1) / p->pt, need = new_pages(p, seq, T);
   if ((int)p->free_pages.size() < need) return MDI_ERR_NOMEM;
   int32_t* row = p->host_tables.data() + (size_t)seq * p->pages_per_seq;
   for (int i = 0; i < need; ++i) { row[have + i] = p->free_pages.back(); p->free_pages.pop_back(); }
   int32_t* drow = p->tables + (size_t)seq * p->pages_per_seq;
   if (need && hipMemcpyAsync(drow + have, row + have, (size_t)need * 4, hipMemcpyHostToDevice, p->stream) != hipSuccess) return MDI_ERR_HIP;
 
-  hipStream_t s = p->stream;
-  const int d = c.d_model, H = c.n_head, K = c.n_kv_head, h = c.head_dim, F = c.d_ff;
-  const int ak = act_kind(c);
-  const bool embed = p->flags & MDI_HAS_EMBED, swiglu = c.mlp_kind == MDI_MLP_SWIGLU;
-  const size_t four = 4 * p->esz;
-  RowSource src{acts_in, embed ? IN_TOKEN : ak, (uintptr_t)acts_in % four == 0, p->wte, p->wpe, (int)c.vocab, p->err, pos0};   // until the first norm has taken it
-  // Residual products with few positions split their inner dimension; the norm that follows adds the partial results.
-  int pend_S = 1;
-  const float* pend_bias = nullptr;
-  auto norm = [&](const float* g, const float* b, void* out, void* hand_off) {
-    NormRowsArgs n{p->p_xres, (int)T, d, (int)c.norm_kind, g, b, c.norm_eps, out, ak, pend_S, p->p_part, (long)T * d, pend_bias, hand_off,
-                   (uintptr_t)hand_off % four == 0, src};
-    launch_norm_rows(s, n);
-    pend_S = 1;
-    src.in = nullptr;
-  };
-  const int aligned = ((uintptr_t)acts_out & 15) == 0;
-  auto resid = [&](const void* A, const void* W, const float* bias, int Kd, void* hand_off) {
-    GemmArgs ga{A, W, bias, (int)T, d, Kd, 1, p->p_xres, hand_off, 0, aligned, {}};
-    const GemmPlan pl = plan_gemm(c.dtype, p->n_cu, (int)T, d, Kd, p->part_cap);
-    ga.S = pl.S;
-    if (pl.S > 1) { ga.out_f32 = p->p_part; ga.out_act = nullptr; pend_S = pl.S; pend_bias = bias; }
-    launch_gemm(s, c.dtype, pl.S > 1 ? GEPI_PART : GEPI_RESID, pl.shape, ga);
-    if (pl.S > 1 && hand_off) norm(nullptr, nullptr, nullptr, hand_off);
-  };
+  const int H = c.n_head, K = c.n_kv_head, h = c.head_dim, ak = act_kind(c);
   const bool flash = p->p_qb != nullptr;
   const float scale = 1.f / sqrtf((float)h);
-  const bool pow2 = (p->pt & (p->pt - 1)) == 0;
-  const int pt_sh = pow2 ? __builtin_ctz((unsigned)p->pt) : -1;
-  const unsigned pt_magic = pow2 ? 0u : 0xFFFFFFFFu / (unsigned)p->pt + 1u;
-  for (int i = 0; i < p->n_local; ++i) {
-    const LayerPacked& L = p->layers[i];
-    norm(L.ln1_g, L.ln1_b, p->p_xn, nullptr);
-    GemmArgs g1{p->p_xn, L.wqkv, L.bqkv, (int)T, (H + 2 * K) * h, d, 1, nullptr, nullptr, 0, 0,
-                {H, K, h, p->pt, pt_sh, pt_magic, pos0, scale * 1.44269504f, p->rope, p->p_q, p->p_qb, L.kv, drow}};   // log2 e: k_flash_prefill's exponentials are powers of two
-    launch_gemm(s, c.dtype, GEPI_QKV, plan_gemm(c.dtype, p->n_cu, (int)T, g1.N, d, 0).shape, g1);
-    if (flash) {
-      FlashArgs fa{p->p_qb, (const bf16_t*)L.kv, drow, (bf16_t*)p->p_o, (int)T, H, K, h, pos0,
-                   p->pt, pt_sh, pt_magic};
-      launch_flash_prefill(s, fa);
-    } else {
-      AttnArgs at{};
-      at.q = p->p_q; at.q_stride = (long)H * h; at.pool = L.kv; at.table = drow;
-      at.ctx0 = pos0 + 1; at.n_q = (int)T; at.H = H; at.K = K; at.h = h; at.pt = p->pt;
-      at.chunk = (int)c.max_ctx; at.n_splits = 1; at.scale = scale;
-      at.part = p->part; at.counters = p->counters; at.out = p->p_o; at.out_stride = (long)H * h; at.out_kind = ak;
-      launch_attn(s, c.dtype, at);
-    }
-    resid(p->p_o, L.wo, L.bo, H * h, nullptr);
-    norm(L.ln2_g, L.ln2_b, p->p_xn, nullptr);
-    GemmArgs g3{p->p_xn, L.wup, L.bup, (int)T, swiglu ? 2 * F : F, d, 1, nullptr, p->p_u, c.mlp_kind == MDI_MLP_GELU_TANH, 1, {}};
-    launch_gemm(s, c.dtype, swiglu ? GEPI_SWIGLU : GEPI_GELU, plan_gemm(c.dtype, p->n_cu, (int)T, g3.N, d, 0).shape, g3);
-    resid(p->p_u, L.wdown, L.bdown, F, i == p->n_local - 1 ? acts_out : nullptr);
-  }
+  const PageDivide pd = page_divide(p->pt);
+  const RowSource src{acts_in, (p->flags & MDI_HAS_EMBED) ? IN_TOKEN : ak, (uintptr_t)acts_in % (4 * p->esz) == 0, p->wte, p->wpe, (int)c.vocab, p->err, pos0};
+  run_layers(p, T, src, acts_out,
+             [&](const LayerPacked& L) {     // log2 e: k_flash_prefill's exponentials are powers of two
+               return QkvOut{H, K, h, p->pt, pd.sh, pd.magic, pos0, scale * 1.44269504f, p->rope, p->p_q, p->p_qb, L.kv, drow};
+             },
+             [&](const LayerPacked& L) {
+               if (flash) {
+                 FlashArgs fa{p->p_qb, (const bf16_t*)L.kv, drow, (bf16_t*)p->p_o, (int)T, H, K, h, pos0,
+                              p->pt, pd.sh, pd.magic};
+                 launch_flash_prefill(p->stream, fa);
+               } else {
+                 AttnArgs at{};
+                 at.q = p->p_q; at.q_stride = (long)H * h; at.pool = L.kv; at.table = drow;
+                 at.ctx0 = pos0 + 1; at.n_q = (int)T; at.H = H; at.K = K; at.h = h; at.pt = p->pt;
+                 at.chunk = (int)c.max_ctx; at.n_splits = 1; at.scale = scale;
+                 at.part = p->part; at.counters = p->counters; at.out = p->p_o; at.out_stride = (long)H * h; at.out_kind = ak;
+                 launch_attn(p->stream, c.dtype, at);
+               }
+             });
   p->seq_len[seq] = (uint32_t)pos0 + T;
+  return hip_status();
+}
+
+// One pass over the weights for n (1 .. kMaxVisits) samples of a partition with an 8-bit cache: T[i] new positions of sample
+// seqs[i], T[0] + .. + T[n - 1] <= Tm rows, one sample's after the other's in acts_in and acts_out; or, with `ins` and `outs`, one
+// position each, the rows apart.  Everything that can be refused has been.
+mdi_status visit_kv8(mdi_partition* p, int n, const uint32_t* seqs, const uint32_t* T, const void* acts_in, void* acts_out,
+                     const void* const* ins, void* const* outs) {
+  const mdi_config& c = p->cfg;
+  const int d = c.d_model, H = c.n_head, K = c.n_kv_head, h = c.head_dim, ak = act_kind(c);
+  const bool embed = p->flags & MDI_HAS_EMBED, apart = ins && n > 1;
+  if (ins && n == 1) { acts_in = ins[0]; acts_out = outs[0]; }
+  Kv8Setup a{};
+  int rows = 0, ctx = 1;
+  bool single = true;                        // one new position per sample
+  for (int i = 0; i < n; ++i) {
+    const uint32_t seq = seqs[i], t = T ? T[i] : 1u;
+    const int len = (int)p->seq_len[seq], have = (len + p->pt - 1) / p->pt, need = new_pages(p, seq, t);
+    int32_t* row = p->host_tables.data() + (size_t)seq * p->pages_per_seq;
+    for (int k = 0; k < need; ++k) { row[have + k] = p->free_pages.back(); p->free_pages.pop_back(); }
+    a.first[i] = rows; a.pos[i] = len; a.seq[i] = (int)seq;
+    a.page_at[i] = need == 1 ? (int)(seq * p->pages_per_seq) + have : -1;
+    a.page[i] = need == 1 ? row[have] : 0;
+    if (need > 1 && hipMemcpyAsync(p->tables + (size_t)seq * p->pages_per_seq + have, row + have, (size_t)need * 4, hipMemcpyHostToDevice, p->stream) != hipSuccess)
+      return MDI_ERR_HIP;
+    if (apart) a.in[i] = ins[i];
+    rows += (int)t;
+    ctx = std::max(ctx, len + (int)t);
+    single = single && t == 1;
+  }
+  a.n = n; a.rows = rows; a.first[n] = rows;
+  a.start = p->p_rows; a.at = p->p_rows + kMaxVisits + 1; a.table = a.at + kMaxVisits; a.zero = a.table + kMaxVisits; a.row_pos = p->p_rows + 4 * kMaxVisits;
+  a.tables = p->tables;
+  const bool several = n > 1;                // a lone sample's angles are a piece of the table
+  a.rope = p->rope; a.rope_rows = several && p->rope ? p->p_rope : nullptr; a.half = h / 2;
+  a.in_rows = apart ? p->p_in : nullptr; a.in_bytes = embed ? 4 : d * p->esz;
+  launch_kv8_setup(p->stream, a);
+
+  const void* in = apart ? p->p_in : acts_in;
+  void* out = apart ? p->p_out : acts_out;
+  RowSource src{in, embed ? IN_TOKEN : ak, (uintptr_t)in % (4 * p->esz) == 0, p->wte, p->wpe, (int)c.vocab, p->err, a.pos[0]};
+  if (several) src.row_pos = a.row_pos;
+  const float2* rope = several ? p->p_rope : p->rope ? p->rope + (size_t)a.pos[0] * (h / 2) : nullptr;
+  const PageDivide pd = page_divide(p->Tm);  // the rows' keys and values: a page of Tm positions, [K][2][Tm][h]
+  const Kv8Rows r{a.table, single ? nullptr : a.start, a.at, n, rows, ctx};
+  const Kv8RowsIO io{p->p_kv, p->p_kv + (size_t)p->Tm * h, h, 2l * p->Tm * h};
+  const Kv8Plan plan = kv8_plan(kv8_cache(p, p->layers[0]), r, H, p->kv8_part_cap);
+  run_layers(p, (uint32_t)rows, src, out,
+             [&](const LayerPacked&) {       // the queries with the softmax's scale and log2 e, for exponentials that are powers of two
+               return QkvOut{H, K, h, p->Tm, pd.sh, pd.magic, 0, 1.44269504f / sqrtf((float)h), rope, nullptr, p->p_qb, p->p_kv, a.zero};
+             },
+             [&](const LayerPacked& L) {
+               const Kv8Cache cache = kv8_cache(p, L);
+               launch_kv8_write(p->stream, MDI_BF16, cache, r, io);
+               launch_kv8_attn(p->stream, cache, r, Kv8Attn{p->p_qb, (long)H * h, (bf16_t*)p->p_o, (long)H * h, H, 1.f, p->p_kv8_part, plan});
+             });
+  if (apart) {
+    Kv8Handoff f{};
+    f.rows = p->p_out; f.n = n; f.bytes = d * p->esz;
+    for (int i = 0; i < n; ++i) f.out[i] = outs[i];
+    launch_kv8_handoff(p->stream, f);
+  }
+  for (int i = 0; i < n; ++i) p->seq_len[seqs[i]] += T ? T[i] : 1u;
   return hip_status();
 }
 
@@ -718,13 +852,41 @@ mdi_status mdi_prefill(mdi_partition* p, uint32_t seq, const void* acts_in, uint
   if (!p || !acts_in || !acts_out || !p->n_local) return MDI_ERR_ARG;
   if (seq >= p->cfg.max_seqs || T == 0) return MDI_ERR_ARG;
   if (p->seq_len[seq]) return MDI_ERR_STATE;
-  return prefill_rows(p, seq, acts_in, T, acts_out);
+  return mdi_prefill_batch(p, 1, &seq, &T, acts_in, acts_out);
 }
 
 mdi_status mdi_prefill_chunk(mdi_partition* p, uint32_t seq, const void* acts_in, uint32_t T, void* acts_out) {
   if (!p || !acts_in || !acts_out || !p->n_local) return MDI_ERR_ARG;
   if (seq >= p->cfg.max_seqs || T == 0) return MDI_ERR_ARG;
-  return prefill_rows(p, seq, acts_in, T, acts_out);
+  return mdi_prefill_batch(p, 1, &seq, &T, acts_in, acts_out);
+}
+
+mdi_status mdi_prefill_batch(mdi_partition* p, uint32_t n, const uint32_t* seqs, const uint32_t* T, const void* acts_in, void* acts_out) {
+  if (!p || !n || !seqs || !T || !acts_in || !acts_out || !p->n_local) return MDI_ERR_ARG;
+  // everything that can be refused is checked before the first sample is taken, so a refusal leaves none half done
+  size_t pages = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    if (seqs[i] >= p->cfg.max_seqs || T[i] == 0) return MDI_ERR_ARG;
+    for (uint32_t k = 0; k < i; ++k)
+      if (seqs[k] == seqs[i]) return MDI_ERR_ARG;
+    if ((uint64_t)p->seq_len[seqs[i]] + T[i] > p->cfg.max_ctx) return MDI_ERR_CTX;
+    if (T[i] > (uint32_t)p->Tm) return MDI_ERR_ARG;
+    pages += (size_t)new_pages(p, seqs[i], T[i]);
+  }
+  if (pages > p->free_pages.size()) return MDI_ERR_NOMEM;
+  const size_t in_row = (p->flags & MDI_HAS_EMBED) ? 4 : (size_t)p->cfg.d_model * p->esz, out_row = (size_t)p->cfg.d_model * p->esz;
+  const char* in = (const char*)acts_in;
+  char* out = (char*)acts_out;
+  for (uint32_t i = 0; i < n;) {
+    uint32_t m = 1, rows = T[i];             // an 8-bit cache: as many samples as the scratch has rows for; else one after the other
+    while (p->kv8 && i + m < n && m < (uint32_t)kMaxVisits && rows + T[i + m] <= (uint32_t)p->Tm) rows += T[i + m++];
+    const mdi_status st = p->kv8 ? visit_kv8(p, (int)m, seqs + i, T + i, in, out, nullptr, nullptr) : prefill_rows(p, seqs[i], in, T[i], out);
+    if (st != MDI_OK) return st;
+    in += rows * in_row;
+    out += rows * out_row;
+    i += m;
+  }
+  return MDI_OK;
 }
 
 namespace {
@@ -866,6 +1028,12 @@ mdi_status launch_messages(mdi_partition* p, int n, const uint32_t* seqs, const 
 mdi_status mdi_decode_step(mdi_partition* p, uint32_t seq, const void* act_in, void* act_out) {
   if (!p || !act_in || !act_out || !p->n_local) return MDI_ERR_ARG;
   const mdi_config& c = p->cfg;
+  if (p->kv8) {
+    const mdi_status st = check_message(p, seq);
+    if (st != MDI_OK) return st;
+    if (new_pages(p, seq, 1) > (int)p->free_pages.size()) return MDI_ERR_NOMEM;
+    return visit_kv8(p, 1, &seq, nullptr, nullptr, nullptr, &act_in, &act_out);
+  }
   MessagePlan mp;
   const mdi_status pst = plan_message(p, seq, &mp);
   if (pst != MDI_OK) return pst;
@@ -1063,7 +1231,7 @@ mdi_status launch_batch(mdi_partition* p, int n, const uint32_t* seqs, const Mes
 
 mdi_status mdi_decode_batch(mdi_partition* p, uint32_t n, const uint32_t* seqs, const void* const* acts_in, void* const* acts_out) {
   if (!p || !n || !seqs || !acts_in || !acts_out || !p->n_local) return MDI_ERR_ARG;
-  if (!p->use_batch) return mdi_decode_steps(p, n, seqs, acts_in, acts_out);
+  if (!p->use_batch && !p->kv8) return mdi_decode_steps(p, n, seqs, acts_in, acts_out);
   // everything that can be refused is checked before the first message is taken, so a refusal leaves no message half done
   size_t new_pages = 0;
   for (uint32_t i = 0; i < n; ++i) {
@@ -1075,6 +1243,15 @@ mdi_status mdi_decode_batch(mdi_partition* p, uint32_t n, const uint32_t* seqs, 
     if (p->seq_len[seqs[i]] % (uint32_t)p->pt == 0) ++new_pages;
   }
   if (new_pages > p->free_pages.size()) return MDI_ERR_NOMEM;
+  if (p->kv8) {
+    const uint32_t most = (uint32_t)std::min(kMaxVisits, p->Tm);   // rows of a pass
+    for (uint32_t i = 0, m; i < n; i += m) {
+      m = std::min(most, n - i);
+      const mdi_status st = visit_kv8(p, (int)m, seqs + i, nullptr, nullptr, nullptr, acts_in + i, acts_out + i);
+      if (st != MDI_OK) return st;
+    }
+    return MDI_OK;
+  }
   for (uint32_t i = 0; i < n;) {
     const uint32_t m = std::min<uint32_t>(kMaxBatch, n - i);
     if (m == 1) {
@@ -1276,7 +1453,7 @@ mdi_status mdi_step_bytes(const mdi_partition* p, uint32_t ctx, int head, uint64
   }
   const uint64_t mlp = (c.mlp_kind == MDI_MLP_SWIGLU ? 3 : 2) * d * F;
   const uint64_t layer = ((H + 2 * K) * h * d + d * H * h + mlp) * B;
-  const uint64_t kv_tok = 2 * K * h * B;
+  const uint64_t kv_tok = p->kv8 ? 2 * K * (h + 4) : 2 * K * h * B;
   *bytes = (uint64_t)p->n_local * (layer + kv_tok * ctx + kv_tok) + 2 * d * B;
   return MDI_OK;
 }
@@ -1327,7 +1504,7 @@ mdi_status mdi_partition_info(const mdi_partition* p, uint32_t what, uint64_t* v
     case 1: *value = p->use_step ? (uint64_t)p->nwg : 0; return MDI_OK;
     case 2: *value = p->use_step ? (uint64_t)p->step_lds : 0; return MDI_OK;
     case 3: *value = p->arena_bytes; return MDI_OK;
-    case 4: *value = p->use_batch ? (uint64_t)kMaxBatch : 0; return MDI_OK;
+    case 4: *value = p->kv8 ? (uint64_t)std::min(kMaxVisits, p->Tm) : p->use_batch ? (uint64_t)kMaxBatch : 0; return MDI_OK;
     case 7: *value = (uint64_t)p->last_waves; return MDI_OK;
     case 8: *value = (uint64_t)p->last_splits; return MDI_OK;
     case 6: *value = p->hb_nwg ? (uint64_t)kMaxBatch : 0; return MDI_OK;

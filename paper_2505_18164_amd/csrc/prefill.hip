@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_rows(NormRowsArgs a) {
     if (!a.src.in) return x[i];
     if (a.src.in_kind != IN_TOKEN) return four(a.src.in, kind, a.src.aligned, (long)t * a.d + 4 * i);
     float4 r = four(a.src.wte, kind, true, tok * a.d + 4 * i);
-    if (a.src.wpe) add(r, four(a.src.wpe, kind, true, (long)(a.src.pos0 + t) * a.d + 4 * i));
+    if (a.src.wpe) add(r, four(a.src.wpe, kind, true, (long)(a.src.row_pos ? a.src.row_pos[t] : a.src.pos0 + t) * a.d + 4 * i));
     return r;
   };
   auto part = [&](int s, int i) __attribute__((always_inline)) { return reinterpret_cast<const float4*>(a.part + s * a.part_stride + (long)t * a.d)[i]; };

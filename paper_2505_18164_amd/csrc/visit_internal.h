@@ -14,6 +14,7 @@ struct RowSource {
   const void* wte; const void* wpe;
   int vocab; int* err;               // a token id outside [0, vocab) sets *err = 2 and is read as token 0
   int pos0;                          // position of row 0 (a first visit in several chunks continues at the cache length)
+  const int32_t* row_pos = nullptr;  // rows of several samples: every row's position
 };
 
 // Residual rows x [T, d], or those of `src`: adds what the product before left as partial results (S > 1: part[0 .. S - 1],

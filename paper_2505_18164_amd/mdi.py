@@ -16,9 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libmdi.so")
 MDI_ABI_VERSION = 1
 MDI_OK, MDI_ERR_ARG, MDI_ERR_STATE, MDI_ERR_CTX, MDI_ERR_NOMEM, MDI_ERR_HIP, MDI_ERR_LIMIT = 0, -1, -2, -3, -4, -5, -6
 MDI_F32, MDI_BF16 = 0, 1
-MDI_HAS_EMBED, MDI_HAS_HEAD = 1, 2
+MDI_HAS_EMBED, MDI_HAS_HEAD, MDI_KV8 = 1, 2, 4
 
-EXPORTS = ["mdi_partition_bytes", "mdi_partition_create", "mdi_prefill", "mdi_prefill_chunk", "mdi_decode_step", "mdi_decode_steps", "mdi_decode_batch",
+EXPORTS = ["mdi_partition_bytes", "mdi_partition_create", "mdi_prefill", "mdi_prefill_chunk", "mdi_prefill_batch", "mdi_decode_step", "mdi_decode_steps", "mdi_decode_batch",
            "mdi_sample_greedy", "mdi_sample_topk", "mdi_sample_topk_static", "mdi_sample_batch", "mdi_partition_sync", "mdi_seq_reset", "mdi_seq_len", "mdi_step_bytes", "mdi_time_kernel",
            "mdi_partition_info", "mdi_partition_trace", "mdi_partition_destroy", "mdi_strerror",
            "mdi_kv8_write", "mdi_kv8_read", "mdi_kv8_attn", "mdi_kv8_attn_bytes"]
@@ -75,6 +75,7 @@ def lib():
                                            vp, C.POINTER(vp)]
         L.mdi_prefill.argtypes = [vp, u32, vp, u32, vp]
         L.mdi_prefill_chunk.argtypes = [vp, u32, vp, u32, vp]
+        L.mdi_prefill_batch.argtypes = [vp, u32, C.POINTER(u32), C.POINTER(u32), vp, vp]
         L.mdi_decode_step.argtypes = [vp, u32, vp, vp]
         L.mdi_decode_steps.argtypes = [vp, u32, C.POINTER(u32), C.POINTER(vp), C.POINTER(vp)]
         L.mdi_decode_batch.argtypes = [vp, u32, C.POINTER(u32), C.POINTER(vp), C.POINTER(vp)]
@@ -149,12 +150,13 @@ class Partition:
     """One model chunk on the GPU (layers [lo, hi), optional embedding / output layers)."""
 
     def __init__(self, cfg, weights, lo, hi, has_embed=False, has_head=False, max_seqs=1, stream=None,
-                 kv_page_tokens=0, kv_pages=0, max_prefill=0, decode_path=0, device="cuda:0"):
-        """weights: {"layers": {L: {name: array}}, "wte": ...} with numpy arrays (see synth.make_weights)
+                 kv_page_tokens=0, kv_pages=0, max_prefill=0, decode_path=0, device="cuda:0", kv8=False):
+        """kv8: KV caches in 8 bits (MDI_KV8).  weights: {"layers": {L: {name: array}}, "wte": ...} with numpy arrays (see synth.make_weights)
         or tensors already on the device in storage dtype (vectors fp32)."""
         self.cfg = dict(cfg)
         self.lo, self.hi = lo, hi
-        self.flags = (MDI_HAS_EMBED if has_embed else 0) | (MDI_HAS_HEAD if has_head else 0)
+        self.kv8 = bool(kv8)
+        self.flags = (MDI_HAS_EMBED if has_embed else 0) | (MDI_HAS_HEAD if has_head else 0) | (MDI_KV8 if kv8 else 0)
         self.device = torch.device(device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.c = make_config(cfg, max_seqs, kv_page_tokens, kv_pages, max_prefill, decode_path)
@@ -231,6 +233,19 @@ class Partition:
         st = lib().mdi_prefill_chunk(self._h, seq, _ptr(acts_in), T, _ptr(acts_out))
         if st != MDI_OK:
             raise MdiError(st, "mdi_prefill_chunk")
+        return acts_out
+
+    def prefill_batch(self, seqs, lengths, acts_in, acts_out=None):
+        """First visits, or their next pieces, of several different samples (mdi_prefill_batch): acts_in holds their rows, lengths[i]
+        of sample seqs[i], one sample's after the other's."""
+        n, rows = len(seqs), sum(lengths)
+        if len(lengths) != n or acts_in.shape[0] != rows:
+            raise ValueError("a length for every sample, and as many rows as they say")
+        if acts_out is None:
+            acts_out = torch.empty((rows, self.d), dtype=self.tdtype, device=self.device)
+        st = lib().mdi_prefill_batch(self._h, n, (C.c_uint32 * n)(*seqs), (C.c_uint32 * n)(*lengths), _ptr(acts_in), _ptr(acts_out))
+        if st != MDI_OK:
+            raise MdiError(st, "mdi_prefill_batch")
         return acts_out
 
     def decode_step(self, seq, act_in, act_out=None):

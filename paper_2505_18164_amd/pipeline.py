@@ -11,7 +11,9 @@ With `drain=True` a stage takes all the messages waiting in its queue in one
 call (mdi_decode_steps) instead of one call per message: on one GPU every
 sample's message is waiting when a stage gets its turn.  With `drain="shared"`
 the waiting messages also share one pass over the stage's weights
-(mdi_decode_batch) and over the vocabulary matrix (mdi_sample_batch).
+(mdi_decode_batch) and over the vocabulary matrix (mdi_sample_batch); where
+every stage keeps its caches in 8 bits, so do the first visits
+(mdi_prefill_batch).
 No arithmetic happens here.
 """
 from __future__ import annotations
@@ -118,7 +120,22 @@ class RecurrentPipeline:
         ev = torch.cuda.Event()
         ev.record(main)
         back = [None] * ns
-        for s in range(ns):                       # first visits: one sample per message, as always
+        lengths = [len(x) for x in prompts]
+        together = shared and all(p.kv8 for p in self.blocks)
+        if together:                              # caches in 8 bits: first visits share a pass over the weights too
+            msg, last = torch.cat(list(prompts)), ev
+            packed = [torch.empty((sum(lengths), d), dtype=tdt, device=dev) for _ in range(nb)]
+            ready = torch.cuda.Event()
+            ready.record(main)
+            self.blocks[0].stream.wait_event(ready)
+            first = msg                           # lives as long as the stages may read it
+            for i, p in enumerate(self.blocks):
+                p.stream.wait_event(last)
+                msg = p.prefill_batch(list(range(ns)), lengths, msg, packed[i])
+                last = torch.cuda.Event()
+                last.record(p.stream)
+            back = [x[-1] for x in msg.split(lengths)]
+        for s in range(ns if not together else 0):   # else one sample per message, as always
             msg, e = prompts[s], ev
             for i, p in enumerate(self.blocks):
                 p.stream.wait_event(e)

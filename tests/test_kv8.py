@@ -70,3 +70,26 @@ def test_the_formula():
     code, scale = quantise(np.array([[1.0, -1.0, 0.5, 0.0], [0, 0, 0, 0], [2.0 ** -101, 0, 0, 0], [1, np.inf, 0, 0], [127, 0.5, 1.5, -2.5]]))
     assert code.tolist() == [[127, -127, 64, 0], [0] * 4, [0] * 4, [0] * 4, [127, 0, 2, -2]]     # ties to even: 63.5 is 64
     assert scale[1] == scale[2] == 0 and np.isnan(scale[3]) and scale[4] == 1
+
+
+def test_partitions_with_8_bit_caches():
+    from paper_2505_18164_amd import synth as S
+    cfg = S.llama3_8b()
+    c = mdi.make_config(cfg, max_seqs=16, kv_page_tokens=64, max_prefill=2048)
+    plain, small = mdi.partition_bytes(c, 8, 16, 0), mdi.partition_bytes(c, 8, 16, mdi.MDI_KV8)
+    rows = 8 * 16 * 8192 * 8 * 2                                              # layers, samples, positions, kv heads, key and value
+    saved = rows * (2 * 128) - rows * (128 + 4)
+    assert saved * 0.95 < plain - small <= saved
+    n = C.c_size_t(0)
+
+    def status(flags, lo=0, hi=2, over=None, **kw):
+        c = mdi.make_config(dict(S.tiny(dtype=S.DT_BF16), **(over or {})), max_seqs=2, **kw)
+        return mdi.lib().mdi_partition_bytes(C.byref(c), lo, hi, flags, C.byref(n))
+
+    assert status(mdi.MDI_KV8) == mdi.MDI_OK
+    assert status(mdi.MDI_KV8 | 1 | 2) == mdi.MDI_OK
+    assert status(8) == mdi.MDI_ERR_ARG
+    assert status(mdi.MDI_KV8, over=dict(dtype=S.DT_F32)) == mdi.MDI_ERR_ARG
+    assert status(mdi.MDI_KV8 | 2, 2, 2) == mdi.MDI_ERR_ARG                   # no blocks, no cache
+    assert status(mdi.MDI_KV8, over=dict(max_ctx=(1 << 24) + 1), kv_page_tokens=64) == mdi.MDI_ERR_ARG
+    assert mdi.lib().mdi_prefill_batch(None, 1, None, None, None, None) == mdi.MDI_ERR_ARG
