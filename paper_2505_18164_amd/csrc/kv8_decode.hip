@@ -10,12 +10,13 @@
 // whichever byte of whichever row's word it is (one conversion, and one byte permutation for two of them).
 //
 // What bounds it: memory.  A code takes 1.5 vector instructions, a score about ten; a wavefront spends 0.7 us on 32 positions,
-// 40 % of the time that twelve of them on a compute unit have until the memory has answered.  Nothing is fetched ahead inside a
+// 40 % of the time that twelve of them on a compute unit have until the memory has answered, so that a second product for the lower
+// digits of the weights (error of the results 0.0024 -> 0.0017 of their size, which is their own rounding) costs 0.7 us of 30.  Nothing is fetched ahead inside a
 // wavefront: a second tile of registers (217 of them, two workgroups a compute unit) only made every load wait longer, the first ones of
 // a unit - page numbers, query - included (8 samples of the 7B shape 42 us, 16 of the 8B shape 55).
-// Shares instead of pieces of one length: 8 samples of 1 .. 4096 positions 41 -> 29.8 us (a piece is as long as the longest
+// Shares instead of pieces of one length: 8 samples of 1 .. 4096 positions 41 -> 29.8 us at that step (a piece is as long as the longest
 // sample's, and few of them are); what a unit costs to begin has to count, or 32 short ones after the other are one workgroup's (69 us).
-// 16 samples of 8100 positions of the 8B shape: 53 us = 5.2 TB/s of codes and scales, 8 of the 7B shape 4.5 TB/s.
+// 16 samples of 8100 positions of the 8B shape: 51.7 us = 5.3 TB/s of codes and scales, 8 of the 7B shape 29.0 us = 4.7 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -141,6 +142,18 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
       }
     };
     auto use = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
+      // What has been asked for is looked at from here on: a product or a shift that is moved up to a load waits for it there
+      // (pages of 40 positions, one sample of 120001 of the 8B shape: 50 -> 69 us).
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float ks = t.ks[u][j], vs = t.vs[u][j];
+          asm volatile("" : "+v"(ks), "+v"(vs));
+          t.ks[u][j] = ks; t.vs[u][j] = vs;
+#pragma unroll
+          for (int w = 0; w < KI; ++w) asm volatile("" : "+v"(t.v[u][j][w]));
+        }
       f32x4 s[2];
       float p[2][4];
 #pragma unroll
@@ -189,24 +202,37 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
           l += p[u][j];
           p[u][j] *= t.vs[u][j];
         }
-      bf16x8 pf;                                                   // the one rounding of a weight: to the matrix cores' operand
+      // A weight as two bf16 operands, its upper digits and what they leave, which is sixteen digits of it: one alone
+      // would be off by as much as the rounding of the result.
+      u32x4 hi_w;
+      bf16x8 lo_w;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) pf[4 * u + j] = (__bf16)p[u][j];
+        for (int j = 0; j < 4; j += 2) {
+          hi_w[2 * u + j / 2] = high_halves(p[u][j], p[u][j + 1]);
+          lo_w[4 * u + j] = (__bf16)(p[u][j] - __uint_as_float(__float_as_uint(p[u][j]) & 0xFFFF0000u));
+          lo_w[4 * u + j + 1] = (__bf16)(p[u][j + 1] - __uint_as_float(__float_as_uint(p[u][j + 1]) & 0xFFFF0000u));
+        }
 #pragma unroll
       for (int w = 0; w < KI; ++w) {
-        auto block = [&](auto byte) __attribute__((always_inline)) {
+        auto operand = [&](auto byte) __attribute__((always_inline)) {
           constexpr int N = decltype(byte)::value;
-          const u32x4 f = {high_halves(code_of<N>(t.v[0][0][w]), code_of<N>(t.v[0][1][w])), high_halves(code_of<N>(t.v[0][2][w]), code_of<N>(t.v[0][3][w])),
-                           high_halves(code_of<N>(t.v[1][0][w]), code_of<N>(t.v[1][1][w])), high_halves(code_of<N>(t.v[1][2][w]), code_of<N>(t.v[1][3][w]))};
-          o[4 * w + N] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pf, o[4 * w + N], 0, 0, 0);
+          return __builtin_bit_cast(bf16x8, u32x4{high_halves(code_of<N>(t.v[0][0][w]), code_of<N>(t.v[0][1][w])), high_halves(code_of<N>(t.v[0][2][w]), code_of<N>(t.v[0][3][w])),
+                                                  high_halves(code_of<N>(t.v[1][0][w]), code_of<N>(t.v[1][1][w])), high_halves(code_of<N>(t.v[1][2][w]), code_of<N>(t.v[1][3][w]))});
+        };
+        auto blocks = [&](auto byte) __attribute__((always_inline)) {   // two: a product waits for the one before it on the same sums
+          constexpr int N = decltype(byte)::value;
+          const bf16x8 f0 = operand(std::integral_constant<int, N>()), f1 = operand(std::integral_constant<int, N + 1>());
+          f32x4 &o0 = o[4 * w + N], &o1 = o[4 * w + N + 1];
+          o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, __builtin_bit_cast(bf16x8, hi_w), o0, 0, 0, 0);
+          o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, __builtin_bit_cast(bf16x8, hi_w), o1, 0, 0, 0);
+          o0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, lo_w, o0, 0, 0, 0);
+          o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, lo_w, o1, 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         };
-        block(std::integral_constant<int, 0>());
-        block(std::integral_constant<int, 1>());
-        block(std::integral_constant<int, 2>());
-        block(std::integral_constant<int, 3>());
+        blocks(std::integral_constant<int, 0>());
+        blocks(std::integral_constant<int, 2>());
       }
     };
 
