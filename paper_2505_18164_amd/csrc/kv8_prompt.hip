@@ -13,7 +13,17 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 constexpr int BK = 64;               // keys of a step
+// Weights and values are multiplied as fp16, which has three more digits than bf16 (with bf16 the results were off by 0.0026 of
+// their size, of which their own rounding is 0.0017) and a smaller range.  Weights are counted so that the largest of a row's first
+// block is 2^kTop, and counted anew when one would exceed 2^kRaise; one below 2^-14 keeps the digits down to 2^-24, 2^-30 of the
+// largest.  Values are multiplied by a power of two, so far that a row's largest magnitude is at most 2^13 where that is
+// chosen, and up to 2^15 before it is chosen anew: a row of 2^-27 of the largest one's size still has the digits of a bf16.
+constexpr float kTop = 6.f, kRaise = 14.f;
+constexpr float kUnitFirst = 0x1p100f;                           // scales are zero, or 2^-107 and more
 
 __device__ __forceinline__ u32x2 read_transposed(const bf16_t* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p));
@@ -60,7 +70,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   constexpr int UB = 64 * HD / GT < 16 ? 64 * HD / GT : 16;      // codes a thread moves at a time
   constexpr int KU = 64 * HD / (GT * UB), PER = HD / UB;         // ... and how often; threads a key
   constexpr int NB = 2;                                          // buffers of keys, and of values
-  constexpr int KV = NB * BK * (KS + VR) + 8 * BK;               // bf16 elements of a group: keys, values, scales of four blocks of keys
+  constexpr int KV = NB * BK * (KS + VR) + 8 * BK + 8;           // 16-bit elements of a group: keys, values, scales of four blocks of keys, units of four blocks of values
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int tid = threadIdx.x & (GT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -68,6 +78,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   bf16_t* const Kb = (bf16_t*)smem + grp * KV;
   bf16_t* const Vb = Kb + NB * BK * KS;
   float* const Sc = (float*)(Vb + NB * BK * VR);                 // [4][64]
+  float* const Un = Sc + 4 * BK;                                 // [4]
   // A sample's longest rows first, and of those all sets.  (Workgroups are handed to the eight compute dies, each with an L2 of its
   // own, in turn: with a multiple of eight sets, a set stays on its die.)
   const int block = blockIdx.x / geo.sets, set = blockIdx.x - block * geo.sets;
@@ -115,6 +126,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   const int n_kb = (hi - lo + BK - 1) / BK, n_it = (n_kb + NG - 1) / NG;
   u32x4 kreg[KU], vreg[KU];
   float vs[KU], sk = 0.f, sv = 0.f;
+  float unit = kUnitFirst, made = kUnitFirst, mine = kUnitFirst;  // of the block whose values are staged; newest that was chosen; of o
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
   auto checked = [&](int page) __attribute__((always_inline)) {
     worst = max(worst, (unsigned)page);
@@ -196,15 +208,24 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   };
   auto stash_values = [&](int j, int n) __attribute__((always_inline)) {
     const int u = n / (UB / 8), h = n % (UB / 8), at = tid + u * GT;
-    const float f = __uint_as_float(here(__float_as_uint(vs[u]))), by = f - f == 0.f ? f : 0.f;
+    const float f = __uint_as_float(here(__float_as_uint(vs[u]))), by = f - f == 0.f ? f * unit : 0.f;
     const uint32_t w0 = here(vreg[u][2 * h]), w1 = here(vreg[u][2 * h + 1]);
-    *reinterpret_cast<bf16x8*>(Vb + ((j - 1) & 1) * BK * VR + at / PER * VR + UB * (at % PER) + 8 * h) =
-        bf16x8{(__bf16)(code_of<0>(w0) * by), (__bf16)(code_of<1>(w0) * by), (__bf16)(code_of<2>(w0) * by), (__bf16)(code_of<3>(w0) * by),
-               (__bf16)(code_of<0>(w1) * by), (__bf16)(code_of<1>(w1) * by), (__bf16)(code_of<2>(w1) * by), (__bf16)(code_of<3>(w1) * by)};
+    *reinterpret_cast<f16x8*>(Vb + ((j - 1) & 1) * BK * VR + at / PER * VR + UB * (at % PER) + 8 * h) =
+        f16x8{(_Float16)(code_of<0>(w0) * by), (_Float16)(code_of<1>(w0) * by), (_Float16)(code_of<2>(w0) * by), (_Float16)(code_of<3>(w0) * by),
+              (_Float16)(code_of<0>(w1) * by), (_Float16)(code_of<1>(w1) * by), (_Float16)(code_of<2>(w1) * by), (_Float16)(code_of<3>(w1) * by)};
   };
   auto stash_scales = [&](int j) __attribute__((always_inline)) {
     const float v = __uint_as_float(here(__float_as_uint(sv)));
-    if (wave == 0) Sc[64 * (j & 3) + lane] = v - v == 0.f ? sk * a.scale : __uint_as_float(0x7FC00000u);   // a value that is not finite makes its weight NaN (and is staged as zeros)
+    if (wave == 0) {
+      const bool fine = v - v == 0.f;
+      Sc[64 * (j & 3) + lane] = fine ? sk * a.scale : __uint_as_float(0x7FC00000u);   // a value that is not finite makes its weight NaN (and is staged as zeros)
+      if (__builtin_expect(__any(v * made > 256.f), 0)) {
+        float top = fine ? v : 0.f;
+        for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        if (top * made > 256.f) made = __uint_as_float((127 + 5 + 127 - (__float_as_uint(top) >> 23)) << 23);   // top is less than 2^6 of these
+      }
+      if (lane == 0) Un[j & 3] = made;
+    }
   };
 
   const int v_lane = (4 * half + ((lane & 15) >> 2)) * VR + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -218,6 +239,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     constexpr int kSets = decltype(keys)::value ? 2 * HT : HT;   // sets of four operands: HT of values, HT of keys
     const bf16_t* const V = Vb + ((j - 1) & 1) * BK * VR + v_lane;
     const bf16_t* const K = Kb + (j & 1) * BK * KS + col * KS + 8 * half;
+    if constexpr (decltype(keys)::value) unit = Un[j & 3];
     u32x4 f[2][4];
     auto read = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
@@ -238,12 +260,11 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const bf16x8 op = __builtin_bit_cast(bf16x8, f[n & 1][x]);
         if (n < HT) {
-          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, __builtin_bit_cast(bf16x8, pf[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
+          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, f[n & 1][x]), __builtin_bit_cast(f16x8, pf[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
         } else {
           const int k = 2 * (n - HT) + (x >> 1);
-          s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[k], k ? s[x & 1] : f32x16{}, 0, 0, 0);
+          s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), qf[k], k ? s[x & 1] : f32x16{}, 0, 0, 0);
         }
       }
       if constexpr (decltype(keys)::value) {                     // staging, in between
@@ -259,8 +280,9 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     }
   };
   // The weights of block j from its scores.  They are counted from m, the row's reference, which is the largest score of the first
-  // block and is raised - in both lanes of a row alike - when a score exceeds it by 2^kKv8Raise: the sum is divided out at
-  // the end, so any reference near the largest score does.  The sum takes the weights as they are multiplied, rounded to bf16.
+  // block and is raised - in both lanes of a row alike - when a weight would exceed 2^kRaise: the sum is divided out at
+  // the end, so any reference near the largest score does.  The sum takes the weights as they are multiplied, cut to
+  // fp16 (by the conversion that is 2 us of 58 faster than the one to the nearest: eight prompts of TinyLlama).
   float alpha = 1.f;
   bool raised = false;
   auto weigh = [&](int j, auto mask) __attribute__((always_inline)) {
@@ -281,9 +303,9 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
           top = fmaxf(top, s[t][e]);
         }
       }
-    if (__builtin_expect(first || __any(top > kKv8Raise), 0)) {
+    if (__builtin_expect(first || __any(top > kRaise), 0)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float by = first ? top : fmaxf(top, 0.f);
+      const float by = first ? top - kTop : fmaxf(top - kTop, 0.f);
       alpha = first ? 1.f : exp2_raw(-by);
       raised = !first;
       m += by;
@@ -298,8 +320,8 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const bf16x2 w = {(__bf16)exp2_raw(s[t][e]), (__bf16)exp2_raw(s[t][e + 1])};
-        l = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+        const f16x2 w = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(exp2_raw(s[t][e]), exp2_raw(s[t][e + 1])));
+        l = __builtin_amdgcn_fdot2(w, f16x2{(_Float16)1.f, (_Float16)1.f}, l, false);
         pf[2 * t + (e >> 3)][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
       }
   };
@@ -311,6 +333,11 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     }
     const int k0 = lo + (NG * j + grp) * BK;
     if (k0 + BK - 1 > wave_pos || k0 + BK > hi) weigh(j, std::true_type()); else weigh(j, std::false_type());
+    if (__builtin_expect(unit != mine, 0)) {                     // the block's values are counted in another unit than the sums
+      alpha = (raised ? alpha : 1.f) * (unit / mine);
+      raised = true;
+      mine = unit;
+    }
   };
 
   // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies and stages, the other takes exponentials; so the later
@@ -345,7 +372,15 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   products(n_it, std::false_type());
   if (!late) __syncthreads();
   __syncthreads();
-  if (first) m = kKv8None;                                       // saw nothing
+  // the largest weights count as one again, and the sums in the values' own unit
+  m = first ? kKv8None : m + kTop;                               // (first: saw nothing)
+  l *= exp2f(-kTop);
+  const float own = exp2f(-kTop) / mine;
+
+#pragma unroll
+  for (int i = 0; i < HT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] *= own;
 
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
   if constexpr (NG > 1) {
@@ -398,7 +433,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
 
 template <int HD, int NG>
 constexpr size_t prompt_lds() {
-  const size_t kv = (size_t)NG * (2 * BK * (HD + 8 + HD + 32) + 8 * BK) * sizeof(bf16_t);
+  const size_t kv = (size_t)NG * (2 * BK * (HD + 8 + HD + 32) + 8 * BK + 8) * sizeof(bf16_t);
   const size_t fold = (size_t)(NG - 1) * (HD / 2 + 2) * (512 / NG) * sizeof(float);
   return kv > fold ? kv : fold;
 }

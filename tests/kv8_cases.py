@@ -22,10 +22,11 @@ def quantise(x):
 
 
 def attention(q, k, v, p0, scale):
-    """q [T, H, h] at positions p0 ..; k, v [ctx, K, h]: (out, sum of w |v|, largest sum of |scale q k| of a row [T, H, 1])."""
+    """q [T, H, h] at positions p0 ..; k, v [ctx, K, h]: (out, sum of w |v|, largest sum of |scale q k| of a row [T, H, 1],
+    2^-30 sum of |v| + 2^-36 max |v|)."""
     T, H, h = q.shape
     G = H // k.shape[1]
-    out, mag, big = np.zeros((T, H, h)), np.zeros((T, H, h)), np.zeros((T, H, 1))
+    out, mag, big, low = np.zeros((T, H, h)), np.zeros((T, H, h)), np.zeros((T, H, 1)), np.zeros((T, H, h))
     for i in range(H):
         kk, vv = k[:, i // G], v[:, i // G]
         s = scale * (q[:, i] @ kk.T)
@@ -35,23 +36,27 @@ def attention(q, k, v, p0, scale):
         w /= w.sum(axis=1, keepdims=True)
         out[:, i], mag[:, i] = w @ vv, w @ np.abs(vv)
         big[:, i, 0] = np.where(seen, np.abs(scale) * (np.abs(q[:, i]) @ np.abs(kk).T), 0.0).max(axis=1)
-    return out, mag, big
+        low[:, i] = 2.0 ** -30 * (seen @ np.abs(vv)) + 2.0 ** -36 * np.abs(vv).max()
+    return out, mag, big, low
 
 
-def bound(out, mag, big, h):
+def bound(out, mag, big, low, h):
     """How far a bf16 result may be from `out`: its own rounding; one rounding to bf16 of every weight, of relative size
     2^-8, moves the weighted sum by up to 2^-8 sum w |v|, and the sum of weights likewise where it is taken of rounded ones;
     a score is a sum of h exact products and four factors in fp32, off by (h + 8) 2^-24 of the sum of magnitudes, which moves
     its weight by that, once above and once below the line; exponentials and the sums of up to 2^14 weights add 2^-24 each
-    (pairwise or in runs of at most 2^7 by lane, so 2^7 2^-24 bounds them)."""
+    (pairwise or in runs of at most 2^7 by lane, so 2^7 2^-24 bounds them).  Weights that are rounded to fp16 with the
+    largest one at 2^6 or more are off by 2^-11 of themselves, as above, or, below 2^-14, by half a step of 2^-24: 2^-31 of the
+    largest, each of them, above and below the line; values in fp16 with the largest of a row at 2^12 or more by 2^-11 or
+    2^-25 / 2^12 of the largest of any row (which may be a later row's)."""
     delta = (h + 8) * 2.0 ** -24 * big
-    return 2.0 ** -8 * np.abs(out) + (2 * 2.0 ** -8 + 2 * delta + 2 * 2.0 ** -17) * mag * 1.01 + 1e-30
+    return 2.0 ** -8 * np.abs(out) + (2 * 2.0 ** -8 + 2 * delta + 2 * 2.0 ** -17) * mag * 1.01 + low * 1.01 + 1e-30
 
 
 class Setup:
     """A cache on the GPU with `behind` earlier positions and `lens` new rows per sample, filled by the formula in 64 bits."""
 
-    def __init__(self, H, K, h, pt, lens, behind, seed=0, spare=2, stale="nan", pos_of=None, k_gain=1.0, rows_behind=0):
+    def __init__(self, H, K, h, pt, lens, behind, seed=0, spare=2, stale="nan", pos_of=None, k_gain=1.0, rows_behind=0, v_gain=None):
         rng = np.random.default_rng(seed)
         self.H, self.K, self.h, self.pt, self.lens, self.behind = H, K, h, pt, lens, behind
         n = len(lens)
@@ -69,6 +74,8 @@ class Setup:
             at += used[i]
             x = rng.standard_normal((2, total[i], K, h)).astype(np.float32)
             x[0] *= k_gain
+            if v_gain is not None:
+                x[1] *= v_gain(np.arange(total[i]))[:, None, None]
             code, scale = quantise(x)
             self.kv.append(code.astype(np.float64) * scale.astype(np.float64)[..., None])
             for p in range(total[i]):
@@ -99,9 +106,9 @@ class Setup:
 
 
 def check(got, want, h, what=""):
-    out, mag, big = want
+    out, mag, big, low = want
     got = got.float().cpu().double().numpy()[:out.shape[0]]
-    off, may = np.abs(got - out), bound(out, mag, big, h)
+    off, may = np.abs(got - out), bound(out, mag, big, low, h)
     if not (off <= may).all():
         at = np.unravel_index(np.argmax(np.where(np.isnan(off), np.inf, off / may)), off.shape)
         raise AssertionError(f"{what}: row, head, channel {at}: {got[at]} instead of {out[at]}, may be off by {may[at]:.3g}")

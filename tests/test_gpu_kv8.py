@@ -171,6 +171,31 @@ def test_long_contexts_are_divided_and_joined(H, K, h, pt, ctx, one_each):
     cache.check()
 
 
+GAINS = {
+    "growing": lambda p: 2.0 ** np.minimum(p / 8.0 - 30, 60),                   # every block of positions larger than the one before
+    "falling": lambda p: 2.0 ** np.maximum(20 - p / 8.0, -90),
+    "here and there": lambda p: np.where(p % 67 == 66, 2.0 ** 14, np.where(p % 5 == 3, 2.0 ** -9, 1.0)),
+    "zeros first": lambda p: np.where(p < 70, 0.0, 1.0),
+    "all zeros": lambda p: 0.0 * p,
+    "tiny": lambda p: 2.0 ** -94 + 0.0 * p,
+    "huge": lambda p: np.where(p < 100, 1.0, 2.0 ** 90),
+}
+
+
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("gain", list(GAINS))
+def test_values_of_all_sizes(gain, h):
+    """Values are multiplied as fp16 of a size that the kernel keeps up with."""
+    for lens, behind, pt in (([150, 1, 64], [0, 330, 500], 64), ([260], [40], 24), ([20, 9], [900, 1500], 64)):
+        s = Setup(4, 2, h, pt, lens, behind, seed=3, v_gain=GAINS[gain])
+        cache = s.cache()
+        check(cache.attn(s.plan(cache), s.q.to(DEV)), s.want(), h, (lens, pt))
+        assert int(s.err.cpu()[0]) == 0
+    s = Setup(4, 2, h, 16, [1, 1, 1], [0, 500, 79], seed=4, v_gain=GAINS[gain])
+    cache = s.cache()
+    check(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), s.want(), h, "one each")
+
+
 @pytest.mark.parametrize("h", [64, 128, 48])
 def test_values_that_decide_alone_and_far_apart(h):
     """Loud keys: one position's weight is all but 1; scores of hundreds either way, and growing along the cache."""
