@@ -823,7 +823,7 @@ mdi_status visit_kv8(mdi_partition* p, int n, const uint32_t* seqs, const uint32
   RowSource src{in, embed ? IN_TOKEN : ak, (uintptr_t)in % (4 * p->esz) == 0, p->wte, p->wpe, (int)c.vocab, p->err, a.pos[0]};
   if (several) src.row_pos = a.row_pos;
   const float2* rope = several ? p->p_rope : p->rope ? p->rope + (size_t)a.pos[0] * (h / 2) : nullptr;
-  const PageDivide pd = page_divide(p->Tm);  // the rows' keys and values: a page of Tm positions, [K][2][Tm][h]
+  const PageDivide pd{30, 0};                // the rows' keys and values: one page of Tm (at most 2^24) positions, [K][2][Tm][h]
   const Kv8Rows r{a.table, single ? nullptr : a.start, a.at, n, rows, ctx};
   const Kv8RowsIO io{p->p_kv, p->p_kv + (size_t)p->Tm * h, h, 2l * p->Tm * h};
   const Kv8Plan plan = kv8_plan(kv8_cache(p, p->layers[0]), r, H, p->kv8_part_cap);

@@ -214,3 +214,16 @@ def test_a_ring_of_nodes_generates():
         for drain, (logits, toks) in got.items():
             check(logits[s, 0], want, cfg, (drain, s))
             assert (toks[s] == logits[s].argmax(-1)).all()        # the tokens are those of the logits it returns
+
+
+def test_more_rows_than_two_bytes_count():
+    """A prompt of 70001 rows in one pass, and in pieces of 8000: what a row's keys and values are does not depend on it."""
+    cfg = S.tiny(n_layer=1, d_model=64, n_head=1, n_kv_head=1, head_dim=64, d_ff=64, vocab=61, max_ctx=70001, dtype=S.DT_BF16)
+    w = S.make_weights(cfg, 31, exercise=True)
+    x = dev_acts(S.make_activations(cfg, 9, 0, 70001), cfg)
+    one, pieces = (mdi.Partition(cfg, w, 0, 1, max_seqs=1, kv_page_tokens=64, max_prefill=most, kv8=True) for most in (70001, 8000))
+    a = one.prefill(0, x)
+    b = torch.cat([pieces.prefill_chunk(0, x[at:at + 8000]) for at in range(0, 70001, 8000)])
+    one.sync()
+    pieces.sync()
+    assert rel_l2_rows(host(a), host(b)).max() < 2 * tol(cfg)         # each is that close to the exact result
