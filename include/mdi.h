@@ -176,7 +176,7 @@ MDI_API mdi_status mdi_partition_bytes(const mdi_config *cfg, uint32_t layer_lo,
  * MDI_KV8 = the KV caches are kept in 8 bits (see mdi_kv8): (head_dim + 4) bytes
  * for a position's key or value of a kv head instead of 2 * head_dim, so the same
  * memory holds nearly twice the samples or positions.  Needs blocks, MDI_BF16,
- * max_ctx at most 2^24.  All positions - a first visit's own as well - are read
+ * max_ctx at most 2^24, max_prefill * n_head below 2^24.  All positions - a first visit's own as well - are read
  * as the cache holds them, so a prompt in pieces and in one gives the same keys
  * and values.  Such a partition runs one kernel per operation; several samples
  * share a pass over the weights in mdi_decode_batch and mdi_prefill_batch, up to
@@ -505,7 +505,8 @@ typedef struct mdi_kv8_rows {
  * Quantise rows into the cache: k and v are device arrays of dtype (MDI_F32 or
  * MDI_BF16), element (row, kv head, channel) at row * row_stride + head *
  * head_stride + channel - the parts of a fused QKV product as they stand, for
- * instance.  Both 16-byte aligned, strides multiples of 16 bytes.  No two rows of
+ * instance.  Both 16-byte aligned, strides multiples of 16 bytes; n_rows *
+ * n_kv_head * head_dim below 2^33.  No two rows of
  * a call may go to the same position of the same page.  The call enqueues on
  * hip_stream (NULL: the default stream), whose device has to be current, and
  * returns; the library keeps nothing.  The same holds for the calls below.
@@ -531,7 +532,9 @@ MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, 
  * apart, 16-byte aligned, strides multiples of 8; they must not overlap.
  * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
  * binary32.  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
- * 2^30, n * n_head * (max_ctx / 128 + 1) below 2^31.
+ * 2^24, n * n_head * (max_ctx / 128 + 3) below 2^30.  Products take a weight with 16
+ * digits for single tokens and as a binary16 of at least 2^-24, the largest being 2^6
+ * or more, for packed rows of 64 or 128 channels.
  * workspace: mdi_kv8_attn_bytes() bytes of device memory, 16-byte aligned (0 bytes:
  * may be NULL); it carries nothing from one call to the next, and calls that can
  * run at the same time need one each.  Results do not depend on timing.

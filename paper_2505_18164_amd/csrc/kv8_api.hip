@@ -27,10 +27,11 @@ mdi_status take(const mdi_kv8* k, const mdi_kv8_rows* g, Kv8Cache* c, Kv8Rows* r
   return st != MDI_OK ? st : take_rows(k, g, r);
 }
 
-// Query rows of the call: heads that the kv heads divide, rows of 16-byte pieces.
+// Query rows of the call: heads that the kv heads divide.  A launch has fewer than 2^32 threads, 256 a row and head; the tiles of all
+// units, and kKv8Begin more each, are counted in 32 bits.
 bool good_heads(const Kv8Cache& c, const Kv8Rows& r, uint32_t n_head) {
-  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 30) &&
-         (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 1) < (1ull << 31);   // tiles of all units are counted in 32 bits
+  return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 24) &&
+         (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 3) < (1ull << 30);
 }
 
 mdi_status hip_status() { return hipGetLastError() == hipSuccess ? MDI_OK : MDI_ERR_HIP; }
@@ -42,6 +43,7 @@ mdi_status rows_io(const mdi_kv8* k, const mdi_kv8_rows* g, void* kp, void* vp, 
   if (dtype > MDI_BF16) return MDI_ERR_ARG;
   const uint64_t unit = dtype == MDI_BF16 ? 8 : 4;               // elements of 16 bytes
   if ((r->n && r->n_rows && (!kp || !vp)) || !aligned16(kp) || !aligned16(vp) || row_stride % unit || head_stride % unit) return MDI_ERR_ARG;
+  if ((uint64_t)r->n_rows * c->K * c->h >= 1ull << 33) return MDI_ERR_ARG;       // a launch has fewer than 2^32 threads
   if (row_stride > 1ull << 38 || head_stride > 1ull << 38) return MDI_ERR_ARG;   // offsets stay within 64 bits
   *io = Kv8RowsIO{kp, vp, (long)row_stride, (long)head_stride};
   return MDI_OK;
@@ -87,7 +89,8 @@ mdi_status mdi_kv8_attn(const mdi_kv8* cache, const mdi_kv8_rows* rows, const vo
   if ((r.n && r.n_rows && (!q || !out)) || !aligned16(q) || !aligned16(out) || !good_heads(c, r, n_head)) return MDI_ERR_ARG;
   const uint64_t width = (uint64_t)n_head * c.h;
   if (q_stride < width || out_stride < width || q_stride % 8 || out_stride % 8 || q_stride > 1ull << 38 || out_stride > 1ull << 38) return MDI_ERR_ARG;
-  if (!(scale - scale == 0.f)) return MDI_ERR_ARG;                // finite
+  const float scale2 = scale * 1.44269504f;                      // scores are exponents of two
+  if (!(scale2 - scale2 == 0.f)) return MDI_ERR_ARG;              // finite
   if (!r.n || !r.n_rows) return MDI_OK;
   const Kv8Plan plan = kv8_plan(c, r, (int)n_head);
   const size_t need = kv8_part_bytes(plan, c, r, (int)n_head);
@@ -95,7 +98,7 @@ mdi_status mdi_kv8_attn(const mdi_kv8* cache, const mdi_kv8_rows* rows, const vo
   if (need > workspace_bytes) return MDI_ERR_NOMEM;
   if (!kv8_allow_lds()) return MDI_ERR_HIP;
   launch_kv8_attn((hipStream_t)hip_stream, c, r,
-                  Kv8Attn{(const bf16_t*)q, (long)q_stride, (bf16_t*)out, (long)out_stride, (int)n_head, scale * 1.44269504f, (float*)workspace, plan});
+                  Kv8Attn{(const bf16_t*)q, (long)q_stride, (bf16_t*)out, (long)out_stride, (int)n_head, scale2, (float*)workspace, plan});
   return hip_status();
 }
 

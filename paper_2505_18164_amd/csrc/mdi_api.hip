@@ -155,6 +155,7 @@ mdi_status check_config(const mdi_config* c, uint32_t lo, uint32_t hi, uint32_t 
     Kv8Cache geometry;
     const uint64_t pt = c->kv_page_tokens ? c->kv_page_tokens : 16, stride = (c->max_ctx + pt - 1) / pt;
     if (lo == hi || c->dtype != MDI_BF16 || c->max_ctx > 1u << 24 || c->n_head > 4096 || c->max_seqs > 1u << 20) return MDI_ERR_ARG;
+    if ((uint64_t)(c->max_prefill ? c->max_prefill : c->max_ctx) * c->n_head >= 1u << 24) return MDI_ERR_ARG;   // as of mdi_kv8_attn
     if (!kv8_geometry(c->kv_pages ? c->kv_pages : c->max_seqs * stride, c->n_kv_head, c->head_dim, pt, c->max_seqs, stride, &geometry)) return MDI_ERR_ARG;
   }
   return MDI_OK;

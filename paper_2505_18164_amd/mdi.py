@@ -391,8 +391,8 @@ _KV8_TYPES = {torch.bfloat16: MDI_BF16, torch.float32: MDI_F32}
 class Kv8Rows:
     """The rows of a call (mdi_kv8_rows), made by Kv8Cache.rows; keeps its device arrays alive."""
 
-    def __init__(self, keep, struct, n_rows):
-        self._keep, self._c, self.n_rows = keep, struct, n_rows
+    def __init__(self, keep, struct, n_rows, device):
+        self._keep, self._c, self.n_rows, self.device = keep, struct, n_rows, device
         self._ref = C.byref(struct)
 
 
@@ -445,13 +445,15 @@ class Kv8Cache:
             raise ValueError("n_rows: the rows of the buffers are not read from the device")
         n_rows = n if n_rows is None else n_rows
         max_ctx = self.tables.shape[1] * self.page_tokens if max_ctx is None else max_ctx
-        return Kv8Rows((pos, start, table), MdiKv8Rows(_ptr(table), _ptr(start), _ptr(pos), n, n_rows, max_ctx), n_rows)
+        if not (0 <= n_rows < 1 << 32 and 0 <= max_ctx < 1 << 32):
+            raise ValueError("n_rows, max_ctx: beyond 32 bits")
+        return Kv8Rows((pos, start, table), MdiKv8Rows(_ptr(table), _ptr(start), _ptr(pos), n, n_rows, max_ctx), n_rows, self.device)
 
     def _rows_io(self, rows, k, v, what):
         shape, stride, dtype = k.shape, k.stride(), k.dtype
         if shape != (rows.n_rows, self.K, self.h) or stride[2] != 1 or v.shape != shape or v.stride() != stride or v.dtype != dtype:
             raise ValueError(f"{what}: k and v [rows, kv heads, head_dim] of one type and layout, channels next to each other")
-        if dtype not in _KV8_TYPES or k.device != self.device or v.device != self.device:
+        if dtype not in _KV8_TYPES or k.device != self.device or v.device != self.device or rows.device != self.device:
             raise ValueError(f"{what}: bfloat16 or float32 on {self.device}")
         return k.data_ptr(), v.data_ptr(), _KV8_TYPES[dtype], stride[0] if shape[0] > 1 else self.K * self.h, stride[1] if shape[1] > 1 else self.h
 
@@ -479,11 +481,14 @@ class Kv8Cache:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         shape, qs, os, h = q.shape, q.stride(), out.stride(), self.h
         if (len(shape) != 3 or shape[0] != rows.n_rows or shape[2] != h or out.shape != shape or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16
-                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or q.device != self.device or out.device != self.device):
+                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or q.device != self.device or out.device != self.device
+                or rows.device != self.device):
             raise ValueError(f"attn: q and out bfloat16 [rows, heads, {h}] on {self.device}, heads next to each other")
         heads = shape[1]
         if workspace is None:
             workspace = self.workspace(rows, heads)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"attn: a contiguous workspace on {self.device}")
         alone = shape[0] < 2                                     # a lone row has no neighbours, whatever its stride says
         self._call("mdi_kv8_attn", self._ref, rows._ref, q.data_ptr(), heads * h if alone else qs[0], heads, h ** -0.5 if scale is None else scale,
                    out.data_ptr(), heads * h if alone else os[0], None if workspace is None else workspace.data_ptr(),

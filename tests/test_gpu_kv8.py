@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from kv8_cases import Setup, check, quantise
+from kv8_cases import Setup, attention, check, quantise
 from paper_2505_18164_amd import mdi
 
 pytestmark = pytest.mark.gpu
@@ -373,3 +373,71 @@ def test_nothing_to_do_and_refusals():
     with pytest.raises(mdi.MdiError) as e:
         cache.attn(s.plan(cache), s.q.to(DEV), workspace=space)
     assert e.value.status == mdi.MDI_ERR_NOMEM
+
+
+@pytest.mark.parametrize("H,K,h,pt,ctx", [(4, 1, 64, 16, [70000, 5]), (2, 1, 128, 1, [5000, 300]), (4, 2, 64, 3, [6200, 1])], ids=["many pieces", "pages of one", "pages of three"])
+def test_more_pieces_and_pages_than_are_looked_at_at_a_time(H, K, h, pt, ctx):
+    s = Setup(H, K, h, pt, [1] * len(ctx), [c - 1 for c in ctx], seed=6)
+    cache = s.cache()
+    q = s.q.to(DEV)
+    check(cache.attn(s.plan(cache, one_each=True), q), s.want(), h, "one each")
+    check(cache.attn(s.plan(cache), q), s.want(), h, "packed")
+    assert int(s.err.cpu()[0]) == 0
+
+
+@pytest.mark.parametrize("h", [64, 128, 16])
+def test_more_samples_than_are_looked_at_at_a_time(h):
+    """131 samples, three of 64 and one: some without rows, some that take no part, long ones last."""
+    lens = [(7 * i) % 4 for i in range(128)] + [40, 0, 3]
+    behind = [(13 * i) % 90 for i in range(128)] + [0, 9, 1900]
+    s = Setup(4, 2, h, 16, lens, behind, seed=7)
+    absent = [5, 63, 64, 127, 128]
+    s.pos[absent] = -1
+    cache = s.cache()
+    want = s.want()
+    rows = np.concatenate([np.arange(s.start[i], s.start[i + 1]) for i in absent])
+    for w in want:
+        w[rows] = 0
+    check(cache.attn(s.plan(cache), s.q.to(DEV)), want, h, "packed")
+    s = Setup(4, 2, h, 16, [1] * 131, [(13 * i) % 90 for i in range(129)] + [2500, 700], seed=8)
+    s.pos[absent] = -1
+    cache = s.cache()
+    want = s.want()
+    for w in want:
+        w[absent] = 0
+    check(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), want, h, "one each")
+
+
+def test_two_graphs_share_a_workspace_and_one_sample_is_asked_twice():
+    a = Setup(8, 2, 64, 16, [1, 1], [4000, 900], seed=9)
+    b = Setup(8, 2, 64, 16, [64], [6000], seed=10)
+    ca, cb = a.cache(), b.cache()
+    twice = torch.tensor([1, 1], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([900, 500], dtype=torch.int32, device=DEV)     # the second sees less of the same sample
+    ra, rb = ca.rows(pos, table=twice, max_ctx=4001), b.plan(cb)
+    qa, qb = a.q.to(DEV), b.q.to(DEV)
+    wa, wb = ca.workspace(ra, 8), cb.workspace(rb, 8)
+    assert wa is not None and wb is not None                          # both are divided
+    work = torch.empty(max(wa.numel(), wb.numel()), dtype=torch.uint8, device=DEV)
+    oa, ob = torch.empty_like(qa), torch.empty_like(qb)
+    ca.attn(ra, qa, out=oa, workspace=work)
+    cb.attn(rb, qb, out=ob, workspace=work)
+    first = oa.clone(), ob.clone()
+    q = a.q.double().numpy()
+    for i, p in enumerate((900, 500)):
+        k, v = a.kv[1]
+        check(oa[i:i + 1], attention(q[i:i + 1], k, v, p, 64 ** -0.5), 64, ("twice", i))
+    check(ob, b.want(), 64)
+    graphs = []
+    for c, r, q, o in ((ca, ra, qa, oa), (cb, rb, qb, ob)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.attn(r, q, out=o, workspace=work)
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1, 0):
+        for o in (oa, ob):
+            o.zero_()
+        graphs[i].replay()
+        graphs[1 - i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(oa, first[0]) and torch.equal(ob, first[1])

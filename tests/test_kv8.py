@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 from kv8_cases import quantise
 from paper_2505_18164_amd import mdi
@@ -93,3 +94,46 @@ def test_partitions_with_8_bit_caches():
     assert status(mdi.MDI_KV8 | 2, 2, 2) == mdi.MDI_ERR_ARG                   # no blocks, no cache
     assert status(mdi.MDI_KV8, over=dict(max_ctx=(1 << 24) + 1), kv_page_tokens=64) == mdi.MDI_ERR_ARG
     assert mdi.lib().mdi_prefill_batch(None, 1, None, None, None, None) == mdi.MDI_ERR_ARG
+
+
+def test_limits_of_a_launch():
+    big = dict(table_stride=1 << 16, n_kv_head=32, head_dim=128)
+    assert bytes_of(cache(**big), rows(n=2, n_rows=(1 << 19) - 1, max_ctx=64), 32)[0] == mdi.MDI_OK
+    assert bytes_of(cache(**big), rows(n=2, n_rows=1 << 19, max_ctx=64), 32)[0] == mdi.MDI_ERR_ARG             # 2^24 rows and heads
+    assert bytes_of(cache(**big), rows(start=None, n=256, n_rows=256, max_ctx=1 << 20), 512)[0] == mdi.MDI_ERR_ARG      # 2^17 units of 2^13 tiles
+    c, r = cache(**big), rows(n=2, n_rows=1 << 21, max_ctx=64)
+    for call in (mdi.lib().mdi_kv8_write, mdi.lib().mdi_kv8_read):
+        assert call(C.byref(c), C.byref(r), 16, 16, 1, 4096, 128, None) == mdi.MDI_ERR_ARG                      # 2^33 elements
+    c, r = cache(), rows()
+    assert mdi.lib().mdi_kv8_attn(C.byref(c), C.byref(r), 16, 256, 4, 3e38, 16, 256, None, 0, None) == mdi.MDI_ERR_ARG   # scale * log2 e
+
+
+def test_what_the_python_calls_refuse():
+    z = lambda *shape, dtype=torch.int32, device="cpu": torch.zeros(shape, dtype=dtype, device=device)
+    codes, scales, tables = z(3, 2, 2, 16, 64, dtype=torch.int8), z(3, 2, 2, 16, dtype=torch.float32), z(2, 4)
+    cache = mdi.Kv8Cache(codes, scales, tables)
+    for a in ((codes[:, :, :1], scales, tables), (codes, scales[:2], tables), (codes, scales, tables[0]), (codes.float(), scales, tables),
+              (codes, scales.double(), tables), (codes, scales, tables.long()), (codes.transpose(0, 1), scales.transpose(0, 1), tables), (codes, scales, tables.T)):
+        with pytest.raises(ValueError):
+            mdi.Kv8Cache(*a)
+    pos, start = z(2), z(3)
+    for a in (dict(pos=pos.long()), dict(pos=pos, start=start), dict(pos=pos, start=z(2), n_rows=4), dict(pos=pos, table=z(3)), dict(pos=pos, n_rows=-1),
+              dict(pos=pos, max_ctx=(1 << 32) + 5), dict(pos=z(4)[::2])):
+        with pytest.raises(ValueError):
+            cache.rows(**a)
+    rows = cache.rows(pos, start, n_rows=4)
+    x, q = z(4, 2, 64, dtype=torch.bfloat16), z(4, 6, 64, dtype=torch.bfloat16)
+    elsewhere = mdi.Kv8Cache(*(t.to("meta") for t in (codes, scales, tables)))
+    for call in (cache.write, cache.read):
+        for k, v in ((x[:3], x[:3]), (x, x.float()), (x.half(), x.half()), (x, x.transpose(0, 1).contiguous().transpose(0, 1)), (x.to("meta"), x.to("meta")),
+                     (x[:, :, ::2], x[:, :, ::2])):
+            with pytest.raises(ValueError):
+                call(rows, k, v)
+    with pytest.raises(ValueError):
+        elsewhere.write(rows, x.to("meta"), x.to("meta"))                     # rows of another GPU
+    for kw in (dict(q=q[:3]), dict(q=q.float()), dict(q=q[:, ::2]), dict(q=q.to("meta")), dict(q=q, out=q[:, :4]), dict(q=q, out=q.float()),
+               dict(q=q, workspace=z(64).to("meta")), dict(q=q, workspace=z(64)[::2])):
+        with pytest.raises(ValueError):
+            cache.attn(rows, **kw)
+    with pytest.raises(ValueError):
+        elsewhere.attn(rows, q.to("meta"))
