@@ -77,7 +77,43 @@ __global__ __launch_bounds__(kBlock) void k_kv8_attn(Kv8Cache c, Kv8Rows r, Kv8A
   }
 }
 
-// A workgroup per row and head adds the pieces, always in the same order: 256 / (h / 4) of them at a time, a float4 a thread.
+// Pieces of equal length, 64 at most: a wavefront per row and head adds them, 64 / (h / 4) at a time, a float4 a lane.  (As
+// k_kv8_join, a workgroup each: 256 rows of 32 heads of 128, four pieces: 19.0 us instead of 8.2.)
+__global__ __launch_bounds__(kBlock) void k_kv8_join_few(Kv8Cache c, Kv8Rows r, Kv8Attn a) {
+  const int lane = threadIdx.x & 63, h = c.h, item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)), row = item / a.H;
+  if (row >= r.n_rows) return;
+  const Kv8View v = kv8_view(c, r, row);
+  if (v.sample < 0 || v.seen <= a.plan.chunk) return;            // finished where it was computed
+  if (kv8_table_row(c, r, v.sample) < 0) return;                 // its zeros are written
+  const int n = (v.seen + a.plan.chunk - 1) / a.plan.chunk;
+  const float2 mark = lane < n ? *kv8_part_marks(a, c, r, item, lane) : make_float2(kKv8None, 0.f);
+  float to = mark.x;
+  for (int off = 32; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, 64));
+  const float f = exp2f(mark.x - to), l = wave_sum(mark.y * f);
+  const int per = h / 4, at_once = 64 / per, slot = lane / per, ch = 4 * (lane - slot * per);
+  const float* sums = kv8_part_sums(a, c, item, 0) + ch;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < n; p0 += at_once) {
+    const int p = p0 + slot;
+    const float w = __shfl(f, min(p, 63), 64);
+    if (slot >= at_once || p >= n) continue;
+    const float4 x = *reinterpret_cast<const float4*>(sums + (long)p * h);
+    acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
+  }
+  float4 all = acc;
+  for (int i = 1; i < at_once; ++i) {
+    const int from = min(i * per + lane, 63);
+    all.x += __shfl(acc.x, from, 64); all.y += __shfl(acc.y, from, 64); all.z += __shfl(acc.z, from, 64); all.w += __shfl(acc.w, from, 64);
+  }
+  if (slot) return;
+  bf16_t* out = a.out + (long)row * a.out_stride + (long)(item - row * a.H) * h + ch;
+  const float inv = 1.f / l;
+  *reinterpret_cast<uint2*>(out) = make_uint2((uint32_t)f32_to_bf16(all.x * inv) | ((uint32_t)f32_to_bf16(all.y * inv) << 16),
+                                              (uint32_t)f32_to_bf16(all.z * inv) | ((uint32_t)f32_to_bf16(all.w * inv) << 16));
+}
+
+// Shares of the stream of tiles, any number of them: a workgroup per row and head, always in the same order: 256 / (h / 4) pieces at a
+// time, a float4 a thread.
 // References and sums of weights are looked at 256 pieces at a time.  (One wavefront that took piece after piece: 237 us for 313
 // pieces of 32 heads, 16 us for 16 pieces of 512.)
 __global__ __launch_bounds__(kBlock) void k_kv8_join(Kv8Cache c, Kv8Rows r, Kv8Attn a) {
@@ -88,15 +124,10 @@ __global__ __launch_bounds__(kBlock) void k_kv8_join(Kv8Cache c, Kv8Rows r, Kv8A
   const Kv8View v = kv8_view(c, r, row);
   if (v.sample < 0 || v.seen == 0) return;
   if (kv8_table_row(c, r, v.sample) < 0) return;                 // its zeros are written
-  int n;                                                         // the row's pieces
-  if (a.plan.wgs) {
-    const int groups = kv8_groups(c, a.H), head = item - row * a.H, G = a.H / c.K;
-    const Kv8Stream all = kv8_stream(c, r, a.plan, c.K * groups, row, kv8_seen(c, r, lane));
-    const int tiles = kv8_tiles(v.seen), from = all.before * c.K * groups + (head / G * groups + head % G / 16) * (tiles + kKv8Begin) + kKv8Begin;
-    n = (from + tiles - 1) / all.per - from / all.per + 1;
-  } else {
-    n = (v.seen + a.plan.chunk - 1) / a.plan.chunk;
-  }
+  const int groups = kv8_groups(c, a.H), head = item - row * a.H, G = a.H / c.K;
+  const Kv8Stream all = kv8_stream(c, r, a.plan, c.K * groups, row, kv8_seen(c, r, lane));
+  const int tiles = kv8_tiles(v.seen), from = all.before * c.K * groups + (head / G * groups + head % G / 16) * (tiles + kKv8Begin) + kKv8Begin;
+  const int n = (from + tiles - 1) / all.per - from / all.per + 1;   // the row's pieces
   if (n == 1) return;                                            // finished where it was computed
   const int per = h / 4, at_once = kBlock / per, slot = tid / per, ch = 4 * (tid - slot * per);
   const float* sums = kv8_part_sums(a, c, item, 0) + ch;
@@ -167,8 +198,9 @@ void launch_kv8_attn(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const K
     while (8 * L < c.h) L *= 2;
     hipLaunchKernelGGL(k_kv8_attn, dim3((unsigned)(r.n_rows * a.H), a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
   }
-  if (a.plan.splits > 1)
-    hipLaunchKernelGGL(k_kv8_join, dim3((unsigned)(r.n_rows * a.H)), dim3(kBlock), 0, s, c, r, a);
+  const unsigned items = (unsigned)(r.n_rows * a.H);
+  if (a.plan.wgs) hipLaunchKernelGGL(k_kv8_join, dim3(items), dim3(kBlock), 0, s, c, r, a);
+  else if (a.plan.splits > 1) hipLaunchKernelGGL(k_kv8_join_few, dim3((items + kBlock / 64 - 1) / (kBlock / 64)), dim3(kBlock), 0, s, c, r, a);
 }
 
 }  // namespace mdi

@@ -458,11 +458,12 @@ PromptGeo geo_of(const Kv8Cache& c, const Kv8Rows& r, int H, int WQ) {
   return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh};
 }
 // Groups of a workgroup and pieces of a row's positions.  A step of 64 NG keys takes `step` us, a workgroup six or seven more to begin
-// and end; what is divided is added by a second launch, whose workgroups - one per row and head - are most of what a division of
-// many rows costs.  How long the single samples are is on the device: they are taken for equal.  Measured, us, undivided with 1 / 2
-// groups: a prompt of 512, 1024, 2048 of the 7B shape 27.8/21.4, 45.3/33.0, 81.3/69.9, four of 512 31.6/39.8, sixteen of 64 20.0/23.0,
-// eight of 333 of TinyLlama 26.2/30.5, one of 1500 44.3/30.0; four pieces of 64 behind 8000 of the 8B shape 264/165, in 4 parts
-// 97/74, in 8 70/84; the prompt of 1024 in two parts 76/80.
+// and end; what is divided is added by a second launch, a wavefront per row and head.  How long the single samples are is on the
+// device: they are taken for equal.  Whole calls, us, undivided with 1 / 2 groups: a prompt of 512, 1024, 2048 of the 7B shape
+// 28.3/21.8, 45.5/33.8, 81.8/69.9, four of 512 32.5/40.8, sixteen of 64 20.8/24.1, eight of 333 of TinyLlama 27.1/32.4, one of 1500
+// 43.9/31.3; four pieces of 64 behind 8000 of the 8B shape 263/161, in 2 parts 144/94, in 4 84/61, in 8 60/74, in 16 77/102; four
+// of 128 behind 2000 79/53, 60/50, 47/62; the prompt of 1024 in two parts 43/49.  Of 25 such shapes the rule takes the best of
+// these ways for all but four short ones, which it misses by up to 11 % (one us).
 struct PromptPlan { int groups, splits; };
 PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_limit) {
   const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
@@ -476,7 +477,7 @@ PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_l
       if (s > 1 && (r.max_ctx < 256 * s || kv8_part_bytes(Kv8Plan{0, s, 0, 0}, c, r, H) > part_limit)) break;
       const double longest = std::ceil(r.max_ctx / (64. * ng * s)), all = items * seen / (64. * ng * 256);
       double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
-      if (s > 1) us += 6 + heads / 800 + heads * s * c.h / 5e5;
+      if (s > 1) us += 2 + heads / 2000 + heads * s * c.h / 4e6;
       if (us < best_us) { best_us = us; best = PromptPlan{ng, s}; }
     }
   }
