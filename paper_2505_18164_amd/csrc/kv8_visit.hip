@@ -5,6 +5,23 @@
 namespace mdi {
 namespace {
 
+// One row by a workgroup: 16 bytes a thread where both lie so, else two (a caller's rows may lie anywhere), eight of them on their way.
+__device__ __forceinline__ void copy_row(void* to, const void* from, int bytes) {
+  if ((((uintptr_t)to | (uintptr_t)from | (unsigned)bytes) & 15) == 0) {
+    for (int e = threadIdx.x; e < bytes / 16; e += kBlock) ((uint4*)to)[e] = ((const uint4*)from)[e];
+    return;
+  }
+  const int n = bytes / 2;
+  for (int e0 = threadIdx.x; e0 < n; e0 += 8 * kBlock) {
+    uint16_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ((const uint16_t*)from)[min(e0 + i * kBlock, n - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (e0 + i * kBlock < n) ((uint16_t*)to)[e0 + i * kBlock] = x[i];
+  }
+}
+
 // Workgroup 0 writes who has which rows; workgroup i + 1 brings row i's angles and input.
 __global__ __launch_bounds__(kBlock) void k_kv8_setup(Kv8Setup a) {
   if (blockIdx.x == 0) {
@@ -18,19 +35,17 @@ __global__ __launch_bounds__(kBlock) void k_kv8_setup(Kv8Setup a) {
     return;
   }
   const int row = blockIdx.x - 1;
-  int s = 0;
-  while (s + 1 < a.n && a.first[s + 1] <= row) ++s;
+  // the row's sample: at most 64 ends, looked at together
+  const int lane = threadIdx.x & 63, s = __popcll(__ballot(lane + 1 < a.n && a.first[min(lane + 1, a.n)] <= row));
   const int pos = a.pos[s] + row - a.first[s];
   if (threadIdx.x == 0) a.row_pos[row] = pos;
   if (a.rope_rows)
     for (int e = threadIdx.x; e < a.half; e += kBlock) a.rope_rows[(long)row * a.half + e] = a.rope[(long)pos * a.half + e];
-  if (a.in_rows)                                                 // (one row each; pieces of two bytes: an input may lie anywhere)
-    for (int e = threadIdx.x; e < a.in_bytes / 2; e += kBlock) ((uint16_t*)a.in_rows)[(long)row * (a.in_bytes / 2) + e] = ((const uint16_t*)a.in[s])[e];
+  if (a.in_rows) copy_row((char*)a.in_rows + (long)row * a.in_bytes, a.in[s], a.in_bytes);   // (one row each)
 }
 
 __global__ __launch_bounds__(kBlock) void k_kv8_handoff(Kv8Handoff a) {
-  const int row = blockIdx.x;
-  for (int e = threadIdx.x; e < a.bytes / 2; e += kBlock) ((uint16_t*)a.out[row])[e] = ((const uint16_t*)a.rows)[(long)row * (a.bytes / 2) + e];
+  copy_row(a.out[blockIdx.x], (const char*)a.rows + (long)blockIdx.x * a.bytes, a.bytes);
 }
 
 }  // namespace

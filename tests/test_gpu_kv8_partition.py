@@ -227,3 +227,27 @@ def test_more_rows_than_two_bytes_count():
     one.sync()
     pieces.sync()
     assert rel_l2_rows(host(a), host(b)).max() < 2 * tol(cfg)         # each is that close to the exact result
+
+
+def test_inputs_and_outputs_that_lie_anywhere():
+    cfg, w, o, g = build("gqa_h64", embed=False)
+    x = dev_acts(S.make_activations(cfg, 9, 0, 4), cfg)
+    d = cfg["d_model"]
+    want = []
+    for shift in (0, 1, 4):                                       # elements: 16 bytes, 2, 8
+        for s in range(4):
+            g.seq_reset(s)
+            g.prefill(s, x[:3])
+        buf = torch.full((4 * (d + 8) + 8,), -7, dtype=torch.bfloat16, device="cuda:0")
+        ins = [buf[s * (d + 8) + shift:][:d] for s in range(4)]
+        for s in range(4):
+            ins[s].copy_(x[s])
+        res = torch.full_like(buf, -7)
+        outs = [res[s * (d + 8) + shift:][:d] for s in range(4)]
+        g.decode_batch([0, 1, 2, 3], ins, outs)
+        g.sync()
+        want.append(torch.stack(outs).clone())
+        for t in outs:
+            t.fill_(-7)
+        assert (res == -7).all()                                  # nothing beside them was written
+    assert torch.equal(want[0], want[1]) and torch.equal(want[0], want[2])
