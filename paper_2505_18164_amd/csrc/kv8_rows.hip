@@ -52,8 +52,11 @@ __device__ __forceinline__ bool place(const Kv8Cache& c, const Kv8Rows& r, int r
 }
 
 // A wavefront takes 64 / L head rows (keys of all heads, then values of all heads) of one row of the call at a time, kUnits
-// times; L lanes hold eight channels each of one.  What bounds it: memory.  (The code is x c + 1.5 2^23: one addition whose
-// rounding is the one to a whole number, and whose low byte is the code.)
+// times; L lanes hold eight channels each of one.  What bounds it: memory - 8192 rows of the 7B shape, bf16, are quantised in 60 us
+// (134 MB in, 69 out; 40 when they are in the last cache) and read back as fp32 in 72 (69 in, 268 out: 4.7 TB/s) -, and for few rows
+// the way to the page: sample, table, page, each behind the one before, 4.5 us.  (Workgroups of sixteen rows that follow one another,
+// whose scales and codes then lie together in a page, are no faster: 41.7 us instead of 39.7, 15.5 instead of 12.6 for the 8B shape.)
+// (The code is x c + 1.5 2^23: one addition whose rounding is the one to a whole number, and whose low byte is the code.)
 template <typename T, bool kWrite>
 __global__ __launch_bounds__(kBlock) void k_kv8_rows(Kv8Cache c, Kv8Rows r, Kv8RowsIO io, int L, int l_sh, int pieces) {
   const int lane = threadIdx.x & 63;
