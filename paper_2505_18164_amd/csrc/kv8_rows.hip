@@ -16,11 +16,19 @@ __device__ __forceinline__ unsigned group_max(unsigned v, int L) {   // over ali
   return v;
 }
 
+// What is written into the cache is read once: without a place in the caches for it, 8192 rows of the 7B shape take 46 us instead of
+// 60 (and reading them back 71 instead of 73; there, written values without a place take 92).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]);
-template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&x)[8]) { Storage<bf16_t>::load(p, x); }
+template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&x)[8]) {
+  const u32x4 w = __builtin_nontemporal_load((const u32x4*)p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
 template <> __device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  const u32x4 a = __builtin_nontemporal_load((const u32x4*)p), b = __builtin_nontemporal_load((const u32x4*)p + 1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = __uint_as_float(a[i]); x[4 + i] = __uint_as_float(b[i]); }
 }
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]);
 template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* p, const float (&x)[8]) {
@@ -52,10 +60,10 @@ __device__ __forceinline__ bool place(const Kv8Cache& c, const Kv8Rows& r, int r
 }
 
 // A wavefront takes 64 / L head rows (keys of all heads, then values of all heads) of one row of the call at a time, kUnits
-// times; L lanes hold eight channels each of one.  What bounds it: memory - 8192 rows of the 7B shape, bf16, are quantised in 60 us
-// (134 MB in, 69 out; 40 when they are in the last cache) and read back as fp32 in 72 (69 in, 268 out: 4.7 TB/s) -, and for few rows
+// times; L lanes hold eight channels each of one.  What bounds it: memory - 8192 rows of the 7B shape, bf16, are quantised in 46 us
+// (134 MB in, 69 out: 4.4 TB/s) and read back as fp32 in 71 (69 in, 268 out: 4.8 TB/s) -, and for few rows
 // the way to the page: sample, table, page, each behind the one before, 4.5 us.  (Workgroups of sixteen rows that follow one another,
-// whose scales and codes then lie together in a page, are no faster: 41.7 us instead of 39.7, 15.5 instead of 12.6 for the 8B shape.)
+// whose scales and codes then lie together in a page, are slower to write: 70 us when that was 61.)
 // (The code is x c + 1.5 2^23: one addition whose rounding is the one to a whole number, and whose low byte is the code.)
 template <typename T, bool kWrite>
 __global__ __launch_bounds__(kBlock) void k_kv8_rows(Kv8Cache c, Kv8Rows r, Kv8RowsIO io, int L, int l_sh, int pieces) {
