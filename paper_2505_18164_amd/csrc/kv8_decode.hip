@@ -16,7 +16,7 @@
 // a unit - page numbers, query - included (8 samples of the 7B shape 42 us, 16 of the 8B shape 55).
 // Shares instead of pieces of one length: 8 samples of 1 .. 4096 positions 41 -> 29.8 us at that step (a piece is as long as the longest
 // sample's, and few of them are); what a unit costs to begin has to count, or 32 short ones after the other are one workgroup's (69 us).
-// 16 samples of 8100 positions of the 8B shape: 51.7 us = 5.3 TB/s of codes and scales, 8 of the 7B shape 29.0 us = 4.7 TB/s.
+// 16 samples of 8100 positions of the 8B shape: 47.9 us = 5.7 TB/s of codes and scales, 8 of the 7B shape 28.2 us = 4.7 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,8 +34,13 @@ template <int HD> struct Tile {      // 32 positions of a wavefront
   f32x4 ks[2], vs[2];
 };
 
+// A cache that no later call finds in the last cache is read without a place in it.
+template <bool kOnce, typename T> __device__ __forceinline__ T load_codes(const void* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load((const T*)p); else return *(const T*)p;
+}
+
 // kWhole16: pages of a multiple of 16 positions, so 16 aligned positions lie in one page, next to each other.
-template <int HD, bool kWhole16>
+template <int HD, bool kWhole16, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Rows r, Kv8Attn a, int groups) {
   constexpr int KI = HD / 64, VB = HD / 16;                      // 16-byte units of a key a lane has; bytes of a value (= channel blocks)
   constexpr int OS = HD + 4;
@@ -116,25 +121,25 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
           const char* sk = (const char*)(c.scales + row);
           const char* sv = sk + 4l * c.pt;
 #pragma unroll
-          for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + (k_off + 64u * i));
+          for (int i = 0; i < KI; ++i) t.k[u][i] = load_codes<kOnce, u32x4>(kp + (k_off + 64u * i));
           t.ks[u] = *reinterpret_cast<const f32x4*>(sk + s_off);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const char* w = vp + (v_off + (unsigned)(j * HD));
-            if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
-            else t.v[u][j][0] = *reinterpret_cast<const uint32_t*>(w);
+            if constexpr (KI == 2) { const u32x2 x = load_codes<kOnce, u32x2>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
+            else t.v[u][j][0] = load_codes<kOnce, uint32_t>(w);
           }
           t.vs[u] = *reinterpret_cast<const f32x4*>(sv + s_off);
         } else {
           const int8_t* kp = c.codes + row_of(min(base + 16 * u + col, hi - 1)) * HD;
 #pragma unroll
-          for (int i = 0; i < KI; ++i) t.k[u][i] = *reinterpret_cast<const u32x4*>(kp + 64 * i + 16 * g);
+          for (int i = 0; i < KI; ++i) t.k[u][i] = load_codes<kOnce, u32x4>(kp + 64 * i + 16 * g);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const long row = row_of(min(base + 16 * u + 4 * g + j, hi - 1));
             const uint32_t* w = reinterpret_cast<const uint32_t*>(c.codes + (row + c.pt) * HD + VB * col);
-            if constexpr (KI == 2) { const u32x2 x = *reinterpret_cast<const u32x2*>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
-            else t.v[u][j][0] = *w;
+            if constexpr (KI == 2) { const u32x2 x = load_codes<kOnce, u32x2>(w); t.v[u][j][0] = x.x; t.v[u][j][1] = x.y; }
+            else t.v[u][j][0] = load_codes<kOnce, uint32_t>(w);
             t.ks[u][j] = c.scales[row];
             t.vs[u][j] = c.scales[row + c.pt];
           }
@@ -287,12 +292,20 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
   }
 }
 
-template <int HD>
+// Read once: more than half of what the last cache holds (256 MB), counting every sample as long as the longest may be.  16 samples of
+// 8192 positions of the 8B shape 51.7 -> 47.9 us, one of 120001 51.0 -> 47.3, 8 of up to 4096 of the 7B shape 28.9 -> 28.2; but the same 4 samples of 8000 again and
+// again, 68 MB, 22.2 -> 23.7, and 8 of 1000 of the 7B shape, 68 MB, 22.6 -> 23.3.
+template <int HD, bool kOnce>
 void launch_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
   const int groups = kv8_groups(c, a.H);
   const dim3 grid((unsigned)(a.plan.wgs ? a.plan.wgs : r.n * c.K * groups)), block(64 * kWaves);
-  if (c.pt % 16 == 0) hipLaunchKernelGGL((k_kv8_decode<HD, true>), grid, block, 0, s, c, r, a, groups);
-  else hipLaunchKernelGGL((k_kv8_decode<HD, false>), grid, block, 0, s, c, r, a, groups);
+  if (c.pt % 16 == 0) hipLaunchKernelGGL((k_kv8_decode<HD, true, kOnce>), grid, block, 0, s, c, r, a, groups);
+  else hipLaunchKernelGGL((k_kv8_decode<HD, false, kOnce>), grid, block, 0, s, c, r, a, groups);
+}
+template <int HD>
+void launch_heads(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
+  const bool once = (double)r.n * r.max_ctx * c.K * 2 * (HD + 4) > 128e6;
+  if (once) launch_decode<HD, true>(s, c, r, a); else launch_decode<HD, false>(s, c, r, a);
 }
 
 }  // namespace
@@ -315,7 +328,7 @@ Kv8Plan kv8_decode_plan(const Kv8Cache& c, const Kv8Rows& r, int H) {
 }
 
 void launch_kv8_decode(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  if (c.h == 128) launch_decode<128>(s, c, r, a); else launch_decode<64>(s, c, r, a);
+  if (c.h == 128) launch_heads<128>(s, c, r, a); else launch_heads<64>(s, c, r, a);
 }
 
 }  // namespace mdi

@@ -441,3 +441,15 @@ def test_two_graphs_share_a_workspace_and_one_sample_is_asked_twice():
         graphs[1 - i].replay()
         torch.cuda.synchronize()
         assert torch.equal(oa, first[0]) and torch.equal(ob, first[1])
+
+
+@pytest.mark.parametrize("pt", [16, 24])
+@pytest.mark.parametrize("h", [64, 128])
+def test_tokens_of_a_call_that_may_read_more_than_the_caches_hold(h, pt):
+    """By its bound of the positions, that is: the tables have room for 200000 of each sample."""
+    s = Setup(4, 2, h, pt, [1, 1, 1], [700, 0, 3000], seed=11, spare=200000 // pt)
+    cache = s.cache()
+    rows = cache.rows(to_dev(s.pos))
+    assert 3 * s.tables.shape[1] * pt * 2 * 2 * (h + 4) > 128e6
+    check(cache.attn(rows, s.q.to(DEV)), s.want(), h)
+    cache.check()
