@@ -41,8 +41,10 @@ constexpr int BK = 64;               // keys of a step
 // block is 2^kTop, and counted anew when one would exceed 2^kRaise; one below 2^-14 keeps the digits down to 2^-24, 2^-30 of the
 // largest.  Values are multiplied by a power of two, so far that a row's largest magnitude is at most 2^13 where that is
 // chosen, and up to 2^15 before it is chosen anew: a row of 2^-27 of the largest one's size still has the digits of a bf16.
-constexpr float kTop = 6.f, kRaise = 14.f;
+constexpr float kTop = 6.f, kFromTop = 0x1p-6f, kRaise = 14.f;
 constexpr float kUnitFirst = 0x1p100f;                           // scales are zero, or 2^-107 and more
+
+__device__ __forceinline__ float reciprocal(float power_of_two) { return __uint_as_float(0x7F000000u - __float_as_uint(power_of_two)); }
 
 __device__ __forceinline__ u32x2 read_transposed(const bf16_t* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p));
@@ -351,9 +353,10 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
       return;
     }
     const int k0 = lo + (NG * j + grp) * BK;
+    if (first) mine = unit;                                      // (the sums are zeros)
     if (k0 + BK - 1 > wave_pos || k0 + BK > hi) weigh(j, std::true_type()); else weigh(j, std::false_type());
     if (__builtin_expect(unit != mine, 0)) {                     // the block's values are counted in another unit than the sums
-      alpha = (raised ? alpha : 1.f) * (unit / mine);
+      alpha = (raised ? alpha : 1.f) * (unit * reciprocal(mine));
       raised = true;
       mine = unit;
     }
@@ -393,8 +396,8 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   __syncthreads();
   // the largest weights count as one again, and the sums in the values' own unit
   m = first ? kKv8None : m + kTop;                               // (first: saw nothing)
-  l *= exp2f(-kTop);
-  const float own = exp2f(-kTop) / mine;
+  l *= kFromTop;
+  const float own = kFromTop * reciprocal(mine);
 
 #pragma unroll
   for (int i = 0; i < HT; ++i)

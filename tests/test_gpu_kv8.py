@@ -453,3 +453,21 @@ def test_tokens_of_a_call_that_may_read_more_than_the_caches_hold(h, pt):
     assert 3 * s.tables.shape[1] * pt * 2 * 2 * (h + 4) > 128e6
     check(cache.attn(rows, s.q.to(DEV)), s.want(), h)
     cache.check()
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, the same cache: every result is the one of the call alone."""
+    a = Setup(8, 2, 128, 64, [200, 33], [1500, 0], seed=13)
+    cache = a.cache()
+    rows, tokens = a.plan(cache), cache.rows(to_dev(np.array([1600, 20], np.int32)))
+    q = a.q.to(DEV)
+    alone = cache.attn(rows, q), cache.attn(tokens, q[:2])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(cache.attn(rows, q) if i == 0 else cache.attn(tokens, q[:2]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, alone[i]) for i in range(2) for x in got[i])
