@@ -26,6 +26,7 @@ namespace mdi {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr float kRaise = 8.f;        // how far (in powers of two) a score may exceed its query's reference before that is raised
 constexpr int kPages = 1024;         // page numbers of a piece: chunk / pt + 2 at most
 
 template <int HD> struct Tile {      // 32 positions of a wavefront
@@ -189,8 +190,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, s[u][j] * t.ks[u][j]);
       // Weights are relative to m, which is raised - for all four lanes of a query alike - only when a score exceeds it by
-      // 2^kKv8Raise: the sum is divided out at the end, so any reference near the largest score does.
-      if (__any(top > m + kKv8Raise)) {
+      // 2^kRaise: the sum is divided out at the end, so any reference near the largest score does.
+      if (__any(top > m + kRaise)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float to = fmaxf(m, top), alpha = exp2_raw(m - to);

@@ -5,7 +5,6 @@
 
 namespace mdi {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -18,7 +17,5 @@ __device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
 template <int N> __device__ __forceinline__ float code_of(uint32_t w) { return (float)(int8_t)(w >> (8 * N)); }   // byte N
 
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-constexpr float kKv8Raise = 8.f;     // how far (in powers of two) a score may exceed its query's reference before that is raised
 
 }  // namespace mdi
