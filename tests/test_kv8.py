@@ -137,3 +137,15 @@ def test_what_the_python_calls_refuse():
             cache.attn(rows, **kw)
     with pytest.raises(ValueError):
         elsewhere.attn(rows, q.to("meta"))
+
+
+def test_rows_of_a_pass_of_a_partition():
+    from paper_2505_18164_amd import synth as S
+    n = C.c_size_t(0)
+
+    def status(**kw):
+        c = mdi.make_config(S.tiny(dtype=S.DT_BF16, n_head=4, n_kv_head=2, head_dim=64, d_model=256, max_ctx=1 << 22), max_seqs=1, kv_page_tokens=64, **kw)
+        return mdi.lib().mdi_partition_bytes(C.byref(c), 0, 1, mdi.MDI_KV8, C.byref(n))
+
+    assert status() == mdi.MDI_ERR_ARG                                        # a first visit of 2^22 rows: 2^24 rows and heads
+    assert status(max_prefill=(1 << 22) - 1) == status(max_prefill=1024) == mdi.MDI_OK
