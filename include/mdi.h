@@ -533,8 +533,11 @@ MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, 
  * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
  * binary32.  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
  * 2^24, n * n_head * (max_ctx / 128 + 3) below 2^30.  Products take a weight with 16
- * digits for single tokens and as a binary16 of at least 2^-24, the largest being 2^6
- * or more, for packed rows of 64 or 128 channels.
+ * digits for single tokens.  For packed rows of 64 or 128 channels weights and values
+ * are binary16: a weight is at least 2^-24 or nothing, the largest being 2^6 or more; a
+ * value keeps eleven digits, whatever a later position holds.  (Among values
+ * whose sizes are further than 2^20 apart rows are computed in binary32 instead, which
+ * takes tens of times as long.)
  * workspace: mdi_kv8_attn_bytes() bytes of device memory, 16-byte aligned (0 bytes:
  * may be NULL); it carries nothing from one call to the next, and calls that can
  * run at the same time need one each.  Results do not depend on timing.

@@ -6,13 +6,7 @@
 namespace mdi {
 namespace {
 
-__device__ __forceinline__ float sum_of(float v, int L) {
-  for (int off = 1; off < L; off <<= 1) v += __shfl_xor(v, off, 64);
-  return v;
-}
-
-// One workgroup per row, head and piece of the positions.  L lanes hold eight channels each of a position; a lane group keeps
-// its own running (reference, sum, output), which are folded at the end.  It serves heads of other than 64 or 128 channels, reads the
+// One workgroup per row, head and piece of the positions, its wavefronts' sums folded at the end.  It serves heads of other than 64 or 128 channels, reads the
 // cache once for every query head, and is bound by vector instructions: 16 tokens of 8100 positions of the 8B shape would take it
 // 374 us (kv8_decode.hip: 52), a prompt of 1024 of the 7B shape 710 (kv8_prompt.hip: 33).
 __global__ __launch_bounds__(kBlock) void k_kv8_attn(Kv8Cache c, Kv8Rows r, Kv8Attn a, int L) {
@@ -32,39 +26,15 @@ __global__ __launch_bounds__(kBlock) void k_kv8_attn(Kv8Cache c, Kv8Rows r, Kv8A
   if (lo >= hi) return;
   const int ch = 8 * (lane & (L - 1)), sub = lane / L, tpw = 64 / L;
   const bool live = ch < h;
-  float q[8], o[8];
+  float q[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) { q[j] = live ? bf16_to_f32(a.q[(long)row * a.q_stride + (long)head * h + ch + j]) * a.scale : 0.f; o[j] = 0.f; }
-  float m = kKv8None, l = 0.f;
-  for (int t0 = lo + wave * tpw; t0 < hi; t0 += 4 * tpw) {
-    const int pos = min(t0 + sub, hi - 1), at = kv8_page_of(c, pos);
-    const long rk = kv8_row(c, kv8_checked_page(c, table[at]), kv, pos), rv = rk + c.pt;
-    const uint2 kc = live ? *reinterpret_cast<const uint2*>(c.codes + rk * h + ch) : make_uint2(0, 0);
-    const uint2 vc = live ? *reinterpret_cast<const uint2*>(c.codes + rv * h + ch) : make_uint2(0, 0);
-    const float ks = c.scales[rk], vs = c.scales[rv];
-    float s = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(q[j], (float)(int8_t)((j < 4 ? kc.x : kc.y) >> (8 * (j & 3))), s);
-    s = sum_of(s, L) * ks;
-    if (t0 + sub >= hi) continue;
-    const float to = fmaxf(m, s), alpha = exp2f(m - to), p = exp2f(s - to), w = p * vs;
-    m = to;
-    l = l * alpha + p;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = o[j] * alpha + w * (float)(int8_t)((j < 4 ? vc.x : vc.y) >> (8 * (j & 3)));
-  }
-  for (int off = L; off < 64; off <<= 1) {
-    const float m1 = __shfl_xor(m, off, 64), l1 = __shfl_xor(l, off, 64), to = fmaxf(m, m1), a0 = exp2f(m - to), a1 = exp2f(m1 - to);
-    l = l * a0 + l1 * a1;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = o[j] * a0 + __shfl_xor(o[j], off, 64) * a1;
-    m = to;
-  }
+  for (int j = 0; j < 8; ++j) q[j] = live ? bf16_to_f32(a.q[(long)row * a.q_stride + (long)head * h + ch + j]) * a.scale : 0.f;
+  const Kv8Sums mine = kv8_attend(c, table, kv, q, L, ch, live, lo + wave * tpw, 4 * tpw, hi);
   if (sub == 0) {
     if (live)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sm[wave][ch + j] = o[j];
-    if (lane == 0) { sm[wave][h] = m; sm[wave][h + 1] = l; }
+      for (int j = 0; j < 8; ++j) sm[wave][ch + j] = mine.o[j];
+    if (lane == 0) { sm[wave][h] = mine.m; sm[wave][h + 1] = mine.l; }
   }
   __syncthreads();
   float to = kKv8None;

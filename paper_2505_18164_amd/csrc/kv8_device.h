@@ -117,4 +117,44 @@ __device__ __forceinline__ Kv8Found kv8_find(const Kv8Cache& c, const Kv8Rows& r
 
 constexpr float kKv8None = -3e38f;   // reference of a softmax that has seen nothing
 
+// One row and head by a wavefront, for any head: L lanes hold eight channels each of a position (`ch` on, `live` where the head has
+// them), the lane groups take positions from, from + 1 .. and `step` further, up to hi.  A lane group keeps its own running (reference,
+// sum, output), which are folded at the end: every lane then has the sums of its eight channels.  Everything is binary32, with no
+// other reference than the largest score so far: no size of scores or values is out of its reach that is not out of binary32's.
+struct Kv8Sums { float m, l, o[8]; };
+__device__ __forceinline__ float kv8_sum_of(float v, int L) {
+  for (int off = 1; off < L; off <<= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+__device__ __forceinline__ Kv8Sums kv8_attend(const Kv8Cache& c, const int32_t* table, int kv, const float (&q)[8], int L, int ch, bool live,
+                                              int from, int step, int hi) {
+  const int sub = (threadIdx.x & 63) / L, h = c.h;
+  Kv8Sums r{kKv8None, 0.f, {}};
+  for (int t0 = from; t0 < hi; t0 += step) {
+    const int pos = min(t0 + sub, hi - 1), at = kv8_page_of(c, pos);
+    const long rk = kv8_row(c, kv8_checked_page(c, table[at]), kv, pos), rv = rk + c.pt;
+    const uint2 kc = live ? *reinterpret_cast<const uint2*>(c.codes + rk * h + ch) : make_uint2(0, 0);
+    const uint2 vc = live ? *reinterpret_cast<const uint2*>(c.codes + rv * h + ch) : make_uint2(0, 0);
+    const float ks = c.scales[rk], vs = c.scales[rv];
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(q[j], (float)(int8_t)((j < 4 ? kc.x : kc.y) >> (8 * (j & 3))), s);
+    s = kv8_sum_of(s, L) * ks;
+    if (t0 + sub >= hi) continue;
+    const float to = fmaxf(r.m, s), alpha = exp2f(r.m - to), p = exp2f(s - to), w = p * vs;
+    r.m = to;
+    r.l = r.l * alpha + p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.o[j] = r.o[j] * alpha + w * (float)(int8_t)((j < 4 ? vc.x : vc.y) >> (8 * (j & 3)));
+  }
+  for (int off = L; off < 64; off <<= 1) {
+    const float m1 = __shfl_xor(r.m, off, 64), l1 = __shfl_xor(r.l, off, 64), to = fmaxf(r.m, m1), a0 = exp2f(r.m - to), a1 = exp2f(m1 - to);
+    r.l = r.l * a0 + l1 * a1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.o[j] = r.o[j] * a0 + __shfl_xor(r.o[j], off, 64) * a1;
+    r.m = to;
+  }
+  return r;
+}
+
 }  // namespace mdi

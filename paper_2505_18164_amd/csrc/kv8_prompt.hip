@@ -40,9 +40,14 @@ constexpr int BK = 64;               // keys of a step
 // their size, of which their own rounding is 0.0017) and a smaller range.  Weights are counted so that the largest of a row's first
 // block is 2^kTop, and counted anew when one would exceed 2^kRaise; one below 2^-14 keeps the digits down to 2^-24, 2^-30 of the
 // largest.  Values are multiplied by a power of two, so far that a row's largest magnitude is at most 2^13 where that is
-// chosen, and up to 2^15 before it is chosen anew: a row of 2^-27 of the largest one's size still has the digits of a bf16.
+// chosen, and up to 2^15 before it is chosen anew.  That serves rows of values whose sizes are within 2^20 of each other: the smallest
+// has a scale of 2^-14 then, so that every value is a normal fp16.  The unit is that of whatever the workgroup has met, seen by
+// all of its rows or by a few; so a workgroup that meets sizes further apart (scale below kLeastScale) computes its rows over
+// again, each by itself, in binary32 (kv8_attend): 1024 rows of the 7B shape of which one value is 2^40 times the others' size 2.4 ms
+// instead of 34 us.
 constexpr float kTop = 6.f, kFromTop = 0x1p-6f, kRaise = 14.f;
 constexpr float kUnitFirst = 0x1p100f;                           // scales are zero, or 2^-107 and more
+constexpr float kLeastScale = 0x1p-14f;
 
 __device__ __forceinline__ float reciprocal(float power_of_two) { return __uint_as_float(0x7F000000u - __float_as_uint(power_of_two)); }
 
@@ -93,6 +98,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   constexpr int NB = 2;                                          // buffers of keys, and of values
   constexpr int KV = NB * BK * (KS + VR) + 8 * BK + 8;           // 16-bit elements of a group: keys, values, scales of four blocks of keys, units of four blocks of values
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ int again[NG];                                      // a group met what these numbers do not hold
 
   const int tid = threadIdx.x & (GT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = NG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GT), late = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
@@ -148,6 +154,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   u32x4 kreg[KU], vreg[KU];
   float vs[KU], sk = 0.f, sv = 0.f;
   float unit = kUnitFirst, made = kUnitFirst, mine = kUnitFirst;  // of the block whose values are staged; newest that was chosen; of o
+  float least = INFINITY;                                        // of the scales that this lane has met, but zeros
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
   auto checked = [&](int page) __attribute__((always_inline)) {
     worst = max(worst, (unsigned)page);
@@ -245,6 +252,8 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
         for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
         if (top * made > 256.f) made = __uint_as_float((127 + 5 + 127 - (__float_as_uint(top) >> 23)) << 23);   // top is less than 2^6 of these
       }
+      if (v > 0.f) least = fminf(least, v);
+      if (__builtin_expect(__any(least * made < kLeastScale), 0)) again[grp] = 1;
       if (lane == 0) Un[j & 3] = made;
     }
   };
@@ -364,6 +373,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
 
   // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies and stages, the other takes exponentials; so the later
   // four are one turn behind.  Block j + 1's keys and block j's values, which both stage in turn j, go over blocks that both have left.
+  if (tid == 0) again[grp] = 0;                                  // (by the wavefront that looks at scales)
   pages(0);
   fetch(0);
 #pragma unroll
@@ -394,6 +404,38 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   products(n_it, std::false_type());
   if (!late) __syncthreads();
   __syncthreads();
+  if (worst >= (unsigned)c.n_pages) kv8_report(c);
+  bool over = again[0] != 0;
+  if constexpr (NG > 1) over = over || again[1] != 0;
+  if (__builtin_expect(over, 0)) {
+    constexpr int L = HD / 8;
+    const int ch = 8 * (lane & (L - 1));
+    for (int i = threadIdx.x >> 6; i < BQ; i += 8) {             // a wavefront takes a row and head
+      const int row1 = q0 + (i >> g_sh), head1 = head0 + (i & ((1 << g_sh) - 1));
+      if (row1 >= at.rows) continue;
+      const int pos1 = (int)min((long)p0 + row1, (long)r.max_ctx - 1);
+      if (pos1 < lo) continue;
+      const bf16_t* const q1 = a.q + (long)(at.first + row1) * a.q_stride + (long)head1 * HD + ch;
+      float q[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] = bf16_to_f32(q1[e]) * a.scale;
+      const Kv8Sums x = kv8_attend(c, table, kv, q, L, ch, true, lo, 64 / L, min(pos1 + 1, hi));
+      if (lane >= L) continue;
+      if (pos1 < a.plan.chunk) {
+        bf16_t* const out1 = a.out + (long)(at.first + row1) * a.out_stride + (long)head1 * HD + ch;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2)
+          *reinterpret_cast<uint32_t*>(out1 + e) = (uint32_t)f32_to_bf16(x.o[e] / x.l) | ((uint32_t)f32_to_bf16(x.o[e + 1] / x.l) << 16);
+      } else {
+        const int item = (at.first + row1) * a.H + head1;
+        float* const part = kv8_part_sums(a, c, item, blockIdx.y) + ch;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part[e] = x.o[e];
+        if (lane == 0) *kv8_part_marks(a, c, r, item, blockIdx.y) = make_float2(x.m, x.l);
+      }
+    }
+    return;
+  }
   // the largest weights count as one again, and the sums in the values' own unit
   m = first ? kKv8None : m + kTop;                               // (first: saw nothing)
   l *= kFromTop;
@@ -404,7 +446,6 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] *= own;
 
-  if (worst >= (unsigned)c.n_pages) kv8_report(c);
   if constexpr (NG > 1) {
     float* fold = (float*)smem + (grp > 0 ? grp - 1 : 0) * (HT * 16 + 2) * GT;
     if (grp > 0) {

@@ -1,0 +1,86 @@
+"""Attention over the 8-bit cache where values and scores are of very different sizes: rows keep the digits of what they see."""
+import numpy as np
+import pytest
+import torch
+
+from kv8_digits import Setup, check_digits, form_of, rekeyed
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+# a loud value just behind a row, in the row's own block of positions and in later ones; what is seen before it is of size one
+BEHIND = {
+    "2^12": lambda p: np.where(p >= 100, 2.0 ** 12, 1.0),
+    "2^19": lambda p: np.where(p >= 100, 2.0 ** 19, 1.0),
+    "2^24": lambda p: np.where(p >= 100, 2.0 ** 24, 1.0),
+    "2^30": lambda p: np.where(p >= 100, 2.0 ** 30, 1.0),
+    "2^40, one": lambda p: np.where(p == 100, 2.0 ** 40, 1.0),
+    "2^100 behind 2^-80": lambda p: np.where(p >= 100, 2.0 ** 100, 2.0 ** -80),
+    "a factor of four each block": lambda p: 4.0 ** (p // 64),
+    "2^15 each block": lambda p: 2.0 ** np.minimum(15.0 * (p // 64), 90),
+    "zeros, then 2^90, then one": lambda p: np.where(p < 70, 0.0, np.where(p == 130, 2.0 ** 90, 1.0)),
+}
+
+
+@pytest.mark.parametrize("h", [64, 128, 40])
+@pytest.mark.parametrize("gain", list(BEHIND))
+def test_a_row_does_not_depend_on_values_behind_it(gain, h):
+    for H, lens, behind, pt in ((4, [150, 1, 64], [0, 330, 90], 64), (2, [260], [40], 24), (2, [20, 9], [90, 900], 16), (10, [110], [0], 48)):
+        s = Setup(H, 2, h, pt, lens, behind, seed=3, v_gain=BEHIND[gain])
+        cache = s.cache()
+        check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, form_of(h), what=(lens, pt))
+        assert int(s.err.cpu()[0]) == 0
+    s = Setup(4, 2, h, 16, [1, 1, 1], [99, 100, 330], seed=4, v_gain=BEHIND[gain])
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), s, form_of(h, True), what="one each")
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_a_row_does_not_depend_on_values_of_no_weight(h):
+    """Every sixteenth value is 2^40 times as large, and its key's score 300 and more below the others'."""
+    gain = lambda p: np.where(p % 16 == 5, 2.0 ** 40, 1.0)
+    for lens, behind, pt in (([150, 70], [0, 200], 64), ([40], [1000], 24)):
+        s = Setup(4, 2, h, pt, lens, behind, seed=5, v_gain=gain, k_gain=0.5)
+        s.q = s.q.abs() + 1
+        for i in range(len(lens)):
+            at = [p for p in range(lens[i] + behind[i]) if p % 16 == 5]
+            for p in at:
+                s.scales[s.tables[i, p // pt], :, 0, p % pt] *= np.float32(256)
+                s.kv[i][0, p] *= 256
+            rekeyed(s, i, at, -1)
+        cache = s.cache()
+        check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, "general", what=(lens, pt))   # both sizes in every block of positions: binary32
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_pieces_of_sizes_far_apart_are_joined(h):
+    """A few rows behind many positions: pieces whose values are of one size beside pieces whose sizes are far apart."""
+    s = Setup(16, 2, h, 64, [9], [6000], seed=6, v_gain=lambda p: np.where((p > 2500) & (p % 3 == 0), 2.0 ** 35, 1.0))
+    cache = s.cache()
+    rows = s.plan(cache)
+    assert cache.workspace(rows, 16) is not None                  # divided
+    first = cache.attn(rows, s.q.to(DEV))
+    check_digits(first, s, "packed")
+    assert torch.equal(cache.attn(rows, s.q.to(DEV)), first)
+
+
+def test_a_size_further_apart_in_a_captured_call():
+    """The same graph, with values of one size and of sizes far apart, in turn."""
+    near, far = (Setup(4, 2, 128, 64, [150, 20], [0, 200], seed=7, v_gain=lambda p, e=e: np.where(p >= 100, 2.0 ** e, 1.0)) for e in (3, 50))
+    assert np.array_equal(near.tables, far.tables) and torch.equal(near.q, far.q)
+    cache = near.cache()
+    rows, q = near.plan(cache), near.q.to(DEV)
+    out = torch.empty_like(q)
+    scales = [torch.from_numpy(x.scales).to(DEV) for x in (near, far)]
+    cache.attn(rows, q, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attn(rows, q, out=out)
+    for i in (0, 1, 1, 0, 1, 0):
+        cache.scales.copy_(scales[i])
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check_digits(out, (near, far)[i], "packed", what=i)
