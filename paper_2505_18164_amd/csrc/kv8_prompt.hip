@@ -48,6 +48,10 @@ constexpr int BK = 64;               // keys of a step
 constexpr float kTop = 6.f, kFromTop = 0x1p-6f, kRaise = 14.f;
 constexpr float kUnitFirst = 0x1p100f;                           // scales are zero, or 2^-107 and more
 constexpr float kLeastScale = 0x1p-14f;
+// Scores are rounded as distances from the row's reference.  When that is raised the block's own are rounded at its distance: up to
+// kFar, by 2^-15 at most.  From further below (keys that count for nothing before those that decide) they would lose their digits,
+// 11 % of a weight at 10^7, so there too the workgroup computes its rows over again.
+constexpr float kFar = 1024.f;
 
 __device__ __forceinline__ float reciprocal(float power_of_two) { return __uint_as_float(0x7F000000u - __float_as_uint(power_of_two)); }
 
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   // block and is raised - in both lanes of a row alike - when a weight would exceed 2^kRaise: the sum is divided out at
   // the end, so any reference near the largest score does.  The sum takes the weights as they are multiplied, cut to
   // fp16 (by the conversion that is 2 us of 58 faster than the one to the nearest: eight prompts of TinyLlama).
-  float alpha = 1.f;
+  float alpha = 1.f, rise = 0.f;                                 // rise: the furthest a reference was raised (kept here: a store where it is raised costs 3 % of a long call)
   bool raised = false;
   auto weigh = [&](int j, auto mask) __attribute__((always_inline)) {
     constexpr bool kMask = decltype(mask)::value;                // some of these keys are not for some of the rows
@@ -336,6 +340,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     if (__builtin_expect(first || __any(top > kRaise), 0)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float by = first ? top - kTop : fmaxf(top - kTop, 0.f);
+      rise = fmaxf(rise, first ? 0.f : by);
       alpha = first ? 1.f : exp2_raw(-by);
       raised = !first;
       m += by;
@@ -401,6 +406,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     }
     __syncthreads();
   }
+  if (__any(rise > kFar)) again[grp] = 1;                        // (a barrier before it is read)
   products(n_it, std::false_type());
   if (!late) __syncthreads();
   __syncthreads();

@@ -84,3 +84,39 @@ def test_a_size_further_apart_in_a_captured_call():
         graph.replay()
         torch.cuda.synchronize()
         check_digits(out, (near, far)[i], "packed", what=i)
+
+
+def low_first(H, h, lens, behind, pt, low, depth, seed=8):
+    """Queries above zero; the keys of the first `low` positions are `depth` and more below the others in their scores, which are small."""
+    s = Setup(H, 2, h, pt, lens, behind, seed=seed, k_gain=0.1)
+    s.q = s.q.abs() + 1
+    for i in range(len(lens)):
+        for p in range(min(low, lens[i] + behind[i])):
+            by = np.float32(20 * depth(p) * h ** -0.5)
+            at = s.tables[i, p // pt], slice(None), 0, p % pt
+            s.scales[at] *= by
+            s.kv[i][0, p] = s.codes[at].astype(np.float64) * s.scales[at].astype(np.float64)[:, None]
+        rekeyed(s, i, range(min(low, lens[i] + behind[i])), -1)
+    return s
+
+
+@pytest.mark.parametrize("h", [64, 128, 40])
+@pytest.mark.parametrize("depth", [300.0, 1e3, 1e5, 1e6, 1e7])
+def test_scores_behind_far_lower_ones(depth, h):
+    """What decides a row stands behind keys whose scores are far below: it keeps the digits of its own scores."""
+    for lens, behind, pt, low in (([200, 90], [0, 100], 64, 64), ([30], [250], 24, 200), ([9], [3000], 64, 1500)):
+        s = low_first(4, h, lens, behind, pt, low, lambda p: depth)
+        cache = s.cache()
+        check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, form_of(h), what=(lens, low))
+    s = low_first(4, h, [1, 1], [250, 99], 16, 200, lambda p: depth)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), s, form_of(h, True), what="one each")
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_scores_that_rise_from_block_to_block(h):
+    """Steps of 40, of 600 and of 6000 a block of positions, up to small ones."""
+    for step in (40, 600, 6000):
+        s = low_first(4, h, [40, 3], [400, 420], 64, 384, lambda p: step * (6.5 - p // 64))
+        cache = s.cache()
+        check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, "packed", what=step)
