@@ -64,7 +64,7 @@ constexpr int kMaxVisits = 64;       // samples one pass over the weights can ta
 struct Kv8Setup {
   int n, rows;
   int first[kMaxVisits + 1], pos[kMaxVisits], seq[kMaxVisits];
-  int page_at[kMaxVisits], page[kMaxVisits];   // entry of `tables` to fill, or -1
+  long page_at[kMaxVisits]; int page[kMaxVisits];   // entry of `tables` to fill (there may be more than 2^31), or -1
   int32_t *start, *at, *table, *row_pos, *zero, *tables;
   const float2* rope; float2* rope_rows; int half;   // rope_rows[row] = rope[its position], `half` pairs each; nullptr: not needed
   const void* in[kMaxVisits]; void* in_rows; int in_bytes;   // in_rows[i] = the in_bytes of in[i]; nullptr: the rows are together already

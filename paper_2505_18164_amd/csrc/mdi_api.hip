@@ -802,7 +802,7 @@ mdi_status visit_kv8(mdi_partition* p, int n, const uint32_t* seqs, const uint32
     int32_t* row = p->host_tables.data() + (size_t)seq * p->pages_per_seq;
     for (int k = 0; k < need; ++k) { row[have + k] = p->free_pages.back(); p->free_pages.pop_back(); }
     a.first[i] = rows; a.pos[i] = len; a.seq[i] = (int)seq;
-    a.page_at[i] = need == 1 ? (int)(seq * p->pages_per_seq) + have : -1;
+    a.page_at[i] = need == 1 ? (long)seq * p->pages_per_seq + have : -1;
     a.page[i] = need == 1 ? row[have] : 0;
     if (need > 1 && hipMemcpyAsync(p->tables + (size_t)seq * p->pages_per_seq + have, row + have, (size_t)need * 4, hipMemcpyHostToDevice, p->stream) != hipSuccess)
       return MDI_ERR_HIP;

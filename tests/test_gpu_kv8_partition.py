@@ -251,3 +251,26 @@ def test_inputs_and_outputs_that_lie_anywhere():
             t.fill_(-7)
         assert (res == -7).all()                                  # nothing beside them was written
     assert torch.equal(want[0], want[1]) and torch.equal(want[0], want[2])
+
+
+def test_tables_of_more_entries_than_31_bits_count():
+    """2050 samples of up to 2^24 positions in pages of 16: sample 2048's entries start at 2^31."""
+    cfg = S.tiny(n_layer=1, d_model=32, n_head=2, n_kv_head=1, head_dim=16, d_ff=64, vocab=61, max_ctx=1 << 24, dtype=S.DT_BF16)
+    w = scale_matrices(S.make_weights(cfg, 31, exercise=True), 4.0)
+    g = mdi.Partition(cfg, w, 0, 1, max_seqs=2050, kv_page_tokens=16, kv_pages=64, max_prefill=64, kv8=True)
+    x = dev_acts(S.make_activations(cfg, 9, 0, 50), cfg)
+    for first in (1, 16, 40):                                     # positions of the first visit: a page, and two or three at once
+        got = {}
+        for s in (0, 2047, 2048, 2049):                           # (others' pages hold other rows)
+            g.prefill_chunk(s, x[s % 7:s % 7 + 9])
+            g.seq_reset(s)
+        for s in (0, 2047, 2048, 2049):
+            y = [g.prefill(s, x[:first])] + [g.decode_step(s, x[first + i]).unsqueeze(0) for i in range(8)]
+            got[s] = torch.cat(y)
+        z = g.decode_batch([2048, 0, 2049], [x[30]] * 3)
+        g.sync()
+        for s in (2047, 2048, 2049):
+            assert torch.equal(got[s], got[0]), (first, s)
+        assert torch.equal(z[0], z[1]) and torch.equal(z[0], z[2])
+        for s in (0, 2047, 2048, 2049):
+            g.seq_reset(s)
