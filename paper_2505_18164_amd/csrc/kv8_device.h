@@ -20,19 +20,30 @@ __device__ __forceinline__ long kv8_row(const Kv8Cache& c, unsigned page, int kv
   return (long)((uint64_t)page * (unsigned)(2 * c.K * c.pt) + (unsigned)(2 * kv * c.pt + pos - kv8_page_of(c, pos) * c.pt));
 }
 
-// The sample that `row` belongs to, or -1; `row` is the same in all lanes.  The samples' ends are looked at 64 at a time: one
-// round trip instead of a search's chain of them.
+// Where the last of n samples stands that `begun` holds for, one that holds for no sample behind it: a window of at most 64
+// samples, or none (len 0).  A round looks at 64 samples, one a lane, so 64 samples take none, 4096 one, 2^24 three; what a wavefront
+// does for every row or workgroup may not grow with the number of samples.
+struct Kv8Window { int base, len; };
+template <typename Begun> __device__ __forceinline__ Kv8Window kv8_window(int n, Begun&& begun) {
+  const int lane = threadIdx.x & 63;
+  int base = 0, len = n;
+  while (len > 64) {
+    const int step = (len + 63) >> 6, at = lane * step, k = __popcll(__ballot(at < len && begun(base + min(at, len - 1))));
+    if (k == 0) return Kv8Window{0, 0};
+    base += (k - 1) * step;
+    len = min(step, len - (k - 1) * step);
+  }
+  return Kv8Window{base, len};
+}
+
+// The sample that `row` belongs to, or -1; `row` is the same in all lanes.  Of the window all ends are looked at at once: one round trip
+// instead of a search's chain of them.
 __device__ __forceinline__ int kv8_sample_of(const Kv8Rows& r, int row) {
   if (!r.start) return row < r.n ? row : -1;
-  const int lane = threadIdx.x & 63;
-  int s = 0;
-  for (int base = 0; base < r.n; base += 64) {
-    const bool past = base + lane < r.n && r.start[base + lane + 1] <= row;
-    const unsigned long long m = __ballot(past);
-    s += __popcll(m);
-    if (m != ~0ull) break;
-  }
-  return s < r.n && r.start[s] <= row ? s : -1;
+  const Kv8Window w = kv8_window(r.n, [&](int i) { return r.start[i] <= row; });
+  const int lane = threadIdx.x & 63, i = w.base + min(lane, max(w.len - 1, 0));
+  const int s = w.base + __popcll(__ballot(lane < w.len && r.start[i + 1] <= row));
+  return s < w.base + w.len && r.start[s] <= row ? s : -1;
 }
 
 // A row of `tables`, or -1 when it is not there.

@@ -66,25 +66,45 @@ __device__ __forceinline__ Span rows_of(const Kv8Rows& r, int i) {
   return Span{first, min(max(r.start[i + 1], first), r.n_rows)};
 }
 
-// The sample that has block x, counting BP positions a block, and which of its blocks that is; sample < 0: there are fewer.
+// The sample that has block x, counting bp positions a block, a power of two, and which of its blocks that is; sample < 0: nobody's.
+// Up to kInOrder samples' blocks follow one another without a gap, which takes a sum over the samples before.  Of more, sample i's
+// start at first_i / bp + min(i, first_i) - rows before it, and samples that may have rows -, which leaves each as many as its
+// rows need and up to one over; there the sample is searched for.  Dense / searched, us: 257 samples of up to 64 rows of 20 heads on
+// one 70 / 75, 300 of up to 30 of the 8B shape 107 / 108, 600 of up to 20 of TinyLlama 101 / 78, 2000 of up to 10 of the 8B shape
+// 1101 / 601.  (What is over costs where the chip is just full: 4 pieces of 64 behind 8000 of the 8B shape, 256 workgroups, 60 us, with as
+// many empty ones between them 96.  Two kernels, because in one that has both the long prompts take 427 us instead of 414.)
+constexpr int kInOrder = 384;
 struct BlockPlace { int sample, block, first, rows, pos, table; };
-template <int BQ>
-__device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int g_sh) {
-  const int lane = threadIdx.x & 63, bp = BQ >> g_sh;
-  for (int base = 0, sum = 0; base < r.n; base += 64) {
-    const int i = min(base + lane, r.n - 1), pos = r.pos[i], table = r.table ? r.table[i] : i;   // (asked for along with the rows)
-    const Span s = base + lane < r.n ? rows_of(r, i) : Span{0, 0};
-    const int t = (s.end - s.first + bp - 1) / bp;
-    int up = t;
-    for (int off = 1; off < 64; off <<= 1) { const int o = __shfl_up(up, off, 64); if (lane >= off) up += o; }
-    const unsigned long long past = __ballot(sum + up > x);
-    if (past) {
-      const int at = __ffsll(past) - 1;
-      return BlockPlace{__builtin_amdgcn_readfirstlane(base + at), __builtin_amdgcn_readfirstlane(x - (sum + __shfl(up - t, at, 64))),
-                        __builtin_amdgcn_readfirstlane(__shfl(s.first, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(s.end - s.first, at, 64)),
-                        __builtin_amdgcn_readfirstlane(__shfl(pos, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(table, at, 64))};
+template <bool kMany> __device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int bp) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (!kMany) {
+    for (int base = 0, sum = 0; base < r.n; base += 64) {
+      const int i = min(base + lane, r.n - 1), pos = r.pos[i], table = r.table ? r.table[i] : i;   // (asked for along with the rows)
+      const Span s = base + lane < r.n ? rows_of(r, i) : Span{0, 0};
+      const int t = (s.end - s.first + bp - 1) / bp;
+      int up = t;
+      for (int off = 1; off < 64; off <<= 1) { const int o = __shfl_up(up, off, 64); if (lane >= off) up += o; }
+      const unsigned long long past = __ballot(sum + up > x);
+      if (past) {
+        const int at = __ffsll(past) - 1;
+        return BlockPlace{__builtin_amdgcn_readfirstlane(base + at), __builtin_amdgcn_readfirstlane(x - (sum + __shfl(up - t, at, 64))),
+                          __builtin_amdgcn_readfirstlane(__shfl(s.first, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(s.end - s.first, at, 64)),
+                          __builtin_amdgcn_readfirstlane(__shfl(pos, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(table, at, 64))};
+      }
+      sum += __shfl(up, 63, 64);
     }
-    sum += __shfl(up, 63, 64);
+  } else {
+    auto starts = [&](int i, int first) { return first / bp + min(i, first); };
+    const Kv8Window w = kv8_window(r.n, [&](int i) { return starts(i, rows_of(r, i).first) <= x; });
+    const int i = w.base + min(lane, max(w.len - 1, 0)), pos = r.pos[i], table = r.table ? r.table[i] : i;
+    const Span s = rows_of(r, i);
+    const int from = starts(i, s.first), at = __popcll(__ballot(lane < w.len && from <= x)) - 1;
+    if (at >= 0) {
+      const int block = __builtin_amdgcn_readfirstlane(x - __shfl(from, at, 64)), rows = __builtin_amdgcn_readfirstlane(__shfl(s.end - s.first, at, 64));
+      if (block >= 0 && block < (rows + bp - 1) / bp)
+        return BlockPlace{__builtin_amdgcn_readfirstlane(w.base + at), block, __builtin_amdgcn_readfirstlane(__shfl(s.first, at, 64)), rows,
+                          __builtin_amdgcn_readfirstlane(__shfl(pos, at, 64)), __builtin_amdgcn_readfirstlane(__shfl(table, at, 64))};
+    }
   }
   return BlockPlace{-1, 0, 0, 0, 0, 0};
 }
@@ -92,8 +112,8 @@ __device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int g_sh
 struct PromptGeo { int n_blocks, sets, g_sh; };                  // bound of the blocks of all samples; sets of 2^g_sh query heads
 
 // A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
-// kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.
-template <int HD, int NG, bool kWhole>
+// kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.  kMany: of more than kInOrder samples.
+template <int HD, int NG, bool kWhole, bool kMany>
 __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv8Attn a, PromptGeo geo) {
   constexpr int WQ = 8 / NG, BQ = 32 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
   constexpr int KS = HD + 8, VR = HD + 32, HT = HD / 32;
@@ -113,7 +133,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   // A sample's longest rows first, and of those all sets.  (Workgroups are handed to the eight compute dies, each with an L2 of its
   // own, in turn: with a multiple of eight sets, a set stays on its die.)
   const int block = blockIdx.x / geo.sets, set = blockIdx.x - block * geo.sets;
-  const BlockPlace at = place_of<BQ>(r, block, geo.g_sh);
+  const BlockPlace at = place_of<kMany>(r, block, BQ >> geo.g_sh);
   if (at.sample < 0) return;
   const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
   const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
@@ -506,14 +526,18 @@ constexpr size_t prompt_lds() {
   const size_t fold = (size_t)(NG - 1) * (HD / 2 + 2) * (512 / NG) * sizeof(float);
   return kv > fold ? kv : fold;
 }
-template <int HD, int NG>
+template <int HD, int NG, bool kWhole, bool kMany>
 bool allow_one() {                                               // 64 KiB is what a kernel gets by default
   constexpr size_t lds = prompt_lds<HD, NG>();
-  return lds <= 64 * 1024 || (hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess &&
-                              hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess);
+  return lds <= 64 * 1024 ||
+         hipFuncSetAttribute((const void*)k_kv8_prompt<HD, NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
+}
+template <int HD, int NG>
+bool allow_groups() {
+  return allow_one<HD, NG, true, false>() && allow_one<HD, NG, false, false>() && allow_one<HD, NG, true, true>() && allow_one<HD, NG, false, true>();
 }
 template <int HD>
-bool allow_heads() { return allow_one<HD, 1>() && allow_one<HD, 2>(); }
+bool allow_heads() { return allow_groups<HD, 1>() && allow_groups<HD, 2>(); }
 
 // Query heads of a kv head that a workgroup's rows take together: the largest power of two that divides their number, up to 32.
 int heads_shift(const Kv8Cache& c, int H) {
@@ -553,13 +577,17 @@ PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_l
   return best;
 }
 
-template <int HD, int NG>
-void launch_groups(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
+template <int HD, int NG, bool kWhole>
+void launch_pages(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
   const PromptGeo g = geo_of(c, r, a.H, 8 / NG);
   const long total = (long)g.n_blocks * g.sets;
   const dim3 grid((unsigned)total, a.plan.splits);
-  if (c.pt % BK == 0) hipLaunchKernelGGL((k_kv8_prompt<HD, NG, true>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
-  else hipLaunchKernelGGL((k_kv8_prompt<HD, NG, false>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+  if (r.n <= kInOrder) hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, false>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+  else hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, true>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+}
+template <int HD, int NG>
+void launch_groups(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
+  if (c.pt % BK == 0) launch_pages<HD, NG, true>(s, c, r, a); else launch_pages<HD, NG, false>(s, c, r, a);
 }
 template <int HD>
 void launch_heads(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
