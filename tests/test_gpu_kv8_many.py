@@ -38,10 +38,10 @@ def expected(q, codes, scales, page, pos, scale):
 def test_packed_samples(H, K, h, n):
     rng = np.random.default_rng(n)
     lens = rng.integers(0, 4, n)
-    if n > 300:
+    if n > 1000:
         lens[n // 2:n // 2 + 200] = 0                             # many without rows, and a long one behind them
     pt = 8 if n > 5000 else 512
-    lens[n // 2 + 200 if n > 300 else 40] = pt // 2 + 1
+    lens[n // 2 + 200 if n > 1000 else 40] = pt // 2 + 1
     pos = rng.integers(0, pt - lens.max() + 1, n)
     pos[rng.random(n) < 0.05] = -1
     start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
