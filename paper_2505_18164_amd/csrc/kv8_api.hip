@@ -1,4 +1,4 @@
-// The entry points of the 8-bit cache (mdi_kv8_* of mdi.h): checks on the host, then one or two launches.
+// The entry points of the 8-bit cache (mdi_kv8_* of mdi.h): checks on the host, then the launches (two at most, but for packed rows of very many samples).
 #include "kv8_internal.h"
 
 using namespace mdi;
@@ -27,8 +27,8 @@ mdi_status take(const mdi_kv8* k, const mdi_kv8_rows* g, Kv8Cache* c, Kv8Rows* r
   return st != MDI_OK ? st : take_rows(k, g, r);
 }
 
-// Query rows of the call: heads that the kv heads divide.  A launch has fewer than 2^32 threads, 256 a row and head; the tiles of all
-// units, and kKv8Begin more each, are counted in 32 bits.
+// Query rows of the call: heads that the kv heads divide.  A launch has fewer than 2^32 threads, 256 a row and head (kv8_prompt.hip,
+// which counts otherwise, takes several launches); the tiles of all units, and kKv8Begin more each, are counted in 32 bits.
 bool good_heads(const Kv8Cache& c, const Kv8Rows& r, uint32_t n_head) {
   return n_head && n_head <= 4096 && n_head % (uint32_t)c.K == 0 && (uint64_t)r.n_rows * n_head < (1ull << 24) &&
          (uint64_t)r.n * n_head * ((unsigned)r.max_ctx / kKv8Tile + 3) < (1ull << 30);

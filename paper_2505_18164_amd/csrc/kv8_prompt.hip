@@ -109,7 +109,7 @@ template <bool kMany> __device__ __forceinline__ BlockPlace place_of(const Kv8Ro
   return BlockPlace{-1, 0, 0, 0, 0, 0};
 }
 
-struct PromptGeo { int n_blocks, sets, g_sh; };                  // bound of the blocks of all samples; sets of 2^g_sh query heads
+struct PromptGeo { int n_blocks, sets, g_sh, from; };            // bound of the blocks of all samples; sets of 2^g_sh query heads; of the launch's first workgroup
 
 // A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
 // kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.  kMany: of more than kInOrder samples.
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   float* const Un = Sc + 4 * BK;                                 // [4]
   // A sample's longest rows first, and of those all sets.  (Workgroups are handed to the eight compute dies, each with an L2 of its
   // own, in turn: with a multiple of eight sets, a set stays on its die.)
-  const int block = blockIdx.x / geo.sets, set = blockIdx.x - block * geo.sets;
+  const int x = kMany ? geo.from + blockIdx.x : blockIdx.x, block = x / geo.sets, set = x - block * geo.sets;
   const BlockPlace at = place_of<kMany>(r, block, BQ >> geo.g_sh);
   if (at.sample < 0) return;
   const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
@@ -548,7 +548,7 @@ int heads_shift(const Kv8Cache& c, int H) {
 }
 PromptGeo geo_of(const Kv8Cache& c, const Kv8Rows& r, int H, int WQ) {
   const int sh = heads_shift(c, H), bp = 32 * WQ >> sh;
-  return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh};
+  return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
 }
 // Groups of a workgroup and pieces of a row's positions.  A step of 64 NG keys takes `step` us, a workgroup six or seven more to begin
 // and end; what is divided is added by a second launch, a wavefront per row and head.  How long the single samples are is on the
@@ -577,13 +577,19 @@ PromptPlan prompt_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_l
   return best;
 }
 
+// A launch has fewer than 2^32 threads.  n_rows * H is below 2^24, so the workgroups of up to kInOrder samples, at most 2^24 / 128 for
+// the rows and H for each sample, are far below that; one for each of very many samples and heads may not be, and go out in several.
+constexpr int kMostWgs = 1 << 22;
 template <int HD, int NG, bool kWhole>
 void launch_pages(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {
-  const PromptGeo g = geo_of(c, r, a.H, 8 / NG);
-  const long total = (long)g.n_blocks * g.sets;
-  const dim3 grid((unsigned)total, a.plan.splits);
-  if (r.n <= kInOrder) hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, false>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
-  else hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, true>), grid, dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+  PromptGeo g = geo_of(c, r, a.H, 8 / NG);
+  const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
+  if (r.n <= kInOrder) {
+    hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, false>), dim3(total, a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+    return;
+  }
+  for (; g.from < total; g.from += kMostWgs)
+    hipLaunchKernelGGL((k_kv8_prompt<HD, NG, kWhole, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
 }
 template <int HD, int NG>
 void launch_groups(hipStream_t s, const Kv8Cache& c, const Kv8Rows& r, const Kv8Attn& a) {

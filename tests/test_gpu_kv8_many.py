@@ -75,3 +75,25 @@ def test_packed_samples(H, K, h, n):
         want, off = expected(q[lo:hi], cache.codes, cache.scales, page[lo:hi], at0[lo:hi], h ** -0.5)
         assert bf16_between(out[lo:hi][part[lo:hi]], want[part[lo:hi]], off[part[lo:hi]]), lo
     cache.check()
+
+
+def test_more_workgroups_than_a_launch_may_have():
+    """2^18 samples of one row and 32 heads, packed: a workgroup each, of 512 threads, would be 1.004 * 2^32 threads."""
+    rng = np.random.default_rng(1)
+    n, K, h, pt = 1 << 18, 32, 64, 8
+    codes = torch.randint(-127, 128, (16, K, 2, pt, h), dtype=torch.int8, device=DEV)
+    scales = torch.rand((16, K, 2, pt), device=DEV) / 50 + 1e-3
+    dev = lambda a: torch.from_numpy(np.array(a)).to(DEV)
+    cache = mdi.Kv8Cache(codes, scales, dev(np.arange(16, dtype=np.int32).reshape(16, 1)), torch.zeros(1, dtype=torch.int32, device=DEV))
+    table, pos = rng.integers(0, 16, n).astype(np.int32), rng.integers(0, pt, n).astype(np.int32)
+    plan = cache.rows(dev(pos), start=dev(np.arange(n + 1, dtype=np.int32)), table=dev(table), n_rows=n)
+    q = torch.randn((n, K, h), dtype=torch.bfloat16, device=DEV)
+    out = torch.full_like(q, 300.0)
+    cache.attn(plan, q, out=out)
+    cache.check()
+    assert (out.abs().amax(-1) < 300).all()                       # every row and head has been written
+    some = np.concatenate([np.arange(500), rng.integers(0, n, 3000), np.arange(n - 2000, n)])
+    for at in np.array_split(some, 11):
+        i = dev(at)
+        want, off = expected(q[i], codes, scales, dev(table[at]).long(), dev(pos[at]).long(), h ** -0.5)
+        assert bf16_between(out[i], want, off), at
