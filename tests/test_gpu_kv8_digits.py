@@ -120,3 +120,37 @@ def test_scores_that_rise_from_block_to_block(h):
         s = low_first(4, h, [40, 3], [400, 420], 64, 384, lambda p: step * (6.5 - p // 64))
         cache = s.cache()
         check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, "packed", what=step)
+
+
+SHORT = [  # H, K, h, page tokens, new rows, positions behind: contexts of so few keys that roundings do not average out
+    (4, 2, 64, 16, [1, 17, 0, 64, 65], [0, 0, 4, 0, 0]),
+    (32, 4, 64, 24, [33, 130], [100, 0]),
+    (8, 8, 128, 64, [128, 1, 63], [0, 200, 1]),
+    (6, 2, 128, 7, [70], [59]),
+    (20, 1, 64, 1, [37], [5]),
+    (24, 4, 128, 32, [5] * 9, [0, 31, 32, 33, 63, 64, 65, 500, 1023]),
+    (4, 2, 40, 16, [21], [20]),
+    (2, 1, 256, 16, [19], [2]),
+]
+
+
+@pytest.mark.parametrize("loud", [1.0, 4.0], ids=["even", "few keys decide"])
+@pytest.mark.parametrize("case", SHORT, ids=lambda c: f"{c[0]}of{c[1]}x{c[2]}-page{c[3]}")
+def test_results_keep_the_digits_of_their_products(case, loud):
+    """Packed rows keep eleven digits of weights and values, single tokens sixteen of a weight times a scale, others all."""
+    H, K, h, pt, lens, behind = case
+    s = Setup(*case, seed=21, k_gain=loud)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, form_of(h), what="packed")
+    ctx = [a + b for a, b in zip(lens, behind) if a + b] + [2, 3, 5, 9]
+    s = Setup(H, K, h, pt, [1] * len(ctx), [c - 1 for c in ctx], seed=22, k_gain=loud)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), s, form_of(h, True), what="one each")
+
+
+@pytest.mark.parametrize("one_each", [False, True], ids=["packed", "tokens"])
+@pytest.mark.parametrize("H,K,h,pt,ctx", [(8, 2, 64, 16, [5000, 1, 300]), (4, 4, 128, 40, [2100, 2111]), (16, 1, 128, 64, [3333]), (3, 1, 32, 16, [1500])])
+def test_divided_results_keep_their_digits(H, K, h, pt, ctx, one_each):
+    s = Setup(H, K, h, pt, [1] * len(ctx), [c - 1 for c in ctx], seed=23)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache, one_each=one_each), s.q.to(DEV)), s, form_of(h, one_each))
