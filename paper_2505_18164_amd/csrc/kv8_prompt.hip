@@ -159,11 +159,6 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   if (lo >= hi) return;
 
   bf16x8 qf[HD / 16];
-  {
-    const bf16_t* qp = a.q + (long)(at.first + min(row, at.rows - 1)) * a.q_stride + (long)head * HD + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < HD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
-  }
   f32x16 o[HT];
 #pragma unroll
   for (int i = 0; i < HT; ++i)
@@ -178,7 +173,7 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   u32x4 kreg[KU], vreg[KU];
   float vs[KU], sk = 0.f, sv = 0.f;
   float unit = kUnitFirst, made = kUnitFirst, mine = kUnitFirst;  // of the block whose values are staged; newest that was chosen; of o
-  float least = INFINITY;                                        // of the scales that this lane has met, but zeros
+  float least = INFINITY;                                        // of the scales that this lane has met, but zeros (the group's first wavefront looks at them)
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
   auto checked = [&](int page) __attribute__((always_inline)) {
     worst = max(worst, (unsigned)page);
@@ -277,7 +272,6 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
         if (top * made > 256.f) made = __uint_as_float((127 + 5 + 127 - (__float_as_uint(top) >> 23)) << 23);   // top is less than 2^6 of these
       }
       if (v > 0.f) least = fminf(least, v);
-      if (__builtin_expect(__any(least * made < kLeastScale), 0)) again[grp] = 1;
       if (lane == 0) Un[j & 3] = made;
     }
   };
@@ -398,15 +392,20 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
 
   // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies and stages, the other takes exponentials; so the later
   // four are one turn behind.  Block j + 1's keys and block j's values, which both stage in turn j, go over blocks that both have left.
-  if (tid == 0) again[grp] = 0;                                  // (by the wavefront that looks at scales)
   pages(0);
   fetch(0);
+  {                                                              // (behind the way to the first codes, which is the longer one)
+    const bf16_t* qp = a.q + (long)(at.first + min(row, at.rows - 1)) * a.q_stride + (long)head * HD + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+  }
 #pragma unroll
   for (int n = 0; n < kUnits; ++n) stash_keys(0, n);
   stash_scales(0);
   fetch(1);
   // (the first step has no values yet: its weights are zeros, and so is what they multiply)
   for (int i = tid; i < BK * VR / 8; i += GT) *reinterpret_cast<u32x4*>(Vb + BK * VR + 8 * i) = u32x4{0, 0, 0, 0};
+  if (tid == 0) again[grp] = 0;
   __syncthreads();
   if (late) __syncthreads();
   for (int j = 0; j < n_it; ++j) {
@@ -426,14 +425,15 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
     }
     __syncthreads();
   }
-  if (__any(rise > kFar)) again[grp] = 1;                        // (a barrier before it is read)
+  if (__any(rise > kFar || least * made < kLeastScale)) again[grp] = 1;   // (least and made only fall; a barrier before it is read)
   products(n_it, std::false_type());
   if (!late) __syncthreads();
   __syncthreads();
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
-  bool over = again[0] != 0;
-  if constexpr (NG > 1) over = over || again[1] != 0;
-  if (__builtin_expect(over, 0)) {
+  int over = again[0];
+  if constexpr (NG > 1) over |= again[1];
+  over = __builtin_amdgcn_readfirstlane(over);
+  if (__builtin_expect(over != 0, 0)) {
     constexpr int L = HD / 8;
     const int ch = 8 * (lane & (L - 1));
     for (int i = threadIdx.x >> 6; i < BQ; i += 8) {             // a wavefront takes a row and head
