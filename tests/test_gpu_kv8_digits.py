@@ -154,3 +154,43 @@ def test_divided_results_keep_their_digits(H, K, h, pt, ctx, one_each):
     s = Setup(H, K, h, pt, [1] * len(ctx), [c - 1 for c in ctx], seed=23)
     cache = s.cache()
     check_digits(cache.attn(s.plan(cache, one_each=one_each), s.q.to(DEV)), s, form_of(h, one_each))
+
+
+@pytest.mark.parametrize("h", [64, 128, 40])
+@pytest.mark.parametrize("loud", [False, True], ids=["even values", "values far apart"])
+def test_a_query_that_is_not_finite_is_its_own(loud, h):
+    """A row and head with an infinity or NaN in its query is NaN (or whatever binary32 makes of it); the others know nothing of it."""
+    gain = (lambda p: np.where(p % 7 == 2, 2.0 ** 30, 1.0)) if loud else None
+    s = Setup(4, 2, h, 64, [70, 5], [0, 300], seed=31, v_gain=gain)
+    marks = {3: float("nan"), 40: float("inf"), 69: float("-inf"), 72: float("nan")}
+    q = s.q.clone()
+    for row, x in marks.items():
+        q[row, row % 4, 5] = x
+    cache = s.cache()
+    out = cache.attn(s.plan(cache), q.to(DEV)).cpu()
+    for row in marks:
+        assert not torch.isfinite(out[row, row % 4]).any()
+        out[row, row % 4] = cache.attn(s.plan(cache), s.q.to(DEV)).cpu()[row, row % 4]
+    check_digits(out, s, form_of(h), what="packed")
+    s = Setup(4, 2, h, 16, [1, 1, 1], [50, 300, 0], seed=32, v_gain=gain)
+    q = s.q.clone()
+    q[1, 2, 0], q[2, 3, h - 1] = float("nan"), float("inf")
+    cache = s.cache()
+    rows = s.plan(cache, one_each=True)
+    out, plain = cache.attn(rows, q.to(DEV)).cpu(), cache.attn(rows, s.q.to(DEV)).cpu()
+    for row, head in ((1, 2), (2, 3)):
+        assert not torch.isfinite(out[row, head]).any()
+        out[row, head] = plain[row, head]
+    check_digits(out, s, form_of(h, True), what="one each")
+
+
+@pytest.mark.parametrize("h", [64, 128, 40])
+@pytest.mark.parametrize("size", [2.0 ** -99, 2.0 ** -60, 2.0 ** 60, 2.0 ** 105])
+def test_values_at_the_ends_of_the_range(size, h):
+    """Values of every size from 2^-100 on, and as large as sums of them hold (mdi.h: their number times their size below 2^120)."""
+    s = Setup(4, 2, h, 16, [90, 3], [0, 300], seed=33, v_gain=lambda p: size + 0.0 * p)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache), s.q.to(DEV)), s, form_of(h), what="packed")
+    s = Setup(4, 2, h, 16, [1, 1, 1, 1], [50, 300, 0, 2000], seed=34, v_gain=lambda p: size + 0.0 * p)
+    cache = s.cache()
+    check_digits(cache.attn(s.plan(cache, one_each=True), s.q.to(DEV)), s, form_of(h, True), what="one each")

@@ -34,13 +34,13 @@ def expected(q, codes, scales, page, pos, scale):
     return out.reshape(m, H, h), 1.01 * off.reshape(m, H, h)
 
 
-@pytest.mark.parametrize("H,K,h,n", [(4, 2, 64, 70000), (3, 1, 128, 4097), (2, 2, 64, 4096), (8, 1, 64, 65), (4, 4, 128, 384), (4, 4, 128, 385), (2, 1, 24, 9000)])
-def test_packed_samples(H, K, h, n):
+@pytest.mark.parametrize("H,K,h,n,pt", [(4, 2, 64, 70000, 8), (3, 1, 128, 4097, 512), (2, 2, 64, 4096, 512), (8, 1, 64, 65, 512), (4, 4, 128, 384, 512),
+                                        (4, 4, 128, 385, 512), (8, 2, 64, 400, 500), (8, 2, 128, 400, 500), (2, 1, 24, 9000, 8)])
+def test_packed_samples(H, K, h, n, pt):
     rng = np.random.default_rng(n)
     lens = rng.integers(0, 4, n)
     if n > 1000:
         lens[n // 2:n // 2 + 200] = 0                             # many without rows, and a long one behind them
-    pt = 8 if n > 5000 else 512
     lens[n // 2 + 200 if n > 1000 else 40] = pt // 2 + 1
     pos = rng.integers(0, pt - lens.max() + 1, n)
     pos[rng.random(n) < 0.05] = -1
