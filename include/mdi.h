@@ -176,11 +176,15 @@ MDI_API mdi_status mdi_partition_bytes(const mdi_config *cfg, uint32_t layer_lo,
  * MDI_KV8 = the KV caches are kept in 8 bits (see mdi_kv8): (head_dim + 4) bytes
  * for a position's key or value of a kv head instead of 2 * head_dim, so the same
  * memory holds nearly twice the samples or positions.  Needs blocks, MDI_BF16,
- * max_ctx at most 2^24, max_prefill * n_head below 2^24.  All positions - a first visit's own as well - are read
- * as the cache holds them, so a prompt in pieces and in one gives the same keys
- * and values.  Such a partition runs one kernel per operation; several samples
- * share a pass over the weights in mdi_decode_batch and mdi_prefill_batch, up to
- * 64 of them and max_prefill rows.
+ * max_ctx at most 2^24, max_prefill * n_head below 2^24, n_head at most 4096,
+ * max_seqs at most 2^20 and what mdi_kv8 asks of pages and kv heads.  All positions
+ * - a first visit's own as well - are read as the cache holds them, so a prompt in
+ * pieces and in one gives the same keys and values.  Such a partition runs one
+ * kernel per operation, those of a first visit in later visits too: vectors
+ * between the matrix products are rounded to bf16 in every call, mdi_decode_step and
+ * mdi_decode_steps included, and so is the query, times the softmax's scale, before
+ * its scores.  Several samples share a pass over the weights in
+ * mdi_decode_batch and mdi_prefill_batch, up to 64 of them and max_prefill rows.
  *
  * The weights are copied, repacked, into `arena` (256-byte aligned device
  * memory of at least mdi_partition_bytes() bytes, owned by the caller and kept
@@ -228,7 +232,8 @@ MDI_API mdi_status mdi_prefill_chunk(mdi_partition *part, uint32_t seq_id, const
  * one pass over the weights for all of them: what many short prompts wait for is
  * the weights.  Other partitions take the samples one after the other.  Each
  * sample's result is that of mdi_prefill_chunk, up to the order in which partial
- * sums are added; a sample that lives and has T[i] = 1 is decoded that way.
+ * sums are added and the digits that mdi_kv8_attn keeps of single tokens and of
+ * packed rows; a sample that lives and has T[i] = 1 is decoded that way.
  * seq_ids, T: host uint32[n], the samples pairwise different.
  * Errors: as mdi_prefill_chunk, checked for all samples before the first is
  * taken; MDI_ERR_ARG also when n == 0 or a sample occurs twice.
@@ -493,8 +498,10 @@ typedef struct mdi_kv8 {
  * that is the sample's; NULL: row i.  n_rows: rows of the buffers, at most 2^24;
  * those from start[n] on belong to nobody and are left as they are.  max_ctx:
  * host's bound of pos + rows over all samples, at most table_stride *
- * page_tokens; it decides how the work is divided, so a call that is captured
- * into a graph and replayed with later positions names the last of them.
+ * page_tokens; it decides how the work is divided and whether what is read keeps a
+ * place in the device's caches, so the nearer it is the better (3 to 7 % for small
+ * caches); a call that is captured into a graph and replayed with later positions
+ * names the last of them.
  */
 typedef struct mdi_kv8_rows {
   const int32_t *table, *start, *pos;
@@ -531,7 +538,9 @@ MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, 
  * out: device bf16 [n_rows][n_head][head_dim], rows q_stride / out_stride elements
  * apart, 16-byte aligned, strides multiples of 8; they must not overlap.
  * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
- * binary32.  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
+ * binary32, and sums of weights times values are divided at the end: the number of
+ * positions times the largest magnitude of a value has to be below 2^120, and a
+ * query's sum of magnitudes below 2^121 (codes are up to 127).  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
  * 2^24, n * n_head * (max_ctx / 128 + 3) below 2^30.  Products take a weight with 16
  * digits for single tokens.  For packed rows of 64 or 128 channels weights and values
  * are binary16: a weight is at least 2^-24 or nothing, the largest being 2^6 or more; a

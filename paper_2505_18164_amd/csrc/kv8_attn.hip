@@ -6,9 +6,9 @@
 namespace mdi {
 namespace {
 
-// One workgroup per row, head and piece of the positions, its wavefronts' sums folded at the end.  It serves heads of other than 64 or 128 channels, reads the
-// cache once for every query head, and is bound by vector instructions: 16 tokens of 8100 positions of the 8B shape would take it
-// 374 us (kv8_decode.hip: 52), a prompt of 1024 of the 7B shape 710 (kv8_prompt.hip: 33).
+// One workgroup per row, head and piece of the positions, its wavefronts' sums folded at the end.  It serves heads of other than 64
+// or 128 channels, reads the cache once for every query head, and is bound by vector instructions: 16 tokens of 8100 positions of the
+// 8B shape would take it 374 us (kv8_decode.hip: 48), a prompt of 1024 of the 7B shape 710 (kv8_prompt.hip: 32).
 __global__ __launch_bounds__(kBlock) void k_kv8_attn(Kv8Cache c, Kv8Rows r, Kv8Attn a, int L) {
   __shared__ float sm[4][8 * 32 + 2];
   const int row = blockIdx.x / a.H, head = blockIdx.x - row * a.H, kv = head / (a.H / c.K), piece = blockIdx.y;

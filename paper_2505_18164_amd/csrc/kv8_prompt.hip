@@ -8,16 +8,17 @@
 // so they never leave the registers.  The workgroup turns each block's codes into bf16 keys and fp16 values once, in the LDS.
 // Which sample a workgroup belongs to it works out from `start`, 64 samples at a time, so the host knows only a bound of the grid.
 //
-// What bounds it, long prompts: 6000 + 2000 + 500 rows of the 8B shape take 416 us = 0.80 PFLOP/s, where a large matrix product
+// What bounds it, long prompts: 6000 + 2000 + 500 rows of the 8B shape take 410 to 440 us = 0.75 to 0.81 PFLOP/s, where a large matrix product
 // reaches 1.19 on the same card.  A block of 128 channels takes 2.15 us, some 4700 cycles, in which a SIMD's matrix core works 2048
-// for its two wavefronts; the vector unit works about as long on their 4096 scores (product with the scale, largest, exponential,
-// conversion: four and a half instructions each, on 64 at a time, of 4.6 cycles and more) and on the codes, and the LDS delivers
-// 32 KB of operands to each wavefront.  Three choices follow.  The wavefronts of a SIMD take turns - one multiplies and stages
+// for its two wavefronts; the vector unit works a little longer on their 4096 scores (product with the scale, largest, exponential,
+// conversion: four and a half instructions each, on 64 at a time, of 4.5 cycles) and on the codes, and the LDS delivers
+// 32 KB of operands to each wavefront.  Counted: of the time that a compute unit has work its matrix cores are busy 38 %, its vector
+// units 45 %, its LDS 34 % (14 % of that bank conflicts).  No one of them is the limit; that two turns do not overlap further is.  Three choices follow.  The wavefronts of a SIMD take turns - one multiplies and stages
 // while the other takes exponentials -, with two barriers a block.  Operands are read one set of four ahead of their products.  A
 // block's codes are asked for a whole block before they are staged.  More wavefronts on a SIMD instead, which have to do with 128
 // registers, cost more in spills than they hide (8 prompts of TinyLlama 56 -> 82 us).
 // Short prompts: a block after the other.  1024 rows of the 7B shape are 256 workgroups, one for each compute unit, of which the
-// longest passes over 16 blocks: two groups of wavefronts take half of the blocks each (45 -> 33 us); six us are the way to the first
+// longest passes over 16 blocks: two groups of wavefronts take half of the blocks each (45 -> 32 us); six us are the way to the first
 // block - rows, page numbers, codes, each behind the one before.
 #include <algorithm>
 #include <cmath>

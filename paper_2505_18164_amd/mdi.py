@@ -433,7 +433,8 @@ class Kv8Cache:
 
     def rows(self, pos, start=None, table=None, n_rows=None, max_ctx=None):
         """pos int32 [n]; start int32 [n + 1] (None: one row per sample), table int32 [n] (None: row i of the tables); n_rows:
-        rows of the call's buffers (needed with start); max_ctx: no sample gets longer (default: what the tables hold)."""
+        rows of the call's buffers (needed with start); max_ctx: no sample gets longer (default: what the tables hold; a nearer bound
+        divides the work better)."""
         n = pos.shape[0]
         self._tensor(pos, torch.int32, "pos")
         for t, size, what in ((start, n + 1, "start"), (table, n, "table")):
