@@ -540,14 +540,15 @@ MDI_API mdi_status mdi_kv8_read(const mdi_kv8 *cache, const mdi_kv8_rows *rows, 
  * Rows of a sample that takes no part become zeros.  Scores, softmax and sums are
  * binary32, and sums of weights times values are divided at the end: the number of
  * positions times the largest magnitude of a value has to be below 2^120, and a
- * query's sum of magnitudes below 2^121 (codes are up to 127).  n_head: a multiple of n_kv_head, at most 4096; n_rows * n_head below
- * 2^24, n * n_head * (max_ctx / 128 + 3) below 2^30.  Products take a weight with 16
- * digits for single tokens.  For packed rows of 64 or 128 channels weights and values
- * are binary16: a weight is at least 2^-24 or nothing, the largest being 2^6 or more (a
- * result lacks up to 2^-30 of the sum of magnitudes of the values that it sees); a
- * value keeps eleven digits, whatever a later position holds.  (Among values
- * whose sizes are further than 2^20 apart rows are computed in binary32 instead, which
- * takes tens of times as long.)
+ * query's sum of magnitudes below 2^121 (codes are up to 127).  n_head: a multiple of
+ * n_kv_head, at most 4096; n_rows * n_head below 2^24, n * n_head * (max_ctx / 128 + 3)
+ * below 2^30.  Products take a weight with 16 digits for single tokens.  For packed
+ * rows of 64 or 128 channels weights and values are binary16: a weight is at least
+ * 2^-24 or nothing, the largest being 2^6 or more (a result lacks up to 2^-30 of the
+ * sum of magnitudes of the values that it sees); a value keeps eleven digits, whatever a
+ * later position holds.  (Where values' sizes are further than 2^20 apart, or scores
+ * rise by more than 2^9 behind far lower ones, rows are computed in binary32 instead,
+ * which takes tens of times as long.)
  * workspace: mdi_kv8_attn_bytes() bytes of device memory, 16-byte aligned (0 bytes:
  * may be NULL); it carries nothing from one call to the next, and calls that can
  * run at the same time need one each.  Results do not depend on timing.
