@@ -563,6 +563,83 @@ MDI_API mdi_status mdi_kv8_attn_bytes(const mdi_kv8 *cache, const mdi_kv8_rows *
                               size_t *workspace_bytes);
 
 /*
+ * A key/value cache in the storage type, bf16 or fp32, in pages: what a partition
+ * keeps in its arena ("rotating KV caches", Sec. III-D), for programs that run
+ * their layers themselves.  data: device memory of the caller, 16-byte aligned,
+ * [n_pages][n_kv_head][2: key, value][page_tokens][head_dim] in dtype (MDI_F32 or
+ * MDI_BF16).  tables, err and the limits are those of mdi_kv8, and so are the rows
+ * of a call (mdi_kv8_rows).
+ */
+typedef struct mdi_kv {
+  void *data;
+  const int32_t *tables;
+  int32_t *err;
+  uint32_t dtype, n_pages, n_kv_head, head_dim, page_tokens, n_tables, table_stride;
+} mdi_kv;
+
+/*
+ * What happens to query and key heads on their way (device vectors; NULL for this
+ * struct or a member: not that part).  First the norm of a head x [head_dim] with
+ * gain g and bias b, binary32 [head_dim], 16-byte aligned: MDI_NORM_RMSNORM
+ * x / sqrt(mean(x^2) + eps) * g + b, MDI_NORM_LAYERNORM (x - mean(x)) /
+ * sqrt(variance(x) + eps) * g + b; queries with q_g, q_b, keys with k_g, k_b, a
+ * kind of head without a gain is not normalised; eps at least 0.  Then the rotation
+ * of the first `rot` channels at position p: the angle of pair i, channels i and
+ * i + rot / 2, is p * freq[i], freq binary64 [rot / 2] in radians (base^(-2i/rot), or
+ * what a model makes of it).  rot: a multiple of 8, at most head_dim; 0: no rotation.
+ * Angles are taken in binary64, all else in binary32, rounded once at the end.
+ */
+typedef struct mdi_qk_prep {
+  const float *q_g, *q_b, *k_g, *k_b;
+  const double *freq;
+  float eps;
+  uint32_t norm_kind, rot;
+} mdi_qk_prep;
+
+/*
+ * Append rows to the cache: keys, after `prep`, and values as they are go to their
+ * positions' places in the pages; queries, after `prep`, to q_out, where mdi_kv_attn
+ * takes them.  All in the cache's dtype.  k, v: as in mdi_kv8_write.  q: element (row,
+ * head, channel) at row * q_row_stride + head * q_head_stride + channel; q_out:
+ * [n_rows][n_head][head_dim], rows q_out_stride elements apart; both 16-byte aligned,
+ * strides multiples of 16 bytes; q_out may be q itself, laid out alike, but must not
+ * overlap it otherwise.  n_head: a multiple of n_kv_head, at most 4096, or 0: no
+ * queries (q and q_out NULL).  Rows of samples that take no part, rows of nobody, and
+ * rows whose page or position is reported (see err) are left as they were, in q_out too.
+ * n_rows * (n_head + 2 n_kv_head) * head_dim below 2^33.  No two rows of a call may go
+ * to the same position of the same page.
+ * Errors: MDI_ERR_ARG for what the descriptions exclude; n = 0 does nothing.
+ */
+MDI_API mdi_status mdi_kv_append(const mdi_kv *cache, const mdi_kv8_rows *rows, const mdi_qk_prep *prep, const void *k,
+                         const void *v, uint64_t row_stride, uint64_t head_stride, const void *q,
+                         uint64_t q_row_stride, uint64_t q_head_stride, uint32_t n_head, void *q_out,
+                         uint64_t q_out_stride, void *hip_stream);
+
+/*
+ * Attention of the call's rows over their samples' caches, single tokens (start =
+ * NULL) or packed pieces of prompts, as mdi_kv8_attn; q and out in the cache's dtype.
+ * The row at position p sees the positions j <= p with p - j < window or j < sinks:
+ * a sliding window of the newest positions, its own among them, and the first ones,
+ * which stay.  window = 0: all positions up to p (sinks is ignored).  What no row of
+ * the call sees is not read, so pages that lie wholly behind the window and the sinks
+ * can be given to others; their table entries may hold anything, and so may what a
+ * page holds at positions that a row does not see (infinities and NaN included).
+ * Scores, softmax and sums are binary32, and sums of weights times values are divided
+ * at the end: the number of positions times the largest magnitude of a value has to be
+ * below 2^120, and |scale| times a query's and key's sum of magnitudes of products below 2^120.
+ * Products of fp32 are fp32's.  Limits, alignment (strides multiples of 16 bytes),
+ * workspace and errors are those of mdi_kv8_attn, its size mdi_kv_attn_bytes'.
+ * Results do not depend on timing.
+ */
+MDI_API mdi_status mdi_kv_attn(const mdi_kv *cache, const mdi_kv8_rows *rows, const void *q, uint64_t q_stride,
+                       uint32_t n_head, float scale, uint32_t window, uint32_t sinks, void *out, uint64_t out_stride,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace that mdi_kv_attn needs for these rows (host only; the device arrays are not read). */
+MDI_API mdi_status mdi_kv_attn_bytes(const mdi_kv *cache, const mdi_kv8_rows *rows, uint32_t n_head, uint32_t window,
+                             uint32_t sinks, size_t *workspace_bytes);
+
+/*
  * The node leaves the ring (the starter's stop message of Sec. III-A ends a
  * secondary's loop, Alg. 2): frees the host object.  Nothing is enqueued and
  * nothing waited for: the caller drains the partition's stream first

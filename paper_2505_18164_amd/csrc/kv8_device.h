@@ -6,17 +6,17 @@
 
 namespace mdi {
 
-__device__ __forceinline__ void kv8_report(const Kv8Cache& c) {
+__device__ __forceinline__ void kv8_report(const KvPages& c) {
   if (c.err) __hip_atomic_store(c.err, 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Quotient of a position and the page size (exact: table_stride * pt * pt < 2^32 is checked on the host).
-__device__ __forceinline__ int kv8_page_of(const Kv8Cache& c, int pos) {
+__device__ __forceinline__ int kv8_page_of(const KvPages& c, int pos) {
   return (int)(__umulhi((unsigned)pos, c.pt_magic) | ((unsigned)pos & c.pt_one));
 }
 
 // The key of position pos in `page`, as a row of codes or an index of scales; its value is c.pt further.
-__device__ __forceinline__ long kv8_row(const Kv8Cache& c, unsigned page, int kv, int pos) {
+__device__ __forceinline__ long kv8_row(const KvPages& c, unsigned page, int kv, int pos) {
   return (long)((uint64_t)page * (unsigned)(2 * c.K * c.pt) + (unsigned)(2 * kv * c.pt + pos - kv8_page_of(c, pos) * c.pt));
 }
 
@@ -47,19 +47,19 @@ __device__ __forceinline__ int kv8_sample_of(const Kv8Rows& r, int row) {
 }
 
 // A row of `tables`, or -1 when it is not there.
-__device__ __forceinline__ int kv8_checked_row(const Kv8Cache& c, int t) {
+__device__ __forceinline__ int kv8_checked_row(const KvPages& c, int t) {
   if ((unsigned)t < (unsigned)c.n_tables) return t;
   kv8_report(c);
   return -1;
 }
 
 // The row of `tables` that is a sample's, or -1 when the one it names is not there.
-__device__ __forceinline__ int kv8_table_row(const Kv8Cache& c, const Kv8Rows& r, int sample) {
+__device__ __forceinline__ int kv8_table_row(const KvPages& c, const Kv8Rows& r, int sample) {
   return kv8_checked_row(c, r.table ? r.table[sample] : sample);
 }
 
 // A page number that is not of this cache is reported and page 0 read in its place.
-__device__ __forceinline__ int kv8_checked_page(const Kv8Cache& c, int page) {
+__device__ __forceinline__ int kv8_checked_page(const KvPages& c, int page) {
   if ((unsigned)page < (unsigned)c.n_pages) return page;
   kv8_report(c);
   return 0;
@@ -69,7 +69,7 @@ __device__ __forceinline__ int kv8_checked_page(const Kv8Cache& c, int page) {
 struct Kv8View {
   int sample, seen;                  // sample < 0: no sample's row, its output is left alone; seen = 0: its output is zeros
 };
-__device__ __forceinline__ Kv8View kv8_view(const Kv8Cache& c, const Kv8Rows& r, int row) {
+__device__ __forceinline__ Kv8View kv8_view(const KvPages& c, const Kv8Rows& r, int row) {
   Kv8View v{kv8_sample_of(r, row), 0};
   if (v.sample < 0) return v;
   const int p0 = r.pos[v.sample];

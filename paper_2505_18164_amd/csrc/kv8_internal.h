@@ -12,12 +12,14 @@
 
 namespace mdi {
 
-struct Kv8Cache {                    // mdi_kv8 as the kernels take it
-  int8_t* codes; float* scales;      // [n_pages][K][2][pt][h], [n_pages][K][2][pt]
+struct KvPages {                     // how a paged cache lies, whatever its rows are: of 8 bits here, of the storage type in kv_internal.h
   const int32_t* tables; int32_t* err;
   int n_pages, K, h, pt;
   unsigned pt_magic, pt_one;         // page of a position: the high word of pos * pt_magic, or (pages of one) the position & pt_one
   int n_tables, table_stride;
+};
+struct Kv8Cache : KvPages {          // mdi_kv8 as the kernels take it
+  int8_t* codes; float* scales;      // [n_pages][K][2][pt][h], [n_pages][K][2][pt]
 };
 struct Kv8Rows {                     // mdi_kv8_rows
   const int32_t *table, *start, *pos;
@@ -36,7 +38,7 @@ void launch_kv8_read(hipStream_t s, int dtype, const Kv8Cache& c, const Kv8Rows&
 // wgs > 0 (kv8_decode.hip): the cut is another, all samples' positions in equal shares for so many workgroups, of at least `chunk`.
 constexpr int kKv8Tile = 128;        // positions that shares are counted in
 struct Kv8Plan { int chunk, splits, wgs, groups; };   // groups: kv8_prompt.hip's, of wavefronts in a workgroup
-__host__ __device__ inline int kv8_groups(const Kv8Cache& c, int H) { return (H / c.K + 15) / 16; }   // sets of up to sixteen query heads of a kv head
+__host__ __device__ inline int kv8_groups(const KvPages& c, int H) { return (H / c.K + 15) / 16; }   // sets of up to sixteen query heads of a kv head
 Kv8Plan kv8_plan(const Kv8Cache& c, const Kv8Rows& r, int H, size_t part_limit = SIZE_MAX);   // part_limit: room for the pieces' sums
 inline size_t kv8_part_bytes(const Kv8Plan& p, const Kv8Cache& c, const Kv8Rows& r, int H) {
   return p.splits > 1 ? (size_t)r.n_rows * H * p.splits * (c.h + 2) * sizeof(float) : 0;
@@ -74,7 +76,7 @@ struct Kv8Handoff { const void* rows; void* out[kMaxVisits]; int n, bytes; };   
 void launch_kv8_handoff(hipStream_t s, const Kv8Handoff& a);
 
 // The geometry of a cache; false when its positions or sizes are beyond what the kernels count with.
-inline bool kv8_geometry(uint64_t n_pages, uint64_t n_kv_head, uint64_t head_dim, uint64_t page_tokens, uint64_t n_tables, uint64_t table_stride, Kv8Cache* c) {
+inline bool kv8_geometry(uint64_t n_pages, uint64_t n_kv_head, uint64_t head_dim, uint64_t page_tokens, uint64_t n_tables, uint64_t table_stride, KvPages* c) {
   if (!n_pages || !n_kv_head || !head_dim || !page_tokens || !n_tables || !table_stride) return false;
   if (head_dim % 8 || head_dim > 256 || n_kv_head > 1024 || n_pages > INT32_MAX || n_tables > INT32_MAX) return false;
   // a position is divided by the page size with one multiplication, exact below the second bound

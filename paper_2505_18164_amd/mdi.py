@@ -17,11 +17,13 @@ MDI_ABI_VERSION = 1
 MDI_OK, MDI_ERR_ARG, MDI_ERR_STATE, MDI_ERR_CTX, MDI_ERR_NOMEM, MDI_ERR_HIP, MDI_ERR_LIMIT = 0, -1, -2, -3, -4, -5, -6
 MDI_F32, MDI_BF16 = 0, 1
 MDI_HAS_EMBED, MDI_HAS_HEAD, MDI_KV8 = 1, 2, 4
+MDI_NORM_LAYERNORM, MDI_NORM_RMSNORM = 0, 1
 
 EXPORTS = ["mdi_partition_bytes", "mdi_partition_create", "mdi_prefill", "mdi_prefill_chunk", "mdi_prefill_batch", "mdi_decode_step", "mdi_decode_steps", "mdi_decode_batch",
            "mdi_sample_greedy", "mdi_sample_topk", "mdi_sample_topk_static", "mdi_sample_batch", "mdi_partition_sync", "mdi_seq_reset", "mdi_seq_len", "mdi_step_bytes", "mdi_time_kernel",
            "mdi_partition_info", "mdi_partition_trace", "mdi_partition_destroy", "mdi_strerror",
-           "mdi_kv8_write", "mdi_kv8_read", "mdi_kv8_attn", "mdi_kv8_attn_bytes"]
+           "mdi_kv8_write", "mdi_kv8_read", "mdi_kv8_attn", "mdi_kv8_attn_bytes",
+           "mdi_kv_append", "mdi_kv_attn", "mdi_kv_attn_bytes"]
 
 
 class MdiConfig(C.Structure):
@@ -52,6 +54,15 @@ class MdiKv8(C.Structure):
 
 class MdiKv8Rows(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("table", "start", "pos")] + [(n, C.c_uint32) for n in ("n", "n_rows", "max_ctx")]
+
+
+class MdiKv(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("data", "tables", "err")] + \
+               [(n, C.c_uint32) for n in ("dtype", "n_pages", "n_kv_head", "head_dim", "page_tokens", "n_tables", "table_stride")]
+
+
+class MdiQkPrep(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_g", "q_b", "k_g", "k_b", "freq")] + [("eps", C.c_float)] + [(n, C.c_uint32) for n in ("norm_kind", "rot")]
 
 
 class MdiError(RuntimeError):
@@ -99,6 +110,10 @@ def lib():
         L.mdi_kv8_read.argtypes = [kv8, rows, vp, vp, u32, u64, u64, vp]
         L.mdi_kv8_attn.argtypes = [kv8, rows, vp, u64, u32, C.c_float, vp, u64, vp, C.c_size_t, vp]
         L.mdi_kv8_attn_bytes.argtypes = [kv8, rows, u32, C.POINTER(C.c_size_t)]
+        kv, prep = C.POINTER(MdiKv), C.POINTER(MdiQkPrep)
+        L.mdi_kv_append.argtypes = [kv, rows, prep, vp, vp, u64, u64, vp, u64, u64, u32, vp, u64, vp]
+        L.mdi_kv_attn.argtypes = [kv, rows, vp, u64, u32, C.c_float, u32, u32, vp, u64, vp, C.c_size_t, vp]
+        L.mdi_kv_attn_bytes.argtypes = [kv, rows, u32, u32, u32, C.POINTER(C.c_size_t)]
         for name in EXPORTS:
             if name not in ("mdi_partition_destroy", "mdi_strerror"):
                 getattr(L, name).restype = C.c_int
@@ -396,25 +411,9 @@ class Kv8Rows:
         self._ref = C.byref(struct)
 
 
-class Kv8Cache:
-    """A key/value cache in 8 bits (mdi_kv8): codes int8 [pages, kv heads, 2, page tokens, head_dim], scales float32
-    [pages, kv heads, 2, page tokens], tables int32 [samples, pages of a sample], all contiguous on one GPU; err: int32 [1]
-    or None, see check().  Calls enqueue on the current stream of that GPU."""
-
-    def __init__(self, codes, scales, tables, err=None):
-        if codes.dim() != 5 or codes.shape[2] != 2 or scales.shape != codes.shape[:4] or tables.dim() != 2:
-            raise ValueError("codes [pages, kv heads, 2, page tokens, head_dim], scales [pages, kv heads, 2, page tokens], tables [samples, pages]")
-        self.device = codes.device
-        self._tensor(codes, torch.int8, "codes")
-        self._tensor(scales, torch.float32, "scales")
-        self._tensor(tables, torch.int32, "tables")
-        if err is not None:
-            self._tensor(err, torch.int32, "err")
-        self.codes, self.scales, self.tables, self.err = codes, scales, tables, err
-        self.n_pages, self.K, _, self.page_tokens, self.h = codes.shape
-        self._c = MdiKv8(_ptr(codes), _ptr(scales), _ptr(tables), _ptr(err), self.n_pages, self.K, self.h, self.page_tokens,
-                         tables.shape[0], tables.shape[1])
-        self._ref = C.byref(self._c)
+class _PagedCache:
+    """What the paged caches have in common: the rows of a call, calls on the current stream of their GPU, device-side checks.
+    A cache has device, tables, page_tokens and err."""
 
     def _tensor(self, t, dtype, what, contiguous=True):
         if t.dtype != dtype or t.device != self.device or (contiguous and not t.is_contiguous()):
@@ -449,6 +448,36 @@ class Kv8Cache:
         if not (0 <= n_rows < 1 << 32 and 0 <= max_ctx < 1 << 32):
             raise ValueError("n_rows, max_ctx: beyond 32 bits")
         return Kv8Rows((pos, start, table), MdiKv8Rows(_ptr(table), _ptr(start), _ptr(pos), n, n_rows, max_ctx), n_rows, self.device)
+
+    def check(self):
+        """Wait for the current stream and report what only the device can detect (needs err): an MdiError for a page, table
+        row or position outside the cache."""
+        torch.cuda.current_stream(self.device).synchronize()
+        if self.err is not None and int(self.err.item()):
+            raise MdiError(MDI_ERR_ARG, self._name)
+
+
+class Kv8Cache(_PagedCache):
+    """A key/value cache in 8 bits (mdi_kv8): codes int8 [pages, kv heads, 2, page tokens, head_dim], scales float32
+    [pages, kv heads, 2, page tokens], tables int32 [samples, pages of a sample], all contiguous on one GPU; err: int32 [1]
+    or None, see check().  Calls enqueue on the current stream of that GPU."""
+
+    _name = "mdi_kv8"
+
+    def __init__(self, codes, scales, tables, err=None):
+        if codes.dim() != 5 or codes.shape[2] != 2 or scales.shape != codes.shape[:4] or tables.dim() != 2:
+            raise ValueError("codes [pages, kv heads, 2, page tokens, head_dim], scales [pages, kv heads, 2, page tokens], tables [samples, pages]")
+        self.device = codes.device
+        self._tensor(codes, torch.int8, "codes")
+        self._tensor(scales, torch.float32, "scales")
+        self._tensor(tables, torch.int32, "tables")
+        if err is not None:
+            self._tensor(err, torch.int32, "err")
+        self.codes, self.scales, self.tables, self.err = codes, scales, tables, err
+        self.n_pages, self.K, _, self.page_tokens, self.h = codes.shape
+        self._c = MdiKv8(_ptr(codes), _ptr(scales), _ptr(tables), _ptr(err), self.n_pages, self.K, self.h, self.page_tokens,
+                         tables.shape[0], tables.shape[1])
+        self._ref = C.byref(self._c)
 
     def _rows_io(self, rows, k, v, what):
         shape, stride, dtype = k.shape, k.stride(), k.dtype
@@ -496,9 +525,124 @@ class Kv8Cache:
                    0 if workspace is None else workspace.numel() * workspace.element_size())
         return out
 
-    def check(self):
-        """Wait for the current stream and report what only the device can detect (needs err): an MdiError for a page, table
-        row or position outside the cache."""
-        torch.cuda.current_stream(self.device).synchronize()
-        if self.err is not None and int(self.err.item()):
-            raise MdiError(MDI_ERR_ARG, "mdi_kv8")
+
+class QkPrep:
+    """What happens to query and key heads on their way into a cache (mdi_qk_prep), made by KvCache.prep; keeps its device
+    vectors alive."""
+
+    def __init__(self, keep, struct, device):
+        self._keep, self._c, self.device = keep, struct, device
+        self._ref = C.byref(struct)
+
+
+def rope_freq(rot, base=10000.0, device="cuda:0"):
+    """The angles by which `rot` channels turn from one position to the next: base^(-2i/rot), float64 [rot / 2]."""
+    return torch.tensor([float(base) ** (-2.0 * i / rot) for i in range(rot // 2)], dtype=torch.float64, device=device)
+
+
+_NORMS = {"layer": MDI_NORM_LAYERNORM, "rms": MDI_NORM_RMSNORM}
+
+
+class KvCache(_PagedCache):
+    """A key/value cache in the storage type (mdi_kv): data bfloat16 or float32 [pages, kv heads, 2, page tokens, head_dim], tables
+    int32 [samples, pages of a sample], both contiguous on one GPU; err: int32 [1] or None, see check().  Calls enqueue on the
+    current stream of that GPU."""
+    _name = "mdi_kv"
+
+    def __init__(self, data, tables, err=None):
+        if data.dim() != 5 or data.shape[2] != 2 or tables.dim() != 2:
+            raise ValueError("data [pages, kv heads, 2, page tokens, head_dim], tables [samples, pages]")
+        if data.dtype not in _KV8_TYPES:
+            raise ValueError("data: bfloat16 or float32")
+        self.device, self.dtype = data.device, data.dtype
+        self._tensor(data, data.dtype, "data")
+        self._tensor(tables, torch.int32, "tables")
+        if err is not None:
+            self._tensor(err, torch.int32, "err")
+        self.data, self.tables, self.err = data, tables, err
+        self.n_pages, self.K, _, self.page_tokens, self.h = data.shape
+        self._c = MdiKv(_ptr(data), _ptr(tables), _ptr(err), _KV8_TYPES[data.dtype], self.n_pages, self.K, self.h, self.page_tokens,
+                        tables.shape[0], tables.shape[1])
+        self._ref = C.byref(self._c)
+
+    def prep(self, freq=None, norm="rms", q_gain=None, k_gain=None, q_bias=None, k_bias=None, eps=1e-6):
+        """Norms and rotation for append: freq float64 [rot / 2] (see rope_freq; None: no rotation); norm "rms" or "layer" with gains
+        and biases float32 [head_dim] (a kind of head without a gain is not normalised, without a bias nothing is added)."""
+        if norm not in _NORMS:
+            raise ValueError("norm: rms or layer")
+        for t, what in ((q_gain, "q_gain"), (k_gain, "k_gain"), (q_bias, "q_bias"), (k_bias, "k_bias")):
+            if t is not None:
+                self._tensor(t, torch.float32, what)
+                if t.shape != (self.h,):
+                    raise ValueError(f"{what}: expected {self.h} channels")
+        rot = 0
+        if freq is not None:
+            self._tensor(freq, torch.float64, "freq")
+            if freq.dim() != 1:
+                raise ValueError("freq [rot / 2]")
+            rot = 2 * freq.shape[0]
+        keep = (q_gain, q_bias, k_gain, k_bias, freq)
+        return QkPrep(keep, MdiQkPrep(*[_ptr(t) for t in keep], eps, _NORMS[norm], rot), self.device)
+
+    def _heads(self, x, heads, rows, what):
+        """Address, row stride and head stride of x [rows, heads, head_dim]."""
+        shape, stride = x.shape, x.stride()
+        if shape != (rows.n_rows, heads, self.h) or stride[2] != 1 or x.dtype != self.dtype or x.device != self.device:
+            raise ValueError(f"append: {what} {self.dtype} [rows, {heads} heads, {self.h}] on {self.device}, channels next to each other")
+        return x.data_ptr(), stride[0] if shape[0] > 1 else heads * self.h, stride[1] if heads > 1 else self.h
+
+    def append(self, rows, k, v, q=None, prep=None, q_out=None):
+        """Rows k, v [rows, kv heads, head_dim] into the cache and q [rows, heads, head_dim] into q_out (any row and head stride, the
+        cache's type), keys and queries through `prep` on the way (see prep(); None: as they are).  Returns q_out, a new tensor
+        by default; it may be q itself."""
+        if rows.device != self.device or (prep is not None and prep.device != self.device):
+            raise ValueError(f"append: rows and prep on {self.device}")
+        kp, k_row, k_head = self._heads(k, self.K, rows, "k")
+        vp, v_row, v_head = self._heads(v, self.K, rows, "v")
+        if (k_row, k_head) != (v_row, v_head):
+            raise ValueError("append: k and v laid out alike")
+        qp, q_row, q_head, heads, op, out_row = None, 0, 0, 0, None, 0
+        if q is not None:
+            heads = q.shape[1] if q.dim() == 3 else 0
+            qp, q_row, q_head = self._heads(q, heads, rows, "q")
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            op, out_row, out_head = self._heads(q_out, heads, rows, "q_out")
+            if out_head != self.h:
+                raise ValueError("append: heads of q_out next to each other")
+        elif q_out is not None:
+            raise ValueError("append: q_out without q")
+        self._call("mdi_kv_append", self._ref, rows._ref, None if prep is None else prep._ref, kp, vp, k_row, k_head, qp, q_row, q_head, heads, op, out_row)
+        return q_out
+
+    def workspace(self, rows, n_head, window=0, sinks=0):
+        """A workspace for attn calls on these rows (None when none is needed)."""
+        n = C.c_size_t(0)
+        st = lib().mdi_kv_attn_bytes(self._ref, rows._ref, n_head, window, sinks, C.byref(n))
+        if st != MDI_OK:
+            raise MdiError(st, "mdi_kv_attn_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device) if n.value else None
+
+    def attn(self, rows, q, scale=None, window=0, sinks=0, out=None, workspace=None):
+        """Attention of rows q [rows, heads, head_dim] (the cache's type) over their samples' caches: everything up to a row's own
+        position, or with a window the newest `window` positions and the first `sinks`; scale: head_dim ** -0.5.  workspace: as made by
+        workspace() (None: taken from the allocator for this call)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        shape, qs, os, h = q.shape, q.stride(), out.stride(), self.h
+        if (len(shape) != 3 or shape[0] != rows.n_rows or shape[2] != h or out.shape != shape or q.dtype != self.dtype or out.dtype != self.dtype
+                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or q.device != self.device or out.device != self.device
+                or rows.device != self.device):
+            raise ValueError(f"attn: q and out {self.dtype} [rows, heads, {h}] on {self.device}, heads next to each other")
+        if not (0 <= window < 1 << 32 and 0 <= sinks < 1 << 32):
+            raise ValueError("window, sinks: beyond 32 bits")
+        heads = shape[1]
+        if workspace is None:
+            workspace = self.workspace(rows, heads, window, sinks)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"attn: a contiguous workspace on {self.device}")
+        alone = shape[0] < 2                                     # a lone row has no neighbours, whatever its stride says
+        self._call("mdi_kv_attn", self._ref, rows._ref, q.data_ptr(), heads * h if alone else qs[0], heads, h ** -0.5 if scale is None else scale,
+                   window, sinks, out.data_ptr(), heads * h if alone else os[0], None if workspace is None else workspace.data_ptr(),
+                   0 if workspace is None else workspace.numel() * workspace.element_size())
+        return out
