@@ -92,27 +92,32 @@ __device__ __forceinline__ float2* kv8_part_marks(const Kv8Attn& a, const Kv8Cac
 // side, kKv8Begin more for every unit, what it costs to begin one - and workgroup w has w * per .. + per - 1 of them.  Every
 // wavefront works this out for itself, 64 samples at a time; `seen` is what the first 64 see, one a lane.
 constexpr int kKv8Begin = 2;         // (1, 2, 4: 30.2, 29.8, 32.1 us for 8 samples of 1 .. 4096 positions of the 7B shape)
-__device__ __forceinline__ int kv8_seen(const Kv8Cache& c, const Kv8Rows& r, int sample) { return sample < r.n ? kv8_view(c, r, sample).seen : 0; }
+__device__ __forceinline__ int kv8_seen(const KvPages& c, const Kv8Rows& r, int sample) { return sample < r.n ? kv8_view(c, r, sample).seen : 0; }
 __device__ __forceinline__ int kv8_tiles(int seen) { return (seen + kKv8Tile - 1) / kKv8Tile; }
 __device__ __forceinline__ int kv8_cost(const Kv8Rows& r, int sample, int seen) { return sample < r.n ? kv8_tiles(seen) + kKv8Begin : 0; }
 
 struct Kv8Stream { int cost, per, before; };                     // of one unit of every sample; a share; of those before `sample`
-__device__ __forceinline__ Kv8Stream kv8_stream(const Kv8Cache& c, const Kv8Rows& r, const Kv8Plan& p, int units, int sample, int seen) {
+template <typename Seen>                                         // seen_of(i): what sample i sees (0: none), `seen` that of the first 64, one a lane
+__device__ __forceinline__ Kv8Stream kv8_stream_of(const Kv8Rows& r, int chunk, int wgs, int units, int sample, int seen, Seen&& seen_of) {
   int sum = 0, before = 0;
   for (int i = threadIdx.x & 63; i < r.n; i += 64) {
-    const int t = kv8_cost(r, i, i < 64 ? seen : kv8_seen(c, r, i));
+    const int t = kv8_cost(r, i, i < 64 ? seen : seen_of(i));
     sum += t;
     if (i < sample) before += t;
   }
   for (int off = 32; off >= 1; off >>= 1) { sum += __shfl_xor(sum, off, 64); before += __shfl_xor(before, off, 64); }
   sum = __builtin_amdgcn_readfirstlane(sum);
-  return Kv8Stream{sum, max(p.chunk / kKv8Tile, (int)(((long)sum * units + p.wgs - 1) / p.wgs)), __builtin_amdgcn_readfirstlane(before)};
+  return Kv8Stream{sum, max(chunk / kKv8Tile, (int)(((long)sum * units + wgs - 1) / wgs)), __builtin_amdgcn_readfirstlane(before)};
+}
+__device__ __forceinline__ Kv8Stream kv8_stream(const Kv8Cache& c, const Kv8Rows& r, const Kv8Plan& p, int units, int sample, int seen) {
+  return kv8_stream_of(r, p.chunk, p.wgs, units, sample, seen, [&](int i) { return kv8_seen(c, r, i); });
 }
 struct Kv8Found { int sample, start, seen; };                    // the sample in whose unit `x` lies, and where that unit starts
-__device__ __forceinline__ Kv8Found kv8_find(const Kv8Cache& c, const Kv8Rows& r, int x, int seen) {
+template <typename Seen>
+__device__ __forceinline__ Kv8Found kv8_find_of(const Kv8Rows& r, int x, int seen, Seen&& seen_of) {
   const int lane = threadIdx.x & 63;
   for (int base = 0, sum = 0;; base += 64) {
-    if (base) seen = kv8_seen(c, r, base + lane);
+    if (base) seen = seen_of(base + lane);
     const int t = kv8_cost(r, base + lane, seen);
     int up = t;
     for (int off = 1; off < 64; off <<= 1) { const int o = __shfl_up(up, off, 64); if (lane >= off) up += o; }
@@ -124,6 +129,9 @@ __device__ __forceinline__ Kv8Found kv8_find(const Kv8Cache& c, const Kv8Rows& r
     }
     sum += __shfl(up, 63, 64);
   }
+}
+__device__ __forceinline__ Kv8Found kv8_find(const Kv8Cache& c, const Kv8Rows& r, int x, int seen) {
+  return kv8_find_of(r, x, seen, [&](int i) { return kv8_seen(c, r, i); });
 }
 
 constexpr float kKv8None = -3e38f;   // reference of a softmax that has seen nothing

@@ -59,6 +59,12 @@ __device__ __forceinline__ int* kv_part_counts(const KvAttn& a, const KvPages& c
   return reinterpret_cast<int*>(a.part + (long)r.n_rows * a.H * a.plan.splits * (c.h + 2));
 }
 
+// How many places the newest row of a sample sees (one new token per sample); 0: it takes no part.
+__device__ __forceinline__ int kv_places(const KvPages& c, const KvRows& r, const KvSight& w, int sample) {
+  const int seen = kv8_seen(c, r, sample);
+  return seen ? kv_span(w, seen).places() : 0;
+}
+
 constexpr float kKvNone = -3e38f;    // reference of a softmax that has seen nothing
 
 // One row and head by a wavefront, for any head: L lanes hold eight channels each of a position (`ch` on, `live` where the head has

@@ -31,7 +31,8 @@ inline int kv_most_seen(const KvSight& w, int max_ctx) { return (int)std::min<lo
 // How an attention call is divided: what a row sees goes to workgroups in pieces, at most `splits` of them.  A row with one piece is
 // finished where it is computed; of the others every piece leaves its h weighted sums, its reference and its sum of
 // weights, which a second launch adds.  How many pieces a row and head has is left by whoever computes the first one.
-struct KvPlan { int chunk, splits; };
+// wgs > 0 (kv_decode.hip): the cut is another, all samples' places in equal shares for so many workgroups, of at least `chunk`.
+struct KvPlan { int chunk, splits, wgs; };
 inline size_t kv_part_bytes(const KvPlan& p, const KvCache& c, const KvRows& r, int H) {
   return p.splits > 1 ? (size_t)r.n_rows * H * (p.splits * (size_t)(c.h + 2) + 1) * sizeof(float) : 0;
 }
@@ -42,6 +43,10 @@ struct KvAttn {
   KvSight sight;
   float* part; KvPlan plan;
 };
+// One new token per sample in bf16 with heads of 64 or 128: on the matrix cores (kv_decode.hip).
+bool kv_decode_supported(const KvCache& c, const KvRows& r);
+KvPlan kv_decode_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
+void launch_kv_decode(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 
