@@ -98,6 +98,7 @@ mdi_status mdi_kv_attn(const mdi_kv* cache, const mdi_kv8_rows* rows, const void
   const size_t need = kv_part_bytes(plan, c, r, (int)n_head);
   if (need && (!workspace || !aligned16(workspace))) return MDI_ERR_ARG;
   if (need > workspace_bytes) return MDI_ERR_NOMEM;
+  if (!kv_allow_lds()) return MDI_ERR_HIP;
   launch_kv_attn((hipStream_t)hip_stream, c, r, KvAttn{q, (long)q_stride, out, (long)out_stride, (int)n_head, scale2, sight, (float*)workspace, plan});
   return hip_status();
 }

@@ -109,6 +109,7 @@ void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   while (8 * L < c.h) L *= 2;
   const unsigned items = (unsigned)(r.n_rows * a.H);
   if (kv_decode_supported(c, r)) launch_kv_decode(s, c, r, a);
+  else if (kv_prompt_supported(c, r)) launch_kv_prompt(s, c, r, a);
   else hipLaunchKernelGGL((k_kv_attn<T>), dim3(items, a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
   if (a.plan.splits > 1) hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
 }
@@ -117,6 +118,7 @@ void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
 
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
   if (kv_decode_supported(c, r)) return kv_decode_plan(c, r, H, w);
+  if (kv_prompt_supported(c, r)) return kv_prompt_plan(c, r, H, w);
   const int most = kv_most_seen(w, r.max_ctx);
   const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / ((long)r.n_rows * H)));
   KvPlan p{};

@@ -1,0 +1,491 @@
+// Attention of packed rows - prompts, or the next pieces of prompts, of several samples - over the bf16 cache, on the matrix cores.
+//
+// A workgroup takes 32 rows of (position, query head) for each of its wavefronts, the heads of one kv head side by side, and passes
+// over the keys they see 64 at a time (KvBlocks).  A wavefront computes S^T = K Q^T with v_mfma_f32_32x32x16_bf16, weighs the scores
+// against a reference of its row, and adds O^T += V^T P^T: the scores of a query lie in the lane, and in the order, in which the second
+// product takes weights, so they never leave the registers.  Keys and values travel from the pages to the LDS without passing
+// registers, a block ahead, 16 bytes a lane; the 16-byte units of a row are permuted by the row's number (the permutation is
+// applied to the address in memory, the LDS then holds it for free), which spreads both kinds of reads over all banks.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "kv8_mfma.h"
+#include "kv_blocks.h"
+#include "kv_device.h"
+#include "once_per_device.h"
+
+namespace mdi {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
+typedef __attribute__((address_space(3))) u32x4* lds_u32x4;
+
+constexpr int BK = 64;               // keys of a step
+// Weights are counted from a reference of their row, the largest score of the first block that the row sees; it is raised only
+// when a block's weights sum to more than this: weights of any size keep their digits in bf16 and in the sums, which are divided
+// out at the end.  So no maximum is looked for where nothing is raised.
+constexpr float kMostSum = 0x1p16f;
+
+__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(uintptr_t)at));
+}
+__device__ __forceinline__ u32x4 read_lds(uint32_t at) { return *(lds_u32x4)(uintptr_t)at; }
+// 64 x 16 bytes global -> LDS: lane l's piece lands at lds + 16 l.
+__device__ __forceinline__ void dma(uint32_t lds, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void dma(uint32_t lds, const void* p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "m0", "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The blocks of 64 positions that some row of a workgroup sees, its first row at position `at`, `end` behind its last: those
+// of the first positions, then from the one that the first row's window begins in.
+struct KvBlocks { int sinks, n_sinks, first, from, end, n; };
+__device__ __forceinline__ KvBlocks kv_blocks(const KvSight& w, int at, int end) {
+  KvBlocks b;
+  b.end = end;
+  b.from = max(at + 1 - w.window, 0);
+  b.sinks = min(w.sinks, b.from);
+  const int s64 = (b.sinks + 63) >> 6, f64 = b.from >> 6;
+  b.n_sinks = s64 < f64 ? s64 : 0;
+  b.first = b.n_sinks || b.sinks == 0 ? f64 << 6 : 0;
+  b.n = b.n_sinks + ((end - b.first + 63) >> 6);
+  return b;
+}
+
+struct PromptGeo { int n_blocks, sets, g_sh, from; };            // bound of the blocks of all samples; sets of 2^g_sh query heads; of the launch's first workgroup
+
+// A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
+// kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.  kMany: of more than kInOrder samples.
+template <int HD, int NG, bool kWhole, bool kMany>
+__global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
+  constexpr int WQ = 8 / NG, BQ = 32 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
+  constexpr int HT = HD / 32, RB = 2 * HD, UN = HD / 8;          // bytes and 16-byte units of a key
+  constexpr int BB = BK * RB;                                    // bytes of a block of keys, or of values
+  constexpr int KP = 64 / UN, NI = BK / KP / WQ;                 // keys of an instruction that loads, instructions of a wavefront
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int again;
+
+  const int tid = threadIdx.x & (GT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = NG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GT), late = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const uint32_t Kb = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + grp * 4 * BB, Vb = Kb + 2 * BB;
+  // A sample's longest rows first, and of those all sets.  (Workgroups are handed to the eight compute dies, each with an L2 of its
+  // own, in turn: with a multiple of eight sets, a set stays on its die.)
+  const int x = kMany ? geo.from + blockIdx.x : blockIdx.x, block = x / geo.sets, set = x - block * geo.sets;
+  const BlockPlace at = place_of<kMany>(r, block, BQ >> geo.g_sh);
+  if (at.sample < 0) return;
+  const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
+  const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
+  const int which = kv8_checked_row(c, at.table), p0 = at.pos;
+  const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
+  const int col = lane & 31, half = lane >> 5;
+  const int row = q0 + ((32 * wave + col) >> g_sh), head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
+  const bool live = row < at.rows;
+  const int item = (at.first + row) * a.H + head;
+  bf16_t* out = (bf16_t*)a.out + (long)(at.first + row) * a.out_stride + (long)head * HD;
+  if (p0 < 0 || which < 0) {                                     // takes no part
+    if (blockIdx.y == 0 && grp == 0 && live) {
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<u32x2*>(out + 32 * i + 8 * g + 4 * half) = u32x2{0, 0};
+      if (a.plan.splits > 1 && half == 0) kv_part_counts(a, c, r)[item] = 1;
+    }
+    return;
+  }
+  // positions up to `pos` are seen by this lane's row; the block's rows end before `far`
+  const long far = (long)p0 + min(q0 + bp, at.rows);
+  if (far > r.max_ctx) kv8_report(c);
+  const int pos = (int)min((long)p0 + min(row, at.rows - 1), (long)r.max_ctx - 1);
+  const KvBlocks kb = kv_blocks(a.sight, (int)min((long)p0 + q0, (long)r.max_ctx - 1), (int)min(far, (long)r.max_ctx));
+  const int b_lo = blockIdx.y * a.plan.chunk, b_hi = (int)min((long)kb.n, (long)b_lo + a.plan.chunk), pieces = (kb.n + a.plan.chunk - 1) / a.plan.chunk;
+  if (b_lo >= b_hi) return;
+
+  bf16x8 qf[HD / 16];
+  f32x16 o[HT];
+#pragma unroll
+  for (int i = 0; i < HT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = kKvNone, l = 0.f;
+  const int wave_pos = (int)min((long)p0 + min(q0 + ((32 * wave) >> g_sh), at.rows - 1), (long)r.max_ctx - 1);   // of the wavefront's first row
+  const int last_pos = (int)min((long)p0 + min(q0 + ((32 * wave + 31) >> g_sh), at.rows - 1), (long)r.max_ctx - 1);
+
+  // Loading.  Stage j: the keys of block j and the values of block j - 1.  A position that no row of the workgroup sees is not read, one
+  // near it in its place.
+  const int n_it = (b_hi - b_lo + NG - 1) / NG;
+  auto block_of = [&](int j) __attribute__((always_inline)) { return min(b_lo + NG * j + grp, b_hi - 1); };
+  auto start_of = [&](int b) __attribute__((always_inline)) { return b < kb.n_sinks ? b << 6 : kb.first + ((b - kb.n_sinks) << 6); };
+  auto visible = [&](int p, int k0) __attribute__((always_inline)) {
+    return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
+  };
+  // lane's key of instruction n, and where in it the 16 bytes are that land at its place
+  auto key_of = [&](int n) __attribute__((always_inline)) { return (wave * NI + n) * KP + lane / UN; };
+  auto unit_of = [&](int key) __attribute__((always_inline)) {
+    return (lane % UN) ^ ((HD == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2) | ((key >> 2) & 3));
+  };
+  unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
+  auto checked = [&](int page) __attribute__((always_inline)) {
+    worst = max(worst, (unsigned)page);
+    return min((unsigned)page, (unsigned)c.n_pages - 1);
+  };
+  int pg[kWhole ? 1 : NI];
+  uint32_t v_off[kWhole ? NI : 1] = {};
+  const char* v_at[kWhole ? 1 : NI] = {};
+  const long v_by = (long)c.pt * RB;                             // from a key to its value
+  auto pages = [&](int j) __attribute__((always_inline)) {
+    const int k0 = start_of(block_of(j));
+    if constexpr (kWhole) {
+      int p = kv8_page_of(c, k0);
+      asm volatile("" : "+v"(p));                                // a vector load: behind a scalar one every read of LDS would have to wait for it
+      pg[0] = table[p];
+    } else {
+#pragma unroll
+      for (int n = 0; n < NI; ++n) pg[n] = table[kv8_page_of(c, visible(k0 + key_of(n), k0))];
+    }
+  };
+  auto issue = [&](int j) __attribute__((always_inline)) {
+    const int k0 = start_of(block_of(j));
+    const uint32_t k_lds = Kb + (j & 1) * BB + wave * NI * 1024, v_lds = Vb + ((j - 1) & 1) * BB + wave * NI * 1024;
+    if constexpr (kWhole) {
+      if (j > 0)
+#pragma unroll
+        for (int n = 0; n < NI; ++n) dma(v_lds + 1024 * n, v_at[0], v_off[n]);
+      const int in_page = k0 - kv8_page_of(c, k0) * c.pt;
+      const char* const kp = (const char*)c.data + ((long)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)checked(pg[0])) * (unsigned)(2 * c.K * c.pt)) + 2 * kv * c.pt + in_page) * RB;
+      const bool inside = (k0 >= kb.from && k0 + BK <= kb.end) || k0 + BK <= kb.sinks;
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        int key = key_of(n);
+        const int unit = unit_of(key);
+        if (!inside) key = visible(k0 + key, k0) - k0;
+        v_off[n] = (uint32_t)(key * RB + 16 * unit);
+        dma(k_lds + 1024 * n, kp, v_off[n]);
+      }
+      v_at[0] = kp + v_by;
+    } else {
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        if (j > 0) dma(v_lds + 1024 * n, v_at[n]);
+        const int key = key_of(n);
+        const char* const kp = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key);
+        dma(k_lds + 1024 * n, kp);
+        v_at[n] = kp + v_by;
+      }
+    }
+    pages(j + 1);
+  };
+
+  // what this lane reads: keys `col` and col + 32, 16 bytes at channels 16 ks + 8 half; values 4 half + kk and 8 further, of every 16 keys,
+  // 8 bytes at channels 32 i + 16 ((lane / 16) mod 2) + 4 (lane mod 4)
+  const int kk = (lane & 15) >> 2;
+  const uint32_t k_lane = col * RB + 16 * (half ^ ((HD == 128 ? (col & 3) << 2 : ((col >> 1) & 1) << 2) | ((col >> 2) & 3)));
+  const uint32_t v_lane = (4 * half + kk) * RB + 64 * (HD == 128 ? kk : kk >> 1) + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
+
+  auto sees = [&](int j) __attribute__((always_inline)) {        // some row of the wavefront, some key of the block
+    if (b_lo + NG * j + grp >= b_hi) return false;
+    const int k0 = start_of(block_of(j));
+    return k0 <= last_pos && (k0 + BK - 1 > wave_pos - a.sight.window || k0 < a.sight.sinks);
+  };
+  f32x16 s[2];
+  u32x4 pf[4] = {};                                              // weights, two a word
+  // The products of a step: the values of block j - 1 with its weights, the keys of block j with the queries.  Four operands are
+  // on their way from the LDS while the four before them are multiplied.
+  auto products = [&](int j, auto keys) __attribute__((always_inline)) {
+    constexpr int kSets = decltype(keys)::value ? 2 * HT : HT;   // sets of four operands: HT of values, HT of keys
+    const uint32_t V = Vb + ((j - 1) & 1) * BB + v_lane, K = Kb + (j & 1) * BB + k_lane;
+    u32x4 f[2][4];
+    auto read = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (n < HT) {
+          const uint32_t p = (V ^ (64 * (x % HT))) + 16 * ((4 * n + x) / HT) * RB;
+          const u32x2 b0 = read_transposed(p), b1 = read_transposed((p ^ 32) + 8 * RB);
+          f[n & 1][x] = u32x4{b0.x, b0.y, b1.x, b1.y};
+        } else {
+          f[n & 1][x] = read_lds((K ^ (32 * (2 * (n - HT) + (x >> 1)))) + 32 * (x & 1) * RB);
+        }
+      }
+    };
+    read(0);
+#pragma unroll
+    for (int n = 0; n < kSets; ++n) {
+      if (n + 1 < kSets) read(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (n < HT) {
+          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), __builtin_bit_cast(bf16x8, pf[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
+        } else {
+          const int k = 2 * (n - HT) + (x >> 1);
+          s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), qf[k], k ? s[x & 1] : f32x16{}, 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // The weights of block j from its scores, rounded to bf16 as the product takes them; their sum takes them as they are multiplied.
+  auto weigh = [&](int j, auto mask) __attribute__((always_inline)) {
+    constexpr bool kMask = decltype(mask)::value;                // some of these keys are not for some of the rows
+    const int k0 = start_of(block_of(j)) + 4 * half, up_to = pos - k0, from = up_to - a.sight.window, stay = a.sight.sinks - k0;
+    auto score = [&](int t, int e, float ref) __attribute__((always_inline)) {
+      const float v = fmaf(s[t][e], a.scale, -ref);
+      if constexpr (!kMask) return v;
+      const int key = 32 * t + 8 * (e >> 2) + (e & 3);
+      return key <= up_to && (key > from || key < stay) ? v : -INFINITY;
+    };
+    float sum;
+    auto weights = [&]() __attribute__((always_inline)) {
+      sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const bf16x2 w = {(__bf16)exp2_raw(score(t, e, m)), (__bf16)exp2_raw(score(t, e + 1, m))};
+          sum = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
+          pf[2 * t + (e >> 3)][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+        }
+    };
+    weights();
+    if (__builtin_expect(__any(!(sum < kMostSum)), 0)) {         // (the first block that a row sees, too)
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, score(t, e, 0.f));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));                 // both lanes of a row raise alike
+      const float to = fmaxf(m, top), alpha = exp2_raw(m - to);
+      m = to;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float v = o[i][e] * alpha;
+          asm volatile("" : "+v"(v));                            // (one after the other, in place: else they are copied, and others spilled)
+          o[i][e] = v;
+        }
+      weights();
+    }
+    l += sum;
+  };
+  auto soften = [&](int j) __attribute__((always_inline)) {
+    if (!sees(j)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) pf[t] = u32x4{0, 0, 0, 0};
+      return;
+    }
+    const int k0 = start_of(block_of(j));
+    const bool whole = k0 + BK - 1 <= wave_pos && (k0 > last_pos - a.sight.window || k0 + BK <= a.sight.sinks);
+    if (whole) weigh(j, std::false_type()); else weigh(j, std::true_type());
+  };
+
+  // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies, the other takes exponentials; so the later four are one
+  // turn behind.  Stage j + 1 is asked for in the turn in which the early ones multiply block j, over blocks that all have left, and
+  // waited for at the end of the next.
+  pages(0);
+  issue(0);
+  {                                                              // (behind the way to the first keys, which is the longer one)
+    const bf16_t* qp = (const bf16_t*)a.q + (long)(at.first + min(row, at.rows - 1)) * a.q_stride + (long)head * HD + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+  }
+  // (the first step has no values yet: its weights are zeros, and so is what they multiply)
+  for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + BB + 16 * i) = u32x4{0, 0, 0, 0};
+  if (threadIdx.x == 0) again = 0;
+  wait_loads();
+  __syncthreads();
+  if (late) {
+    issue(1);
+    __syncthreads();
+  }
+  for (int j = 0; j < n_it; ++j) {
+    if (!late) issue(j + 1);
+    products(j, std::true_type());
+    if (late) wait_loads();
+    __syncthreads();
+    if (late) issue(j + 2);
+    soften(j);
+    if (!late) wait_loads();
+    __syncthreads();
+  }
+  products(n_it, std::false_type());
+  if (late) wait_loads();                                        // (what was asked for last is for nobody)
+  if (worst >= (unsigned)c.n_pages) kv8_report(c);
+  l += __shfl_xor(l, 32, 64);
+  // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
+  // are computed once more, each by itself.  (Weights that are no numbers are what they should be.)
+  {
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) odd = fmaf(o[i][e], 0.f, odd);
+    if (__any(!(odd == 0.f) && l - l == 0.f)) again = 1;
+  }
+  if (!late) __syncthreads();
+  __syncthreads();
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) {
+    constexpr int L = HD / 8;
+    const int ch = 8 * (lane & (L - 1));
+    for (int i = threadIdx.x >> 6; i < BQ; i += 8) {             // a wavefront takes a row and head
+      const int row1 = q0 + (i >> g_sh), head1 = head0 + (i & ((1 << g_sh) - 1)), item1 = (at.first + row1) * a.H + head1;
+      if (row1 >= at.rows) continue;
+      const int end1 = (int)min((long)p0 + row1 + 1, (long)r.max_ctx), from1 = max(end1 - a.sight.window, 0), shift = kb.first - 64 * kb.n_sinks;
+      const KvSpan span{min(a.sight.sinks, from1), 64 * kb.n_sinks, shift, from1, end1};
+      float q[8];
+      KvType<bf16_t>::load8((const bf16_t*)a.q + (long)(at.first + row1) * a.q_stride + (long)head1 * HD + ch, q);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] *= a.scale;
+      const KvSums sums = kv_attend<bf16_t>(c, table, kv, span, q, L, ch, true, 64 * b_lo, 64 / L, min(64 * b_hi, end1 - shift));
+      if (lane >= L) continue;
+      bf16_t* const out1 = (bf16_t*)a.out + (long)(at.first + row1) * a.out_stride + (long)head1 * HD + ch;
+      float* const part = kv_part_sums(a, c, item1, blockIdx.y) + ch;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (pieces == 1) out1[e] = f32_to_bf16(sums.o[e] / sums.l);
+        else part[e] = sums.o[e];
+      if (lane == 0 && pieces > 1) *kv_part_marks(a, c, r, item1, blockIdx.y) = make_float2(sums.m, sums.l);
+      if (lane == 0 && blockIdx.y == 0 && a.plan.splits > 1) kv_part_counts(a, c, r)[item1] = pieces;
+    }
+    return;
+  }
+
+  if constexpr (NG > 1) {
+    float* fold = (float*)smem;
+    if (grp > 0) {
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) fold[(i * 16 + e) * GT + tid] = o[i][e];
+      fold[(HT * 16) * GT + tid] = m;
+      fold[(HT * 16 + 1) * GT + tid] = l;
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    const float m1 = fold[(HT * 16) * GT + tid], l1 = fold[(HT * 16 + 1) * GT + tid];
+    const float to = fmaxf(m, m1), a0 = exp2_raw(m - to), a1 = exp2_raw(m1 - to);
+    l = l * a0 + l1 * a1;
+    m = to;
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * a0 + fold[(i * 16 + e) * GT + tid] * a1;
+  }
+
+  if (!live) return;
+  if (a.plan.splits > 1 && blockIdx.y == 0 && half == 0) kv_part_counts(a, c, r)[item] = pieces;
+  if (pieces == 1) {
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint32_t w0 = (uint32_t)f32_to_bf16(o[i][4 * g] * inv) | ((uint32_t)f32_to_bf16(o[i][4 * g + 1] * inv) << 16);
+        const uint32_t w1 = (uint32_t)f32_to_bf16(o[i][4 * g + 2] * inv) | ((uint32_t)f32_to_bf16(o[i][4 * g + 3] * inv) << 16);
+        *reinterpret_cast<u32x2*>(out + 32 * i + 8 * g + 4 * half) = u32x2{w0, w1};
+      }
+  } else {
+    float* part = kv_part_sums(a, c, item, blockIdx.y);
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(part + 32 * i + 8 * g + 4 * half) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+    if (half == 0) *kv_part_marks(a, c, r, item, blockIdx.y) = make_float2(m, l);
+  }
+}
+
+template <int HD, int NG>
+constexpr size_t prompt_lds() {
+  const size_t kv = (size_t)NG * 4 * BK * 2 * HD, fold = (size_t)(NG - 1) * (HD / 2 + 2) * (512 / NG) * sizeof(float);
+  return kv > fold ? kv : fold;
+}
+template <int HD, int NG, bool kWhole, bool kMany>
+bool allow_one() {                                               // 64 KiB is what a kernel gets by default
+  constexpr size_t lds = prompt_lds<HD, NG>();
+  return hipFuncSetAttribute((const void*)k_kv_prompt<HD, NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
+}
+template <int HD, int NG>
+bool allow_groups() {
+  return allow_one<HD, NG, true, false>() && allow_one<HD, NG, false, false>() && allow_one<HD, NG, true, true>() && allow_one<HD, NG, false, true>();
+}
+
+PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int WQ) {
+  const int sh = kv_heads_shift(c, H), bp = 32 * WQ >> sh;
+  return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
+}
+// Groups of a workgroup and pieces of a row's blocks.  A step of 64 NG keys takes `step` us, a workgroup some more to begin
+// and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are taken for equal.
+struct PromptPlan { int groups, splits; };
+PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
+  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
+  const double heads = (double)r.n_rows * H;
+  PromptPlan best{1, 1};
+  double best_us = 1e30;
+  for (int ng = 1; ng <= 2; ++ng) {
+    const int sh = kv_heads_shift(c, H), bp = 256 / ng >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, rows) + 64);
+    const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.0 : 2.4) : (ng == 1 ? 1.35 : 1.55);
+    const double seen = std::min<double>(most, r.max_ctx - 0.5 * std::min(r.max_ctx, rows));   // what a workgroup sees, on average
+    for (int s = 1; s <= 32; s *= 2) {
+      if (s > 1 && most < 256 * s) break;
+      const double longest = std::ceil(most / (64. * ng * s)), all = items * seen / (64. * ng * 256);
+      double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
+      if (s > 1) us += 2 + heads / 2000 + heads * s * c.h / 4e6;
+      if (us < best_us) { best_us = us; best = PromptPlan{ng, s}; }
+    }
+  }
+  return best;
+}
+
+// A launch has fewer than 2^32 threads.  n_rows * H is below 2^24, so the workgroups of up to kInOrder samples, at most 2^24 / 128 for
+// the rows and H for each sample, are far below that; one for each of very many samples and heads may not be, and go out in several.
+constexpr int kMostWgs = 1 << 22;
+template <int HD, int NG, bool kWhole>
+void launch_pages(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  PromptGeo g = geo_of(c, r, a.H, 8 / NG);
+  const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
+  if (r.n <= kInOrder) {
+    hipLaunchKernelGGL((k_kv_prompt<HD, NG, kWhole, false>), dim3(total, a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+    return;
+  }
+  for (; g.from < total; g.from += kMostWgs)
+    hipLaunchKernelGGL((k_kv_prompt<HD, NG, kWhole, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
+}
+template <int HD, int NG>
+void launch_groups(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  if (c.pt % BK == 0) launch_pages<HD, NG, true>(s, c, r, a); else launch_pages<HD, NG, false>(s, c, r, a);
+}
+template <int HD>
+void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  if (a.plan.groups == 1) launch_groups<HD, 1>(s, c, r, a); else launch_groups<HD, 2>(s, c, r, a);
+}
+
+}  // namespace
+
+bool kv_prompt_supported(const KvCache& c, const KvRows& r) { return r.start && c.dtype == MDI_BF16 && (c.h == 64 || c.h == 128); }
+bool kv_allow_lds() {
+  static OncePerDevice done;
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_groups<64, 1>() && allow_groups<64, 2>() && allow_groups<128, 1>() && allow_groups<128, 2>(); });
+}
+
+KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
+  const PromptPlan p = prompt_plan(c, r, H, w);
+  // blocks that a workgroup of up to `bp` positions may have: of the first ones, and of a window that begins inside one
+  const int bp = 256 / p.groups >> kv_heads_shift(c, H);
+  const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
+  const int chunk = (int)((most + p.splits - 1) / p.splits);
+  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
+}
+
+void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  if (c.h == 128) launch_heads<128>(s, c, r, a); else launch_heads<64>(s, c, r, a);
+}
+
+}  // namespace mdi
