@@ -113,6 +113,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = kKvNone, l = 0.f;
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);
   const int wave_pos = (int)min((long)p0 + min(q0 + ((32 * wave) >> g_sh), at.rows - 1), (long)r.max_ctx - 1);   // of the wavefront's first row
   const int last_pos = (int)min((long)p0 + min(q0 + ((32 * wave + 31) >> g_sh), at.rows - 1), (long)r.max_ctx - 1);
 
@@ -153,11 +154,15 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
     const int k0 = start_of(block_of(j));
     const uint32_t k_lds = Kb + (j & 1) * BB + wave * NI * 1024, v_lds = Vb + ((j - 1) & 1) * BB + wave * NI * 1024;
     if constexpr (kWhole) {
+      // (the page's number is looked at before anything else is asked for: whoever waits for it waits for that, too)
+      unsigned page = __builtin_amdgcn_readfirstlane((int)checked(pg[0]));
+      asm volatile("" : "+s"(page));
+      pages(j + 1);
       if (j > 0)
 #pragma unroll
         for (int n = 0; n < NI; ++n) dma(v_lds + 1024 * n, v_at[0], v_off[n]);
       const int in_page = k0 - kv8_page_of(c, k0) * c.pt;
-      const char* const kp = (const char*)c.data + ((long)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)checked(pg[0])) * (unsigned)(2 * c.K * c.pt)) + 2 * kv * c.pt + in_page) * RB;
+      const char* const kp = (const char*)c.data + ((long)((uint64_t)page * (unsigned)(2 * c.K * c.pt)) + 2 * kv * c.pt + in_page) * RB;
       const bool inside = (k0 >= kb.from && k0 + BK <= kb.end) || k0 + BK <= kb.sinks;
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
@@ -169,16 +174,21 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       }
       v_at[0] = kp + v_by;
     } else {
+      const char* kp[NI];
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        const int key = key_of(n);
+        kp[n] = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key);
+        asm volatile("" : "+v"(kp[n]));
+      }
+      pages(j + 1);
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
         if (j > 0) dma(v_lds + 1024 * n, v_at[n]);
-        const int key = key_of(n);
-        const char* const kp = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key);
-        dma(k_lds + 1024 * n, kp);
-        v_at[n] = kp + v_by;
+        dma(k_lds + 1024 * n, kp[n]);
+        v_at[n] = kp[n] + v_by;
       }
     }
-    pages(j + 1);
   };
 
   // what this lane reads: keys `col` and col + 32, 16 bytes at channels 16 ks + 8 half; values 4 half + kk and 8 further, of every 16 keys,
@@ -230,15 +240,9 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
     }
   };
   // The weights of block j from its scores, rounded to bf16 as the product takes them; their sum takes them as they are multiplied.
-  auto weigh = [&](int j, auto mask) __attribute__((always_inline)) {
-    constexpr bool kMask = decltype(mask)::value;                // some of these keys are not for some of the rows
-    const int k0 = start_of(block_of(j)) + 4 * half, up_to = pos - k0, from = up_to - a.sight.window, stay = a.sight.sinks - k0;
-    auto score = [&](int t, int e, float ref) __attribute__((always_inline)) {
-      const float v = fmaf(s[t][e], a.scale, -ref);
-      if constexpr (!kMask) return v;
-      const int key = 32 * t + 8 * (e >> 2) + (e & 3);
-      return key <= up_to && (key > from || key < stay) ? v : -INFINITY;
-    };
+  float alpha = 1.f;
+  bool raised = false;
+  auto weigh = [&]() __attribute__((always_inline)) {
     float sum;
     auto weights = [&]() __attribute__((always_inline)) {
       sum = 0.f;
@@ -246,7 +250,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const bf16x2 w = {(__bf16)exp2_raw(score(t, e, m)), (__bf16)exp2_raw(score(t, e + 1, m))};
+          const bf16x2 w = {(__bf16)exp2_raw(fmaf(s[t][e], scale, -m)), (__bf16)exp2_raw(fmaf(s[t][e + 1], scale, -m))};
           sum = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
           pf[2 * t + (e >> 3)][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
         }
@@ -257,19 +261,13 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, score(t, e, 0.f));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));                 // both lanes of a row raise alike
-      const float to = fmaxf(m, top), alpha = exp2_raw(m - to);
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;         // both lanes of a row raise alike
+      const float to = fmaxf(m, top);
+      alpha = exp2_raw(m - to);
+      raised = true;
       m = to;
       l *= alpha;
-#pragma unroll
-      for (int i = 0; i < HT; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float v = o[i][e] * alpha;
-          asm volatile("" : "+v"(v));                            // (one after the other, in place: else they are copied, and others spilled)
-          o[i][e] = v;
-        }
       weights();
     }
     l += sum;
@@ -281,8 +279,17 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       return;
     }
     const int k0 = start_of(block_of(j));
-    const bool whole = k0 + BK - 1 <= wave_pos && (k0 > last_pos - a.sight.window || k0 + BK <= a.sight.sinks);
-    if (whole) weigh(j, std::false_type()); else weigh(j, std::true_type());
+    if (k0 + BK - 1 > wave_pos || (k0 <= last_pos - a.sight.window && k0 + BK > a.sight.sinks)) {   // some of these keys are not for some of the rows
+      const int up_to = pos - k0 - 4 * half, from = up_to - a.sight.window, stay = a.sight.sinks - k0 - 4 * half;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 32 * t + 8 * (e >> 2) + (e & 3);
+          s[t][e] = key <= up_to && (key > from || key < stay) ? s[t][e] : -INFINITY;
+        }
+    }
+    weigh();
   };
 
   // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies, the other takes exponentials; so the later four are one
@@ -292,30 +299,58 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   issue(0);
   {                                                              // (behind the way to the first keys, which is the longer one)
     const bf16_t* qp = (const bf16_t*)a.q + (long)(at.first + min(row, at.rows - 1)) * a.q_stride + (long)head * HD + 8 * half;
+    u32x4 w[HD / 16];
 #pragma unroll
-    for (int ks = 0; ks < HD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+    for (int ks = 0; ks < HD / 16; ++ks) w[ks] = *reinterpret_cast<const u32x4*>(qp + 16 * ks);
+    // (scores are multiplied by a positive number: a masked one is -inf before that)
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : ~0u;
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t x = (w[ks][i] ^ flip) & keep;
+        asm volatile("" : "+v"(x));                              // (looked at here: else the loop waits for them, and for all that it has asked for)
+        w[ks][i] = x;
+      }
+      qf[ks] = __builtin_bit_cast(bf16x8, w[ks]);
+    }
   }
   // (the first step has no values yet: its weights are zeros, and so is what they multiply)
   for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + BB + 16 * i) = u32x4{0, 0, 0, 0};
   if (threadIdx.x == 0) again = 0;
   wait_loads();
   __syncthreads();
-  if (late) {
-    issue(1);
-    __syncthreads();
-  }
-  for (int j = 0; j < n_it; ++j) {
-    if (!late) issue(j + 1);
-    products(j, std::true_type());
-    if (late) wait_loads();
-    __syncthreads();
-    if (late) issue(j + 2);
-    soften(j);
-    if (!late) wait_loads();
-    __syncthreads();
-  }
-  products(n_it, std::false_type());
-  if (late) wait_loads();                                        // (what was asked for last is for nobody)
+  auto turns = [&](auto second) __attribute__((always_inline)) {
+    constexpr bool kLate = decltype(second)::value;
+    if constexpr (kLate) {
+      issue(1);
+      __syncthreads();
+    }
+    for (int j = 0; j < n_it; ++j) {
+      if constexpr (!kLate) issue(j + 1);
+      products(j, std::true_type());
+      if constexpr (kLate) wait_loads();
+      __syncthreads();
+      if constexpr (kLate) issue(j + 2);
+      soften(j);
+      if (__builtin_expect(raised, 0)) {
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float v = o[i][e] * alpha;
+            asm volatile("" : "+v"(v));                          // (one after the other, in place: else they are copied, and others spilled)
+            o[i][e] = v;
+          }
+        raised = false;
+      }
+      if constexpr (!kLate) wait_loads();
+      __syncthreads();
+    }
+    products(n_it, std::false_type());
+    if constexpr (kLate) wait_loads();                           // (what was asked for last is for nobody)
+  };
+  if (late) turns(std::true_type()); else turns(std::false_type());
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
   l += __shfl_xor(l, 32, 64);
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
