@@ -292,9 +292,9 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
     weigh();
   };
 
-  // The wavefronts of a SIMD, w and w + 4, take turns: while one multiplies, the other takes exponentials; so the later four are one
-  // turn behind.  Stage j + 1 is asked for in the turn in which the early ones multiply block j, over blocks that all have left, and
-  // waited for at the end of the next.
+  // Of the wavefronts of a SIMD, w and w + 4, one multiplies while the other takes exponentials: in a step the early four multiply and
+  // then weigh the new scores, the late four weigh those of the step before and then multiply.  Stage j + 1 is asked for at the
+  // beginning of step j, over blocks that all have left, and waited for at its end.
   pages(0);
   issue(0);
   {                                                              // (behind the way to the first keys, which is the longer one)
@@ -320,35 +320,31 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   if (threadIdx.x == 0) again = 0;
   wait_loads();
   __syncthreads();
+  auto rescale = [&]() __attribute__((always_inline)) {
+    if (__builtin_expect(raised, 0)) {
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float v = o[i][e] * alpha;
+          asm volatile("" : "+v"(v));                            // (one after the other, in place: else they are copied, and others spilled)
+          o[i][e] = v;
+        }
+      raised = false;
+    }
+  };
   auto turns = [&](auto second) __attribute__((always_inline)) {
     constexpr bool kLate = decltype(second)::value;
-    if constexpr (kLate) {
-      issue(1);
-      __syncthreads();
-    }
     for (int j = 0; j < n_it; ++j) {
-      if constexpr (!kLate) issue(j + 1);
+      issue(j + 1);
+      if (kLate && j > 0) { soften(j - 1); rescale(); }
       products(j, std::true_type());
-      if constexpr (kLate) wait_loads();
-      __syncthreads();
-      if constexpr (kLate) issue(j + 2);
-      soften(j);
-      if (__builtin_expect(raised, 0)) {
-#pragma unroll
-        for (int i = 0; i < HT; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float v = o[i][e] * alpha;
-            asm volatile("" : "+v"(v));                          // (one after the other, in place: else they are copied, and others spilled)
-            o[i][e] = v;
-          }
-        raised = false;
-      }
-      if constexpr (!kLate) wait_loads();
+      if constexpr (!kLate) { soften(j); rescale(); }
+      wait_loads();
       __syncthreads();
     }
+    if constexpr (kLate) { soften(n_it - 1); rescale(); }
     products(n_it, std::false_type());
-    if constexpr (kLate) wait_loads();                           // (what was asked for last is for nobody)
   };
   if (late) turns(std::true_type()); else turns(std::false_type());
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
@@ -363,7 +359,6 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       for (int e = 0; e < 16; ++e) odd = fmaf(o[i][e], 0.f, odd);
     if (__any(!(odd == 0.f) && l - l == 0.f)) again = 1;
   }
-  if (!late) __syncthreads();
   __syncthreads();
   if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) {
     constexpr int L = HD / 8;
