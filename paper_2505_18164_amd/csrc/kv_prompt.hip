@@ -10,55 +10,11 @@
 #include <cmath>
 #include <type_traits>
 
-#include "kv8_mfma.h"
-#include "kv_blocks.h"
-#include "kv_device.h"
+#include "kv_prompt_device.h"
 #include "once_per_device.h"
 
 namespace mdi {
 namespace {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
-typedef __attribute__((address_space(3))) u32x4* lds_u32x4;
-
-constexpr int BK = 64;               // keys of a step
-// Weights are counted from a reference of their row, the largest score of the first block that the row sees; it is raised only
-// when a block's weights sum to more than this: weights of any size keep their digits in bf16 and in the sums, which are divided
-// out at the end.  So no maximum is looked for where nothing is raised.
-constexpr float kMostSum = 0x1p16f;
-
-__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(uintptr_t)at));
-}
-__device__ __forceinline__ u32x4 read_lds(uint32_t at) { return *(lds_u32x4)(uintptr_t)at; }
-// 64 x 16 bytes global -> LDS: lane l's piece lands at lds + 16 l.
-__device__ __forceinline__ void dma(uint32_t lds, const void* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "m0", "memory");
-}
-__device__ __forceinline__ void dma(uint32_t lds, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "m0", "memory");
-}
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-// The blocks of 64 positions that some row of a workgroup sees, its first row at position `at`, `end` behind its last: those
-// of the first positions, then from the one that the first row's window begins in.
-struct KvBlocks { int sinks, n_sinks, first, from, end, n; };
-__device__ __forceinline__ KvBlocks kv_blocks(const KvSight& w, int at, int end) {
-  KvBlocks b;
-  b.end = end;
-  b.from = max(at + 1 - w.window, 0);
-  b.sinks = min(w.sinks, b.from);
-  const int s64 = (b.sinks + 63) >> 6, f64 = b.from >> 6;
-  b.n_sinks = s64 < f64 ? s64 : 0;
-  b.first = b.n_sinks || b.sinks == 0 ? f64 << 6 : 0;
-  b.n = b.n_sinks + ((end - b.first + 63) >> 6);
-  return b;
-}
-
-struct PromptGeo { int n_blocks, sets, g_sh, from; };            // bound of the blocks of all samples; sets of 2^g_sh query heads; of the launch's first workgroup
 
 // A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
 // kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.  kMany: of more than kInOrder samples.
@@ -86,16 +42,8 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   const int col = lane & 31, half = lane >> 5;
   const int row = q0 + ((32 * wave + col) >> g_sh), head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
   const bool live = row < at.rows;
-  const int item = (at.first + row) * a.H + head;
-  bf16_t* out = (bf16_t*)a.out + (long)(at.first + row) * a.out_stride + (long)head * HD;
   if (p0 < 0 || which < 0) {                                     // takes no part
-    if (blockIdx.y == 0 && grp == 0 && live) {
-#pragma unroll
-      for (int i = 0; i < HT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) *reinterpret_cast<u32x2*>(out + 32 * i + 8 * g + 4 * half) = u32x2{0, 0};
-      if (a.plan.splits > 1 && half == 0) kv_part_counts(a, c, r)[item] = 1;
-    }
+    if (blockIdx.y == 0 && grp == 0 && live) prompt_zeros<HT>(c, r, a, at, row, head);
     return;
   }
   // positions up to `pos` are seen by this lane's row; the block's rows end before `far`
@@ -105,6 +53,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   const KvBlocks kb = kv_blocks(a.sight, (int)min((long)p0 + q0, (long)r.max_ctx - 1), (int)min(far, (long)r.max_ctx));
   const int b_lo = blockIdx.y * a.plan.chunk, b_hi = (int)min((long)kb.n, (long)b_lo + a.plan.chunk), pieces = (kb.n + a.plan.chunk - 1) / a.plan.chunk;
   if (b_lo >= b_hi) return;
+  const PromptRows mine{at, g_sh, head0, kv, q0, p0, table, kb, (int)blockIdx.y, b_lo, b_hi, pieces};
 
   bf16x8 qf[HD / 16];
   f32x16 o[HT];
@@ -361,28 +310,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   }
   __syncthreads();
   if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) {
-    constexpr int L = HD / 8;
-    const int ch = 8 * (lane & (L - 1));
-    for (int i = threadIdx.x >> 6; i < BQ; i += 8) {             // a wavefront takes a row and head
-      const int row1 = q0 + (i >> g_sh), head1 = head0 + (i & ((1 << g_sh) - 1)), item1 = (at.first + row1) * a.H + head1;
-      if (row1 >= at.rows) continue;
-      const int end1 = (int)min((long)p0 + row1 + 1, (long)r.max_ctx), from1 = max(end1 - a.sight.window, 0), shift = kb.first - 64 * kb.n_sinks;
-      const KvSpan span{min(a.sight.sinks, from1), 64 * kb.n_sinks, shift, from1, end1};
-      float q[8];
-      KvType<bf16_t>::load8((const bf16_t*)a.q + (long)(at.first + row1) * a.q_stride + (long)head1 * HD + ch, q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) q[e] *= a.scale;
-      const KvSums sums = kv_attend<bf16_t>(c, table, kv, span, q, L, ch, true, 64 * b_lo, 64 / L, min(64 * b_hi, end1 - shift));
-      if (lane >= L) continue;
-      bf16_t* const out1 = (bf16_t*)a.out + (long)(at.first + row1) * a.out_stride + (long)head1 * HD + ch;
-      float* const part = kv_part_sums(a, c, item1, blockIdx.y) + ch;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (pieces == 1) out1[e] = f32_to_bf16(sums.o[e] / sums.l);
-        else part[e] = sums.o[e];
-      if (lane == 0 && pieces > 1) *kv_part_marks(a, c, r, item1, blockIdx.y) = make_float2(sums.m, sums.l);
-      if (lane == 0 && blockIdx.y == 0 && a.plan.splits > 1) kv_part_counts(a, c, r)[item1] = pieces;
-    }
+    prompt_again<HD>(c, r, a, mine, BQ, 8);
     return;
   }
 
@@ -408,27 +336,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * a0 + fold[(i * 16 + e) * GT + tid] * a1;
   }
 
-  if (!live) return;
-  if (a.plan.splits > 1 && blockIdx.y == 0 && half == 0) kv_part_counts(a, c, r)[item] = pieces;
-  if (pieces == 1) {
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int i = 0; i < HT; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const uint32_t w0 = (uint32_t)f32_to_bf16(o[i][4 * g] * inv) | ((uint32_t)f32_to_bf16(o[i][4 * g + 1] * inv) << 16);
-        const uint32_t w1 = (uint32_t)f32_to_bf16(o[i][4 * g + 2] * inv) | ((uint32_t)f32_to_bf16(o[i][4 * g + 3] * inv) << 16);
-        *reinterpret_cast<u32x2*>(out + 32 * i + 8 * g + 4 * half) = u32x2{w0, w1};
-      }
-  } else {
-    float* part = kv_part_sums(a, c, item, blockIdx.y);
-#pragma unroll
-    for (int i = 0; i < HT; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(part + 32 * i + 8 * g + 4 * half) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
-    if (half == 0) *kv_part_marks(a, c, r, item, blockIdx.y) = make_float2(m, l);
-  }
+  if (live) prompt_store<HT>(c, r, a, mine, row, head, o, m, l);
 }
 
 template <int HD, int NG>
@@ -480,6 +388,11 @@ template <int HD, int NG, bool kWhole>
 void launch_pages(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   PromptGeo g = geo_of(c, r, a.H, 8 / NG);
   const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
+  if (a.plan.wide) {
+    if (r.n <= kInOrder) launch_kv_wide(s, c, r, a, g, total, false);
+    else for (; g.from < total; g.from += kMostWgs) launch_kv_wide(s, c, r, a, g, std::min(kMostWgs, total - g.from), true);
+    return;
+  }
   if (r.n <= kInOrder) {
     hipLaunchKernelGGL((k_kv_prompt<HD, NG, kWhole, false>), dim3(total, a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
     return;
@@ -502,7 +415,7 @@ bool kv_prompt_supported(const KvCache& c, const KvRows& r) { return r.start && 
 bool kv_allow_lds() {
   static OncePerDevice done;
   int dev = -1;
-  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_groups<64, 1>() && allow_groups<64, 2>() && allow_groups<128, 1>() && allow_groups<128, 2>(); });
+  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_groups<64, 1>() && allow_groups<64, 2>() && allow_groups<128, 1>() && allow_groups<128, 2>() && kv_wide_allow_lds(); });
 }
 
 KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
@@ -511,7 +424,7 @@ KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w
   const int bp = 256 / p.groups >> kv_heads_shift(c, H);
   const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
   const int chunk = (int)((most + p.splits - 1) / p.splits);
-  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
+  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups, c.h == 128};
 }
 
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

@@ -1,0 +1,413 @@
+// Attention of packed rows over the bf16 cache, heads of 128: 64 rows of (position, query head) a wavefront, one wavefront a SIMD.
+//
+// The products of kv_prompt.hip read an operand of every matrix instruction from the LDS, 1 KiB in 32 cycles for each of the four SIMDs of
+// a compute unit: all that its LDS delivers.  Here an operand serves two of them, for the wavefront's two sets of 32 rows.  What a
+// second wavefront on the SIMD did, exponentials while the first multiplies, the wavefront does itself: in step i, of 32
+// keys, it multiplies the keys of step i + 1 and the values of step i - 1 and in between weighs the scores of step i, three vector
+// instructions behind every matrix instruction.  Everything of a step is in registers (the operands of the next are read
+// meanwhile), some 400 of them.
+#include <type_traits>
+
+#include "kv_prompt_device.h"
+#include "kv_prompt_wide.h"
+
+namespace mdi {
+namespace {
+
+constexpr float kFarSum = 0x1p30f;
+
+// A workgroup is four wavefronts: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
+template <int HD, int NG, bool kWhole, bool kMany>
+__global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
+  constexpr int WQ = 4 / NG, BQ = 64 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
+  constexpr int HT = HD / 32, KS = HD / 16, RB = 2 * HD, UN = HD / 8;   // bytes and 16-byte units of a key
+  constexpr int BB = BK * RB;                                    // bytes of a block of keys, or of values
+  constexpr int KP = 64 / UN, NI = BK / KP / WQ;                 // keys of an instruction that loads, instructions of a wavefront
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+
+  const int tid = threadIdx.x & (GT - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = NG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GT);
+  const uint32_t Kb = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + grp * 5 * BB, Vb = Kb + 2 * BB;   // two blocks of keys, three of values
+  const int x = kMany ? geo.from + blockIdx.x : blockIdx.x, block = x / geo.sets, set = x - block * geo.sets;   // (as in kv_prompt.hip)
+  const BlockPlace at = place_of<kMany>(r, block, BQ >> geo.g_sh);
+  if (at.sample < 0) return;
+  const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
+  const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
+  const int which = kv8_checked_row(c, at.table), p0 = at.pos;
+  const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
+  const int col = lane & 31, half = lane >> 5, head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
+  int row[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) row[u] = q0 + ((64 * wave + 32 * u + col) >> g_sh);
+  if (p0 < 0 || which < 0) {                                     // takes no part
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (blockIdx.y == 0 && grp == 0 && row[u] < at.rows) prompt_zeros<HT>(c, r, a, at, row[u], head);
+    return;
+  }
+  const long far = (long)p0 + min(q0 + bp, at.rows);             // behind the workgroup's last position
+  if (far > r.max_ctx) kv8_report(c);
+  const int cap = r.max_ctx - 1;
+  auto pos_of = [&](int row1) __attribute__((always_inline)) { return (int)min((long)p0 + min(row1, at.rows - 1), (long)cap); };
+  const KvBlocks kb = kv_blocks(a.sight, pos_of(q0), (int)min(far, (long)r.max_ctx));
+  const int b_lo = blockIdx.y * a.plan.chunk, b_hi = (int)min((long)kb.n, (long)b_lo + a.plan.chunk), pieces = (kb.n + a.plan.chunk - 1) / a.plan.chunk;
+  if (b_lo >= b_hi) return;
+  const PromptRows mine{at, g_sh, head0, kv, q0, p0, table, kb, (int)blockIdx.y, b_lo, b_hi, pieces};
+
+  f32x16 o[2][HT];
+  float m[2], l[2];
+  int pos[2];                                                    // a lane's rows see positions up to these
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    pos[u] = pos_of(row[u]);
+    m[u] = kKvNone;
+  }
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);
+  const int wave_pos = pos_of(q0 + ((64 * wave) >> g_sh)), last_pos = pos_of(q0 + ((64 * wave + 63) >> g_sh));   // of the wavefront's first and last rows
+
+  // Loading, as in kv_prompt.hip: stage j is the keys of block j and the values of block j - 1.
+  const int n_it = (b_hi - b_lo + NG - 1) / NG;
+  auto block_of = [&](int j) __attribute__((always_inline)) { return min(b_lo + NG * j + grp, b_hi - 1); };
+  auto start_of = [&](int b) __attribute__((always_inline)) { return b < kb.n_sinks ? b << 6 : kb.first + ((b - kb.n_sinks) << 6); };
+  auto visible = [&](int p, int k0) __attribute__((always_inline)) {
+    return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
+  };
+  auto key_of = [&](int n) __attribute__((always_inline)) { return (wave * NI + n) * KP + lane / UN; };
+  auto unit_of = [&](int key) __attribute__((always_inline)) {
+    return (lane % UN) ^ ((HD == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2) | ((key >> 2) & 3));
+  };
+  unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
+  auto checked = [&](int page) __attribute__((always_inline)) {
+    worst = max(worst, (unsigned)page);
+    return min((unsigned)page, (unsigned)c.n_pages - 1);
+  };
+  int pg[kWhole ? 1 : NI];
+  uint32_t at_off[NI];                                           // of a block whose positions are all seen by some row
+#pragma unroll
+  for (int n = 0; n < NI; ++n) at_off[n] = (uint32_t)(key_of(n) * RB + 16 * unit_of(key_of(n)));
+  const char *k_at[kWhole ? 1 : NI] = {}, *v_at[kWhole ? 1 : NI] = {};   // the stage's keys; its values
+  uint32_t k_off[kWhole ? NI : 1], v_off[kWhole ? NI : 1];
+  const long v_by = (long)c.pt * RB;                             // from a key to its value
+  auto pages = [&](int j) __attribute__((always_inline)) {
+    const int k0 = start_of(block_of(j));
+    if constexpr (kWhole) {
+      int p = kv8_page_of(c, k0);
+      asm volatile("" : "+v"(p));                                // a vector load: behind a scalar one every read of LDS would have to wait for it
+      pg[0] = table[p];
+    } else {
+#pragma unroll
+      for (int n = 0; n < NI; ++n) pg[n] = table[kv8_page_of(c, visible(k0 + key_of(n), k0))];
+    }
+  };
+  // Where stage j is: its keys' addresses from the page numbers that were asked for a stage before, its values' from the keys of
+  // that.  (The page numbers are looked at before anything else is asked for: whoever waits for them waits for that, too.)
+  auto find = [&](int j) __attribute__((always_inline)) {
+    const int k0 = start_of(block_of(j));
+    if constexpr (kWhole) {
+      unsigned page = __builtin_amdgcn_readfirstlane((int)checked(pg[0]));
+      asm volatile("" : "+s"(page));
+      v_at[0] = k_at[0] + v_by;
+      const int in_page = k0 - kv8_page_of(c, k0) * c.pt;
+      k_at[0] = (const char*)c.data + ((long)((uint64_t)page * (unsigned)(2 * c.K * c.pt)) + 2 * kv * c.pt + in_page) * RB;
+      const int k1 = start_of(block_of(max(j - 1, 0)));
+#pragma unroll
+      for (int n = 0; n < NI; ++n) { k_off[n] = at_off[n]; v_off[n] = at_off[n]; }
+      auto inside = [&](int k) __attribute__((always_inline)) { return (k >= kb.from && k + BK <= kb.end) || k + BK <= kb.sinks; };
+      if (__builtin_expect(!inside(k0) || !inside(k1), 0))
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+          const int key = key_of(n);
+          k_off[n] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key));
+          v_off[n] = (uint32_t)((visible(k1 + key, k1) - k1) * RB + 16 * unit_of(key));
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        const int key = key_of(n);
+        v_at[n] = k_at[n] + v_by;
+        k_at[n] = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key);
+        asm volatile("" : "+v"(k_at[n]));
+      }
+    }
+    pages(j + 1);
+  };
+  auto ask_keys = [&](uint32_t lds, int n) __attribute__((always_inline)) {   // lds: the wavefront's part of the block
+    if constexpr (kWhole) dma(lds + 1024 * n, k_at[0], k_off[n]); else dma(lds + 1024 * n, k_at[n]);
+  };
+  auto ask_values = [&](uint32_t lds, int n) __attribute__((always_inline)) {
+    if constexpr (kWhole) dma(lds + 1024 * n, v_at[0], v_off[n]); else dma(lds + 1024 * n, v_at[n]);
+  };
+  const uint32_t w_lds = wave * NI * 1024;
+
+  const int kk = (lane & 15) >> 2;                               // what this lane reads: as in kv_prompt.hip
+  const uint32_t k_lane = col * RB + 16 * (half ^ ((HD == 128 ? (col & 3) << 2 : ((col >> 1) & 1) << 2) | ((col >> 2) & 3)));
+  const uint32_t v_lane = (4 * half + kk) * RB + 64 * (HD == 128 ? kk : kk >> 1) + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
+  u32x4 kf[KS], vf[2][HT];                                       // operands: keys of a step; values of its first and second 16 keys
+  bf16x8 qf[2][KS];
+  auto read_key = [&](uint32_t K, int ks) __attribute__((always_inline)) { kf[ks] = read_lds(K ^ (32 * ks)); };
+  auto read_value = [&](uint32_t V, int pp, int n) __attribute__((always_inline)) {   // n: channel block and half of the operand
+    const uint32_t p = V ^ (64 * (n >> 1));
+    const u32x2 w = read_transposed(n & 1 ? (p ^ 32) + 8 * RB : p);
+    vf[pp][n >> 1][2 * (n & 1)] = w.x;
+    vf[pp][n >> 1][2 * (n & 1) + 1] = w.y;
+  };
+
+  // A row's reference is the largest score of the first keys that it sees.  Where later ones would have weights of more than
+  // kFarSum the reference is raised, but not the sums so far: then all is done once more, from the references that the first time
+  // ended with, which nothing exceeds.  (A rescaling would have the sums in registers that vector instructions reach, and copied
+  // there and back around every step.)
+  bool once_more = false;
+  // Step i = 2 j + t: scores sn of step i + 1 (operands there), weights pn of step i from its scores sc, and the values of step i - 1
+  // times its weights pc.  K: where the keys of step i + 2 are; V1: the second 16 values of step i - 1; V0: the first 16 of step i.
+  // ask(n): what is asked for behind matrix instruction n.
+  auto step = [&](int k0, float (&sc)[2][16], float (&sn)[2][16], u32x4 (&pc)[2][2], u32x4 (&pn)[2][2], uint32_t K, uint32_t V1, uint32_t V0, auto&& ask) __attribute__((always_inline)) {
+    if (k0 + 31 > wave_pos || (k0 <= last_pos - a.sight.window && k0 + 32 > a.sight.sinks) || k0 < 0) {   // some of these keys are not for some of the rows
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int up_to = k0 < 0 ? -1 : pos[u] - k0 - 4 * half, from = up_to - a.sight.window, stay = a.sight.sinks - k0 - 4 * half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 8 * (e >> 2) + (e & 3);
+          sc[u][e] = key <= up_to && (key > from || key < stay) ? sc[u][e] : -INFINITY;
+        }
+      }
+    }
+    f32x16 acc[2];
+    float sum[2] = {0.f, 0.f}, next = fmaf(sc[0][0], scale, -m[0]), w0 = 0.f, w1 = 0.f;
+    auto pack = [&](int n) __attribute__((always_inline)) {      // weights n - 2 and n - 1
+      const int u = (n - 2) >> 4, e = (n - 2) & 15;
+      const bf16x2 w = {(__bf16)w0, (__bf16)w1};
+      sum[u] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[u], false);
+      pn[u][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < 32; ++n) {
+      if (n < 2 * KS) {
+        const int ks = n >> 1, u = n & 1;
+        acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[ks]), qf[u][ks], ks ? acc[u] : f32x16{}, 0, 0, 0);
+      } else {
+        const int q = n - 2 * KS, pp = q / (2 * HT), h = (q >> 1) % HT, u = q & 1;
+        o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[pp][h]), __builtin_bit_cast(bf16x8, pc[u][pp]), o[u][h], 0, 0, 0);
+      }
+      if (n < 2 * HT) read_value(V1, 1, n);
+      else if (n >= 4 * HT && n < 4 * HT + KS) read_key(K, n - 4 * HT);
+      else if (n >= 6 * HT) read_value(V0, 0, n - 6 * HT);
+      ask(n);
+      if (n >= 2 && (n & 1) == 0) pack(n);
+      const float w = exp2_raw(next);
+      if (n & 1) w1 = w; else w0 = w;
+      if (n < 31) next = fmaf(sc[(n + 1) >> 4][(n + 1) & 15], scale, -m[(n + 1) >> 4]);
+      // (the matrix instructions leave the scores in accumulation registers: out of them a few at a time)
+      if (n >= 17)
+#pragma unroll
+        for (int i = (n - 17) * 32 / 15; i < (n - 16) * 32 / 15; ++i) {
+          float v = acc[i >> 4][i & 15];
+          asm volatile("" : "+v"(v));
+          sn[i >> 4][i & 15] = v;
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    pack(32);
+    if (__builtin_expect(__any(!(sum[0] < kFarSum) || !(sum[1] < kFarSum)), 0)) {   // (the first keys that a row sees, too)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[u][e]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;       // both lanes of a row raise alike
+        const float to = fmaxf(m[u], top);
+        once_more |= to > m[u] && m[u] != kKvNone;
+        m[u] = to;
+        sum[u] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const bf16x2 w = {(__bf16)exp2_raw(fmaf(sc[u][e], scale, -to)), (__bf16)exp2_raw(fmaf(sc[u][e + 1], scale, -to))};
+          sum[u] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[u], false);
+          pn[u][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+        }
+      }
+    }
+    l[0] += sum[0];
+    l[1] += sum[1];
+  };
+
+  {
+    // (scores are multiplied by a positive number: a masked one is -inf before that)
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : ~0u;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16_t* qp = (const bf16_t*)a.q + (long)(at.first + min(row[u], at.rows - 1)) * a.q_stride + (long)head * HD + 8 * half;
+      u32x4 w[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) w[ks] = *reinterpret_cast<const u32x4*>(qp + 16 * ks);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t y = (w[ks][i] ^ flip) & keep;
+          asm volatile("" : "+v"(y));                            // (looked at here: else the loop waits for them, and for all that it has asked for)
+          w[ks][i] = y;
+        }
+        qf[u][ks] = __builtin_bit_cast(bf16x8, w[ks]);
+      }
+    }
+  }
+  int again;                                                     // 1: once more with other references; 2: a value that is not finite
+  do {
+  pages(0);
+  find(0);
+#pragma unroll
+  for (int n = 0; n < NI; ++n) ask_keys(Kb + w_lds, n);
+  // (the first step has no values yet: its weights are zeros, and so is what they multiply)
+  for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + 2 * BB + 16 * i) = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int h = 0; h < HT; ++h) vf[0][h] = u32x4{0, 0, 0, 0};
+  wait_loads();
+  find(1);
+#pragma unroll
+  for (int n = 0; n < NI; ++n) { ask_values(Vb + w_lds, n); ask_keys(Kb + BB + w_lds, n); }
+  wait_loads();
+  __syncthreads();
+
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    l[u] = 0.f;
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[u][i][e] = 0.f;
+  }
+  float s0[2][16], s1[2][16];
+  u32x4 w0[2][2] = {}, w1[2][2] = {};
+  // scores of step 0, and the keys of step 1
+  {
+    f32x16 acc[2];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane, ks);
+#pragma unroll
+    for (int n = 0; n < 2 * KS; ++n)
+      acc[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[n >> 1]), qf[n & 1][n >> 1], n > 1 ? acc[n & 1] : f32x16{}, 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < 32; ++n) {
+      float v = acc[n >> 4][n & 15];
+      asm volatile("" : "+v"(v));
+      s0[n >> 4][n & 15] = v;
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane + 32 * RB, ks);
+  }
+  __syncthreads();                                               // (the first step loads over these)
+
+  uint32_t v_before = Vb + 2 * BB, v_now = Vb;
+  for (int j = 0; j < n_it; ++j) {
+    find(j + 2);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[u][ks]));   // (in the accumulation registers: the others are needed for what is not only multiplied)
+    const bool mine_too = b_lo + NG * j + grp < b_hi;            // (a group's last step may have no block)
+    const int k0 = mine_too ? start_of(block_of(j)) : -(1 << 30);
+    const uint32_t K = Kb + ((j + 1) & 1) * BB + k_lane, v_next = v_now == Vb + 2 * BB ? Vb : v_now + BB, k_lds = Kb + (j & 1) * BB + w_lds;
+    step(k0, s0, s1, w1, w0, K, v_before + v_lane + 48 * RB, v_now + v_lane, [&](int n) __attribute__((always_inline)) {
+      constexpr int kEvery = 24 / (2 * NI);
+      if (n % kEvery == 0 && n / kEvery < 2 * NI) { if (n / kEvery & 1) ask_keys(k_lds, n / kEvery / 2); else ask_values(v_next + w_lds, n / kEvery / 2); }
+    });
+    step(k0 + (mine_too ? 32 : 0), s1, s0, w0, w1, K + 32 * RB, v_now + v_lane + 16 * RB, v_now + v_lane + 32 * RB, [](int) {});
+    v_before = v_now;
+    v_now = v_next;
+    wait_loads();
+    __syncthreads();
+  }
+  // the values of the last step
+#pragma unroll
+  for (int n = 0; n < 2 * HT; ++n) read_value(v_before + v_lane + 48 * RB, 1, n);
+#pragma unroll
+  for (int n = 0; n < 4 * HT; ++n) {
+    const int pp = n / (2 * HT), h = (n >> 1) % HT, u = n & 1;
+    o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[pp][h]), __builtin_bit_cast(bf16x8, w1[u][pp]), o[u][h], 0, 0, 0);
+  }
+  __syncthreads();
+  // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
+  // are computed once more, each by itself.  (Weights that are no numbers are what they should be.)
+  int* const flag = (int*)smem;
+  if (threadIdx.x == 0) *flag = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    l[u] += __shfl_xor(l[u], 32, 64);
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) odd = fmaf(o[u][i][e], 0.f, odd);
+    if (__any(!(odd == 0.f) && l[u] - l[u] == 0.f)) atomicOr(flag, 2);
+  }
+  if (__any(once_more)) atomicOr(flag, 1);
+  once_more = false;
+  __syncthreads();
+  again = __builtin_amdgcn_readfirstlane(*flag);
+  __syncthreads();
+  } while (__builtin_expect(again & 1, 0));
+  if (worst >= (unsigned)c.n_pages) kv8_report(c);
+  if (__builtin_expect(again, 0)) {
+    prompt_again<HD>(c, r, a, mine, BQ, 4);
+    return;
+  }
+  if constexpr (NG > 1) {
+    __syncthreads();
+    float* fold = (float*)smem;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                                // (element j of thread t at [j][t])
+      if (grp > 0) {
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) fold[(u * (HT * 16 + 2) + i * 16 + e) * GT + tid] = o[u][i][e];
+        fold[(u * (HT * 16 + 2) + HT * 16) * GT + tid] = m[u];
+        fold[(u * (HT * 16 + 2) + HT * 16 + 1) * GT + tid] = l[u];
+      }
+    }
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float* f = fold + u * (HT * 16 + 2) * GT + tid;
+      const float m1 = f[HT * 16 * GT], l1 = f[(HT * 16 + 1) * GT], to = fmaxf(m[u], m1), a0 = exp2_raw(m[u] - to), a1 = exp2_raw(m1 - to);
+      l[u] = l[u] * a0 + l1 * a1;
+      m[u] = to;
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[u][i][e] = o[u][i][e] * a0 + f[(i * 16 + e) * GT] * a1;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (row[u] < at.rows) prompt_store<HT>(c, r, a, mine, row[u], head, o[u], m[u], l[u]);
+}
+
+template <int NG> constexpr size_t wide_lds() { return (size_t)NG * 5 * BK * 256; }
+template <int NG, bool kWhole, bool kMany>
+bool allow_one() {                                               // 64 KiB is what a kernel gets by default
+  return hipFuncSetAttribute((const void*)k_kv_prompt_wide<128, NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds<NG>()) == hipSuccess;
+}
+template <int NG, bool kWhole>
+void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs, bool many) {
+  if (many) hipLaunchKernelGGL((k_kv_prompt_wide<128, NG, kWhole, true>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
+  else hipLaunchKernelGGL((k_kv_prompt_wide<128, NG, kWhole, false>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
+}
+
+}  // namespace
+
+bool kv_wide_allow_lds() {
+  return allow_one<1, true, false>() && allow_one<1, false, false>() && allow_one<1, true, true>() && allow_one<1, false, true>() &&
+         allow_one<2, true, false>() && allow_one<2, false, false>() && allow_one<2, true, true>() && allow_one<2, false, true>();
+}
+void launch_kv_wide(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs, bool many) {
+  const bool whole = c.pt % BK == 0;
+  if (a.plan.groups == 1) { if (whole) launch<1, true>(s, c, r, a, g, wgs, many); else launch<1, false>(s, c, r, a, g, wgs, many); }
+  else { if (whole) launch<2, true>(s, c, r, a, g, wgs, many); else launch<2, false>(s, c, r, a, g, wgs, many); }
+}
+
+}  // namespace mdi
