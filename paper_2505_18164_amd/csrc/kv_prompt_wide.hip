@@ -16,6 +16,18 @@ namespace {
 
 constexpr float kFarSum = 0x1p30f;
 
+// Four times 64 x 16 bytes global -> LDS, the places 1024 bytes apart: an instruction's offset counts for both addresses.
+__device__ __forceinline__ void dma4(uint32_t lds, const char* base, const uint32_t* off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+               "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+               ::"s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void dma4(uint32_t lds, const char* const* p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:1024\n\t"
+               "global_load_lds_dwordx4 %3, off offset:2048\n\tglobal_load_lds_dwordx4 %4, off offset:3072"
+               ::"s"(lds), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]) : "m0", "memory");
+}
+
 // A workgroup is four wavefronts: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
 template <int HD, int NG, bool kWhole, bool kMany>
 __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
@@ -66,9 +78,13 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   const int wave_pos = pos_of(q0 + ((64 * wave) >> g_sh)), last_pos = pos_of(q0 + ((64 * wave + 63) >> g_sh));   // of the wavefront's first and last rows
 
   // Loading, as in kv_prompt.hip: stage j is the keys of block j and the values of block j - 1.
-  const int n_it = (b_hi - b_lo + NG - 1) / NG;
+  const int n_it = (b_hi - b_lo + NG - 1) / NG, gap = kb.first - (kb.n_sinks << 6);
   auto block_of = [&](int j) __attribute__((always_inline)) { return min(b_lo + NG * j + grp, b_hi - 1); };
-  auto start_of = [&](int b) __attribute__((always_inline)) { return b < kb.n_sinks ? b << 6 : kb.first + ((b - kb.n_sinks) << 6); };
+  auto start_of = [&](int b) __attribute__((always_inline)) { return (b << 6) + (b < kb.n_sinks ? 0 : gap); };
+  // Blocks whose positions are all seen by some row of the workgroup, and by all rows of the wavefront (of those behind the first positions).
+  auto first_from = [&](int pos) __attribute__((always_inline)) { return max(kb.n_sinks, (pos - gap + 63) >> 6); };   // that starts at or behind pos
+  const int in_lo = first_from(kb.from), in_hi = (kb.end - gap) >> 6;
+  const int all_lo = first_from(max(last_pos - a.sight.window + 1, 0)), all_hi = (wave_pos + 1 - gap) >> 6;
   auto visible = [&](int p, int k0) __attribute__((always_inline)) {
     return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
   };
@@ -76,19 +92,23 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   auto unit_of = [&](int key) __attribute__((always_inline)) {
     return (lane % UN) ^ ((HD == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2) | ((key >> 2) & 3));
   };
+  auto by_of = [](int n) __attribute__((always_inline)) { return 4096 - 1024 * (n & 3); };   // (dma4 adds what is missing)
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
   auto checked = [&](int page) __attribute__((always_inline)) {
     worst = max(worst, (unsigned)page);
     return min((unsigned)page, (unsigned)c.n_pages - 1);
   };
-  int pg[kWhole ? 1 : NI];
+  constexpr int kPages = kWhole ? 1 : NI;
+  int pg[kPages];
   uint32_t at_off[NI];                                           // of a block whose positions are all seen by some row
 #pragma unroll
-  for (int n = 0; n < NI; ++n) at_off[n] = (uint32_t)(key_of(n) * RB + 16 * unit_of(key_of(n)));
+  for (int n = 0; n < NI; ++n) at_off[n] = (uint32_t)(key_of(n) * RB + 16 * unit_of(key_of(n)) + by_of(n));
   const char *k_at[kWhole ? 1 : NI] = {}, *v_at[kWhole ? 1 : NI] = {};   // the stage's keys; its values
   uint32_t k_off[kWhole ? NI : 1], v_off[kWhole ? NI : 1];
   const long v_by = (long)c.pt * RB;                             // from a key to its value
-  auto pages = [&](int j) __attribute__((always_inline)) {
+  const char* const heads_at = (const char*)c.data + 2 * kv * v_by;
+  const uint64_t page_bytes = 2ull * c.K * v_by;
+  auto pages = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
     const int k0 = start_of(block_of(j));
     if constexpr (kWhole) {
       int p = kv8_page_of(c, k0);
@@ -101,41 +121,40 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   };
   // Where stage j is: its keys' addresses from the page numbers that were asked for a stage before, its values' from the keys of
   // that.  (The page numbers are looked at before anything else is asked for: whoever waits for them waits for that, too.)
-  auto find = [&](int j) __attribute__((always_inline)) {
+  auto find = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
     const int k0 = start_of(block_of(j));
     if constexpr (kWhole) {
       unsigned page = __builtin_amdgcn_readfirstlane((int)checked(pg[0]));
       asm volatile("" : "+s"(page));
       v_at[0] = k_at[0] + v_by;
-      const int in_page = k0 - kv8_page_of(c, k0) * c.pt;
-      k_at[0] = (const char*)c.data + ((long)((uint64_t)page * (unsigned)(2 * c.K * c.pt)) + 2 * kv * c.pt + in_page) * RB;
-      const int k1 = start_of(block_of(max(j - 1, 0)));
+      k_at[0] = heads_at + ((uint64_t)page * page_bytes + (unsigned)((k0 - kv8_page_of(c, k0) * c.pt) * RB));
 #pragma unroll
       for (int n = 0; n < NI; ++n) { k_off[n] = at_off[n]; v_off[n] = at_off[n]; }
-      auto inside = [&](int k) __attribute__((always_inline)) { return (k >= kb.from && k + BK <= kb.end) || k + BK <= kb.sinks; };
-      if (__builtin_expect(!inside(k0) || !inside(k1), 0))
+      const int b0 = block_of(j), b1 = block_of(max(j - 1, 0));
+      if (__builtin_expect(b1 < in_lo || b0 >= in_hi, 0)) {
+        const int k1 = start_of(b1);
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
           const int key = key_of(n);
-          k_off[n] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key));
-          v_off[n] = (uint32_t)((visible(k1 + key, k1) - k1) * RB + 16 * unit_of(key));
+          k_off[n] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key) + by_of(n));
+          v_off[n] = (uint32_t)((visible(k1 + key, k1) - k1) * RB + 16 * unit_of(key) + by_of(n));
         }
+      }
     } else {
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
         const int key = key_of(n);
         v_at[n] = k_at[n] + v_by;
-        k_at[n] = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key);
+        k_at[n] = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key) + by_of(n) - 4096;
         asm volatile("" : "+v"(k_at[n]));
       }
     }
-    pages(j + 1);
   };
-  auto ask_keys = [&](uint32_t lds, int n) __attribute__((always_inline)) {   // lds: the wavefront's part of the block
-    if constexpr (kWhole) dma(lds + 1024 * n, k_at[0], k_off[n]); else dma(lds + 1024 * n, k_at[n]);
+  auto ask_keys = [&](uint32_t lds, int n) __attribute__((always_inline)) {   // instructions 4 n .. + 3; lds: the wavefront's part of the block
+    if constexpr (kWhole) dma4(lds + 4096 * n, k_at[0] - 4096, &k_off[4 * n]); else dma4(lds + 4096 * n, &k_at[4 * n]);
   };
   auto ask_values = [&](uint32_t lds, int n) __attribute__((always_inline)) {
-    if constexpr (kWhole) dma(lds + 1024 * n, v_at[0], v_off[n]); else dma(lds + 1024 * n, v_at[n]);
+    if constexpr (kWhole) dma4(lds + 4096 * n, v_at[0] - 4096, &v_off[4 * n]); else dma4(lds + 4096 * n, &v_at[4 * n]);
   };
   const uint32_t w_lds = wave * NI * 1024;
 
@@ -160,8 +179,8 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   // Step i = 2 j + t: scores sn of step i + 1 (operands there), weights pn of step i from its scores sc, and the values of step i - 1
   // times its weights pc.  K: where the keys of step i + 2 are; V1: the second 16 values of step i - 1; V0: the first 16 of step i.
   // ask(n): what is asked for behind matrix instruction n.
-  auto step = [&](int k0, float (&sc)[2][16], float (&sn)[2][16], u32x4 (&pc)[2][2], u32x4 (&pn)[2][2], uint32_t K, uint32_t V1, uint32_t V0, auto&& ask) __attribute__((always_inline)) {
-    if (k0 + 31 > wave_pos || (k0 <= last_pos - a.sight.window && k0 + 32 > a.sight.sinks) || k0 < 0) {   // some of these keys are not for some of the rows
+  auto step = [&](bool whole, int k0, f32x16 (&sc)[2], f32x16 (&sn)[2], u32x4 (&pc)[2][2], u32x4 (&pn)[2][2], uint32_t K, uint32_t V1, uint32_t V0, auto&& ask) __attribute__((always_inline)) {
+    if (!whole) {                                                // some of these keys are not for some of the rows
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int up_to = k0 < 0 ? -1 : pos[u] - k0 - 4 * half, from = up_to - a.sight.window, stay = a.sight.sinks - k0 - 4 * half;
@@ -172,7 +191,6 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
         }
       }
     }
-    f32x16 acc[2];
     float sum[2] = {0.f, 0.f}, next = fmaf(sc[0][0], scale, -m[0]), w0 = 0.f, w1 = 0.f;
     auto pack = [&](int n) __attribute__((always_inline)) {      // weights n - 2 and n - 1
       const int u = (n - 2) >> 4, e = (n - 2) & 15;
@@ -185,9 +203,11 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
     for (int n = 0; n < 32; ++n) {
       if (n < 2 * KS) {
         const int ks = n >> 1, u = n & 1;
-        acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[ks]), qf[u][ks], ks ? acc[u] : f32x16{}, 0, 0, 0);
+        if (u == 0) asm volatile("" : "+a"(kf[ks]));
+        sn[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[ks]), qf[u][ks], ks ? sn[u] : f32x16{}, 0, 0, 0);
       } else {
         const int q = n - 2 * KS, pp = q / (2 * HT), h = (q >> 1) % HT, u = q & 1;
+        if (u == 0) asm volatile("" : "+a"(vf[pp][h]));
         o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[pp][h]), __builtin_bit_cast(bf16x8, pc[u][pp]), o[u][h], 0, 0, 0);
       }
       if (n < 2 * HT) read_value(V1, 1, n);
@@ -198,14 +218,6 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
       const float w = exp2_raw(next);
       if (n & 1) w1 = w; else w0 = w;
       if (n < 31) next = fmaf(sc[(n + 1) >> 4][(n + 1) & 15], scale, -m[(n + 1) >> 4]);
-      // (the matrix instructions leave the scores in accumulation registers: out of them a few at a time)
-      if (n >= 17)
-#pragma unroll
-        for (int i = (n - 17) * 32 / 15; i < (n - 16) * 32 / 15; ++i) {
-          float v = acc[i >> 4][i & 15];
-          asm volatile("" : "+v"(v));
-          sn[i >> 4][i & 15] = v;
-        }
       __builtin_amdgcn_sched_barrier(0);
     }
     pack(32);
@@ -255,18 +267,22 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   }
   int again;                                                     // 1: once more with other references; 2: a value that is not finite
   do {
-  pages(0);
-  find(0);
+  {
+    int pg0[kPages];
+    pages(0, pg0);
+    pages(1, pg);
+    find(0, pg0);
 #pragma unroll
-  for (int n = 0; n < NI; ++n) ask_keys(Kb + w_lds, n);
+    for (int n = 0; n < NI / 4; ++n) ask_keys(Kb + w_lds, n);
+    find(1, pg);
+#pragma unroll
+    for (int n = 0; n < NI / 4; ++n) { ask_values(Vb + w_lds, n); ask_keys(Kb + BB + w_lds, n); }
+    pages(2, pg);
+  }
   // (the first step has no values yet: its weights are zeros, and so is what they multiply)
   for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + 2 * BB + 16 * i) = u32x4{0, 0, 0, 0};
 #pragma unroll
   for (int h = 0; h < HT; ++h) vf[0][h] = u32x4{0, 0, 0, 0};
-  wait_loads();
-  find(1);
-#pragma unroll
-  for (int n = 0; n < NI; ++n) { ask_values(Vb + w_lds, n); ask_keys(Kb + BB + w_lds, n); }
   wait_loads();
   __syncthreads();
 
@@ -278,42 +294,34 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[u][i][e] = 0.f;
   }
-  float s0[2][16], s1[2][16];
+  f32x16 s0[2], s1[2];
   u32x4 w0[2][2] = {}, w1[2][2] = {};
   // scores of step 0, and the keys of step 1
-  {
-    f32x16 acc[2];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane, ks);
+  for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane, ks);
 #pragma unroll
-    for (int n = 0; n < 2 * KS; ++n)
-      acc[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[n >> 1]), qf[n & 1][n >> 1], n > 1 ? acc[n & 1] : f32x16{}, 0, 0, 0);
+  for (int n = 0; n < 2 * KS; ++n)
+    s0[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[n >> 1]), qf[n & 1][n >> 1], n > 1 ? s0[n & 1] : f32x16{}, 0, 0, 0);
 #pragma unroll
-    for (int n = 0; n < 32; ++n) {
-      float v = acc[n >> 4][n & 15];
-      asm volatile("" : "+v"(v));
-      s0[n >> 4][n & 15] = v;
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane + 32 * RB, ks);
-  }
+  for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane + 32 * RB, ks);
   __syncthreads();                                               // (the first step loads over these)
 
   uint32_t v_before = Vb + 2 * BB, v_now = Vb;
   for (int j = 0; j < n_it; ++j) {
-    find(j + 2);
+    find(j + 2, pg);
+    pages(j + 3, pg);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[u][ks]));   // (in the accumulation registers: the others are needed for what is not only multiplied)
-    const bool mine_too = b_lo + NG * j + grp < b_hi;            // (a group's last step may have no block)
-    const int k0 = mine_too ? start_of(block_of(j)) : -(1 << 30);
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[u][ks]));   // (operands: in the accumulation registers, which vector instructions do not reach)
+    const bool mine_too = NG == 1 || b_lo + NG * j + grp < b_hi;            // (a group's last step may have no block)
+    const int b = b_lo + NG * j + grp, k0 = mine_too ? start_of(b) : -(1 << 30);
+    const bool whole = b >= all_lo && b < all_hi && mine_too;
     const uint32_t K = Kb + ((j + 1) & 1) * BB + k_lane, v_next = v_now == Vb + 2 * BB ? Vb : v_now + BB, k_lds = Kb + (j & 1) * BB + w_lds;
-    step(k0, s0, s1, w1, w0, K, v_before + v_lane + 48 * RB, v_now + v_lane, [&](int n) __attribute__((always_inline)) {
-      constexpr int kEvery = 24 / (2 * NI);
-      if (n % kEvery == 0 && n / kEvery < 2 * NI) { if (n / kEvery & 1) ask_keys(k_lds, n / kEvery / 2); else ask_values(v_next + w_lds, n / kEvery / 2); }
+    step(whole, k0, s0, s1, w1, w0, K, v_before + v_lane + 48 * RB, v_now + v_lane, [&](int n) __attribute__((always_inline)) {
+      if (n % 4 == 0 && n / 4 < NI / 2) { if (n & 4) ask_keys(k_lds, n / 8); else ask_values(v_next + w_lds, n / 8); }
     });
-    step(k0 + (mine_too ? 32 : 0), s1, s0, w0, w1, K + 32 * RB, v_now + v_lane + 16 * RB, v_now + v_lane + 32 * RB, [](int) {});
+    step(whole, k0 + (mine_too ? 32 : 0), s1, s0, w0, w1, K + 32 * RB, v_now + v_lane + 16 * RB, v_now + v_lane + 32 * RB, [](int) {});
     v_before = v_now;
     v_now = v_next;
     wait_loads();
