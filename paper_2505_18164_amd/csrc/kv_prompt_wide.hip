@@ -83,8 +83,10 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   auto start_of = [&](int b) __attribute__((always_inline)) { return (b << 6) + (b < kb.n_sinks ? 0 : gap); };
   // Blocks whose positions are all seen by some row of the workgroup, and by all rows of the wavefront (of those behind the first positions).
   auto first_from = [&](int pos) __attribute__((always_inline)) { return max(kb.n_sinks, (pos - gap + 63) >> 6); };   // that starts at or behind pos
-  const int in_lo = first_from(kb.from), in_hi = (kb.end - gap) >> 6;
-  const int all_lo = first_from(max(last_pos - a.sight.window + 1, 0)), all_hi = (wave_pos + 1 - gap) >> 6;
+  auto step_from = [&](int b) __attribute__((always_inline)) { return max(b - b_lo - grp + NG - 1, 0) / NG; };   // the group's first whose block is b or behind it
+  // steps whose block is the wavefront's rows' as a whole; stages whose keys and values all are
+  const int all_lo = step_from(first_from(max(last_pos - a.sight.window + 1, 0))), all_hi = step_from(min((wave_pos + 1 - gap) >> 6, b_hi));
+  const int rare_lo = step_from(first_from(kb.from)) + 1, rare_hi = step_from(min((kb.end - gap) >> 6, b_hi));
   auto visible = [&](int p, int k0) __attribute__((always_inline)) {
     return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
   };
@@ -109,38 +111,44 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   const char* const heads_at = (const char*)c.data + 2 * kv * v_by;
   const uint64_t page_bytes = 2ull * c.K * v_by;
   auto pages = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
-    const int k0 = start_of(block_of(j));
-    if constexpr (kWhole) {
-      int p = kv8_page_of(c, k0);
-      asm volatile("" : "+v"(p));                                // a vector load: behind a scalar one every read of LDS would have to wait for it
-      pg[0] = table[p];
-    } else {
+    const int k0 = start_of(block_of(kWhole ? j + lane : j));
 #pragma unroll
-      for (int n = 0; n < NI; ++n) pg[n] = table[kv8_page_of(c, visible(k0 + key_of(n), k0))];
-    }
+    for (int n = 0; n < kPages; ++n) pg[n] = table[kv8_page_of(c, kWhole ? k0 : visible(k0 + key_of(n), k0))];
   };
-  // Where stage j is: its keys' addresses from the page numbers that were asked for a stage before, its values' from the keys of
-  // that.  (The page numbers are looked at before anything else is asked for: whoever waits for them waits for that, too.)
+  // Pages that blocks lie in whole: lane i of `list` has the address of the keys of stage 64 n + i, worked out for 64 stages at a time, from
+  // page numbers that were asked for 64 stages before.
+  uint32_t list[2] = {};
+  auto fill = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
+    const int k0 = start_of(block_of(j + lane));
+    const uint64_t k = (uint64_t)(heads_at - 4096) + (checked(pg[0]) * page_bytes + (unsigned)((k0 - kv8_page_of(c, k0) * c.pt) * RB));   // (4096: see dma4)
+    list[0] = (uint32_t)k;
+    list[1] = (uint32_t)(k >> 32);
+    asm volatile("" : "+v"(list[0]), "+v"(list[1]));
+  };
+  // Where stage j is: its keys' addresses, and its values' from the keys of the one before.  (Page numbers are looked at before anything
+  // else is asked for: whoever waits for them waits for that, too.)
   auto find = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
-    const int k0 = start_of(block_of(j));
     if constexpr (kWhole) {
-      unsigned page = __builtin_amdgcn_readfirstlane((int)checked(pg[0]));
-      asm volatile("" : "+s"(page));
       v_at[0] = k_at[0] + v_by;
-      k_at[0] = heads_at + ((uint64_t)page * page_bytes + (unsigned)((k0 - kv8_page_of(c, k0) * c.pt) * RB));
-#pragma unroll
-      for (int n = 0; n < NI; ++n) { k_off[n] = at_off[n]; v_off[n] = at_off[n]; }
-      const int b0 = block_of(j), b1 = block_of(max(j - 1, 0));
-      if (__builtin_expect(b1 < in_lo || b0 >= in_hi, 0)) {
-        const int k1 = start_of(b1);
+      if ((j & 63) == 0) {
+        fill(j, pg);
+        pages(j + 64, pg);
+      }
+      k_at[0] = (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)list[1], j & 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)list[0], j & 63));
+      if (__builtin_expect(j < rare_lo || j >= rare_hi, 0)) {
+        const int k0 = start_of(block_of(j)), k1 = start_of(block_of(max(j - 1, 0)));
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
           const int key = key_of(n);
           k_off[n] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key) + by_of(n));
           v_off[n] = (uint32_t)((visible(k1 + key, k1) - k1) * RB + 16 * unit_of(key) + by_of(n));
         }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NI; ++n) { k_off[n] = at_off[n]; v_off[n] = at_off[n]; }
       }
     } else {
+      const int k0 = start_of(block_of(j));
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
         const int key = key_of(n);
@@ -151,10 +159,10 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
     }
   };
   auto ask_keys = [&](uint32_t lds, int n) __attribute__((always_inline)) {   // instructions 4 n .. + 3; lds: the wavefront's part of the block
-    if constexpr (kWhole) dma4(lds + 4096 * n, k_at[0] - 4096, &k_off[4 * n]); else dma4(lds + 4096 * n, &k_at[4 * n]);
+    if constexpr (kWhole) dma4(lds + 4096 * n, k_at[0], &k_off[4 * n]); else dma4(lds + 4096 * n, &k_at[4 * n]);
   };
   auto ask_values = [&](uint32_t lds, int n) __attribute__((always_inline)) {
-    if constexpr (kWhole) dma4(lds + 4096 * n, v_at[0] - 4096, &v_off[4 * n]); else dma4(lds + 4096 * n, &v_at[4 * n]);
+    if constexpr (kWhole) dma4(lds + 4096 * n, v_at[0], &v_off[4 * n]); else dma4(lds + 4096 * n, &v_at[4 * n]);
   };
   const uint32_t w_lds = wave * NI * 1024;
 
@@ -270,14 +278,14 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   {
     int pg0[kPages];
     pages(0, pg0);
-    pages(1, pg);
+    if constexpr (!kWhole) pages(1, pg);
     find(0, pg0);
 #pragma unroll
     for (int n = 0; n < NI / 4; ++n) ask_keys(Kb + w_lds, n);
-    find(1, pg);
+    if constexpr (kWhole) find(1, pg0); else find(1, pg);
 #pragma unroll
     for (int n = 0; n < NI / 4; ++n) { ask_values(Vb + w_lds, n); ask_keys(Kb + BB + w_lds, n); }
-    pages(2, pg);
+    if constexpr (kWhole) pg[0] = pg0[0]; else pages(2, pg);
   }
   // (the first step has no values yet: its weights are zeros, and so is what they multiply)
   for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + 2 * BB + 16 * i) = u32x4{0, 0, 0, 0};
@@ -309,14 +317,14 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   uint32_t v_before = Vb + 2 * BB, v_now = Vb;
   for (int j = 0; j < n_it; ++j) {
     find(j + 2, pg);
-    pages(j + 3, pg);
+    if constexpr (!kWhole) pages(j + 3, pg);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[u][ks]));   // (operands: in the accumulation registers, which vector instructions do not reach)
     const bool mine_too = NG == 1 || b_lo + NG * j + grp < b_hi;            // (a group's last step may have no block)
-    const int b = b_lo + NG * j + grp, k0 = mine_too ? start_of(b) : -(1 << 30);
-    const bool whole = b >= all_lo && b < all_hi && mine_too;
+    const bool whole = j >= all_lo && j < all_hi;
+    const int k0 = whole ? 0 : mine_too ? start_of(block_of(j)) : -(1 << 30);
     const uint32_t K = Kb + ((j + 1) & 1) * BB + k_lane, v_next = v_now == Vb + 2 * BB ? Vb : v_now + BB, k_lds = Kb + (j & 1) * BB + w_lds;
     step(whole, k0, s0, s1, w1, w0, K, v_before + v_lane + 48 * RB, v_now + v_lane, [&](int n) __attribute__((always_inline)) {
       if (n % 4 == 0 && n / 4 < NI / 2) { if (n & 4) ask_keys(k_lds, n / 8); else ask_values(v_next + w_lds, n / 8); }
