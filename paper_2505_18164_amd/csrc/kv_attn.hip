@@ -52,7 +52,40 @@ __global__ __launch_bounds__(kBlock) void k_kv_attn(KvCache c, KvRows r, KvAttn 
   if (piece == 0 && a.plan.splits > 1 && threadIdx.x == 0) kv_part_counts(a, c, r)[item] = pieces;
 }
 
-// The pieces of every row and head, always in the same order: a workgroup each, 256 / (h / 4) pieces at a time, a float4 a thread.
+// Up to 64 pieces of every row and head, always in the same order: a wavefront each, 64 / (h / 4) pieces at a time, a float4 a lane.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_kv_join_few(KvCache c, KvRows r, KvAttn a) {
+  const int lane = threadIdx.x & 63, h = c.h, item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)), row = item / a.H;
+  if (row >= r.n_rows || kv8_sample_of(r, row) < 0) return;      // nobody's: nothing was left
+  const int n = __builtin_amdgcn_readfirstlane(min(kv_part_counts(a, c, r)[item], a.plan.splits));
+  if (n <= 1) return;                                            // finished where it was computed
+  const float2 mark = lane < n ? *kv_part_marks(a, c, r, item, lane) : make_float2(kKvNone, 0.f);
+  float to = mark.x;
+  for (int off = 32; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, 64));
+  const float f = exp2f(mark.x - to), l = wave_sum(mark.y * f);
+  const int per = h / 4, at_once = 64 / per, slot = lane / per, ch = 4 * (lane - slot * per);
+  const float* sums = kv_part_sums(a, c, item, 0) + ch;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p0 = 0; p0 < n; p0 += at_once) {
+    const int p = p0 + slot;
+    const float w = __shfl(f, min(p, 63), 64);
+    if (slot >= at_once || p >= n) continue;
+    const float4 x = *reinterpret_cast<const float4*>(sums + (long)p * h);
+    acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
+  }
+  float4 all = acc;
+  for (int i = 1; i < at_once; ++i) {
+    const int from = min(i * per + lane, 63);
+    all.x += __shfl(acc.x, from, 64); all.y += __shfl(acc.y, from, 64); all.z += __shfl(acc.z, from, 64); all.w += __shfl(acc.w, from, 64);
+  }
+  if (slot) return;
+  T* out = (T*)a.out + ((long)row * a.out_stride + (long)(item - row * a.H) * h + ch);
+  const float inv = 1.f / l;
+  Storage<T>::put(out, all.x * inv); Storage<T>::put(out + 1, all.y * inv); Storage<T>::put(out + 2, all.z * inv); Storage<T>::put(out + 3, all.w * inv);
+}
+
+// More of them: a workgroup each, 256 / (h / 4) pieces at a time, a float4 a thread.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_kv_join(KvCache c, KvRows r, KvAttn a) {
   __shared__ float weight[kBlock], red[8];
@@ -111,7 +144,8 @@ void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (kv_decode_supported(c, r)) launch_kv_decode(s, c, r, a);
   else if (kv_prompt_supported(c, r)) launch_kv_prompt(s, c, r, a);
   else hipLaunchKernelGGL((k_kv_attn<T>), dim3(items, a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
-  if (a.plan.splits > 1) hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
+  if (a.plan.splits > 1 && a.plan.splits <= 64) hipLaunchKernelGGL((k_kv_join_few<T>), dim3((items + kBlock / 64 - 1) / (kBlock / 64)), dim3(kBlock), 0, s, c, r, a);
+  else if (a.plan.splits > 1) hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
 }
 
 }  // namespace

@@ -1,4 +1,5 @@
-// Attention of packed rows - prompts, or the next pieces of prompts, of several samples - over the bf16 cache, on the matrix cores.
+// Attention of packed rows - prompts, or the next pieces of prompts, of several samples - over the bf16 cache, on the matrix cores: heads
+// of 64, and the plan for these and for heads of 128 (kv_prompt_wide.hip).
 //
 // A workgroup takes 32 rows of (position, query head) for each of its wavefronts, the heads of one kv head side by side, and passes
 // over the keys they see 64 at a time (KvBlocks).  A wavefront computes S^T = K Q^T with v_mfma_f32_32x32x16_bf16, weighs the scores
@@ -18,9 +19,9 @@ namespace {
 
 // A workgroup is eight wavefronts: NG groups of WQ, which work on the same 32 WQ rows; group g takes the key blocks NG i + g.
 // kWhole: pages of a multiple of 64 positions, so that a block of keys lies in one.  kMany: of more than kInOrder samples.
-template <int HD, int NG, bool kWhole, bool kMany>
+template <int NG, bool kWhole, bool kMany>
 __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
-  constexpr int WQ = 8 / NG, BQ = 32 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
+  constexpr int HD = 64, WQ = 8 / NG, BQ = 32 * WQ, GT = 64 * WQ;   // rows of a workgroup - (position, head) pairs -, threads of a group
   constexpr int HT = HD / 32, RB = 2 * HD, UN = HD / 8;          // bytes and 16-byte units of a key
   constexpr int BB = BK * RB;                                    // bytes of a block of keys, or of values
   constexpr int KP = 64 / UN, NI = BK / KP / WQ;                 // keys of an instruction that loads, instructions of a wavefront
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   // lane's key of instruction n, and where in it the 16 bytes are that land at its place
   auto key_of = [&](int n) __attribute__((always_inline)) { return (wave * NI + n) * KP + lane / UN; };
   auto unit_of = [&](int key) __attribute__((always_inline)) {
-    return (lane % UN) ^ ((HD == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2) | ((key >> 2) & 3));
+    return (lane % UN) ^ ((((key >> 1) & 1) << 2) | ((key >> 2) & 3));
   };
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
   auto checked = [&](int page) __attribute__((always_inline)) {
@@ -143,8 +144,8 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   // what this lane reads: keys `col` and col + 32, 16 bytes at channels 16 ks + 8 half; values 4 half + kk and 8 further, of every 16 keys,
   // 8 bytes at channels 32 i + 16 ((lane / 16) mod 2) + 4 (lane mod 4)
   const int kk = (lane & 15) >> 2;
-  const uint32_t k_lane = col * RB + 16 * (half ^ ((HD == 128 ? (col & 3) << 2 : ((col >> 1) & 1) << 2) | ((col >> 2) & 3)));
-  const uint32_t v_lane = (4 * half + kk) * RB + 64 * (HD == 128 ? kk : kk >> 1) + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
+  const uint32_t k_lane = col * RB + 16 * (half ^ ((((col >> 1) & 1) << 2) | ((col >> 2) & 3)));
+  const uint32_t v_lane = (4 * half + kk) * RB + 64 * (kk >> 1) + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
 
   auto sees = [&](int j) __attribute__((always_inline)) {        // some row of the wavefront, some key of the block
     if (b_lo + NG * j + grp >= b_hi) return false;
@@ -229,14 +230,12 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
     }
     const int k0 = start_of(block_of(j));
     if (k0 + BK - 1 > wave_pos || (k0 <= last_pos - a.sight.window && k0 + BK > a.sight.sinks)) {   // some of these keys are not for some of the rows
-      const int up_to = pos - k0 - 4 * half, from = up_to - a.sight.window, stay = a.sight.sinks - k0 - 4 * half;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t seen = seen_keys(pos - k0 - 32 * t, a.sight.window, a.sight.sinks - k0 - 32 * t) >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = 32 * t + 8 * (e >> 2) + (e & 3);
-          s[t][e] = key <= up_to && (key > from || key < stay) ? s[t][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) s[t][e] = masked(s[t][e], seen, 8 * (e >> 2) + (e & 3));
+      }
     }
     weigh();
   };
@@ -339,19 +338,14 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   if (live) prompt_store<HT>(c, r, a, mine, row, head, o, m, l);
 }
 
-template <int HD, int NG>
+template <int NG>
 constexpr size_t prompt_lds() {
-  const size_t kv = (size_t)NG * 4 * BK * 2 * HD, fold = (size_t)(NG - 1) * (HD / 2 + 2) * (512 / NG) * sizeof(float);
+  const size_t kv = (size_t)NG * 4 * BK * 128, fold = (size_t)(NG - 1) * 34 * (512 / NG) * sizeof(float);
   return kv > fold ? kv : fold;
 }
-template <int HD, int NG, bool kWhole, bool kMany>
+template <int NG, bool kWhole, bool kMany>
 bool allow_one() {                                               // 64 KiB is what a kernel gets by default
-  constexpr size_t lds = prompt_lds<HD, NG>();
-  return hipFuncSetAttribute((const void*)k_kv_prompt<HD, NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
-}
-template <int HD, int NG>
-bool allow_groups() {
-  return allow_one<HD, NG, true, false>() && allow_one<HD, NG, false, false>() && allow_one<HD, NG, true, true>() && allow_one<HD, NG, false, true>();
+  return hipFuncSetAttribute((const void*)k_kv_prompt<NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)prompt_lds<NG>()) == hipSuccess;
 }
 
 PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int WQ) {
@@ -368,7 +362,7 @@ PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& 
   double best_us = 1e30;
   for (int ng = 1; ng <= 2; ++ng) {
     const int sh = kv_heads_shift(c, H), bp = 256 / ng >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, rows) + 64);
-    const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.0 : 2.4) : (ng == 1 ? 1.35 : 1.55);
+    const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.0 : 2.25) : (ng == 1 ? 1.35 : 1.55);
     const double seen = std::min<double>(most, r.max_ctx - 0.5 * std::min(r.max_ctx, rows));   // what a workgroup sees, on average
     for (int s = 1; s <= 32; s *= 2) {
       if (s > 1 && most < 256 * s) break;
@@ -384,29 +378,10 @@ PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& 
 // A launch has fewer than 2^32 threads.  n_rows * H is below 2^24, so the workgroups of up to kInOrder samples, at most 2^24 / 128 for
 // the rows and H for each sample, are far below that; one for each of very many samples and heads may not be, and go out in several.
 constexpr int kMostWgs = 1 << 22;
-template <int HD, int NG, bool kWhole>
-void launch_pages(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  PromptGeo g = geo_of(c, r, a.H, 8 / NG);
-  const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
-  if (a.plan.wide) {
-    if (r.n <= kInOrder) launch_kv_wide(s, c, r, a, g, total, false);
-    else for (; g.from < total; g.from += kMostWgs) launch_kv_wide(s, c, r, a, g, std::min(kMostWgs, total - g.from), true);
-    return;
-  }
-  if (r.n <= kInOrder) {
-    hipLaunchKernelGGL((k_kv_prompt<HD, NG, kWhole, false>), dim3(total, a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
-    return;
-  }
-  for (; g.from < total; g.from += kMostWgs)
-    hipLaunchKernelGGL((k_kv_prompt<HD, NG, kWhole, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(512), (prompt_lds<HD, NG>()), s, c, r, a, g);
-}
-template <int HD, int NG>
-void launch_groups(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  if (c.pt % BK == 0) launch_pages<HD, NG, true>(s, c, r, a); else launch_pages<HD, NG, false>(s, c, r, a);
-}
-template <int HD>
-void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  if (a.plan.groups == 1) launch_groups<HD, 1>(s, c, r, a); else launch_groups<HD, 2>(s, c, r, a);
+template <int NG, bool kWhole>
+void launch_pages(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs) {
+  if (r.n <= kInOrder) hipLaunchKernelGGL((k_kv_prompt<NG, kWhole, false>), dim3(wgs, a.plan.splits), dim3(512), prompt_lds<NG>(), s, c, r, a, g);
+  else hipLaunchKernelGGL((k_kv_prompt<NG, kWhole, true>), dim3(wgs, a.plan.splits), dim3(512), prompt_lds<NG>(), s, c, r, a, g);
 }
 
 }  // namespace
@@ -415,7 +390,7 @@ bool kv_prompt_supported(const KvCache& c, const KvRows& r) { return r.start && 
 bool kv_allow_lds() {
   static OncePerDevice done;
   int dev = -1;
-  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_groups<64, 1>() && allow_groups<64, 2>() && allow_groups<128, 1>() && allow_groups<128, 2>() && kv_wide_allow_lds(); });
+  return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_one<2, true, false>() && allow_one<2, false, false>() && allow_one<2, true, true>() && allow_one<2, false, true>() && kv_wide_allow_lds(); });
 }
 
 KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
@@ -424,11 +399,20 @@ KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w
   const int bp = 256 / p.groups >> kv_heads_shift(c, H);
   const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
   const int chunk = (int)((most + p.splits - 1) / p.splits);
-  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups, c.h == 128};
+  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
 }
 
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  if (c.h == 128) launch_heads<128>(s, c, r, a); else launch_heads<64>(s, c, r, a);
+  PromptGeo g = geo_of(c, r, a.H, 8 / a.plan.groups);
+  const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
+  const bool many = r.n > kInOrder, whole = c.pt % BK == 0;
+  for (; g.from < total; g.from += kMostWgs) {
+    const int wgs = many ? std::min(kMostWgs, total - g.from) : total;
+    if (c.h == 128) launch_kv_wide(s, c, r, a, g, wgs, many);
+    else if (a.plan.groups == 1) { if (whole) launch_pages<1, true>(s, c, r, a, g, wgs); else launch_pages<1, false>(s, c, r, a, g, wgs); }
+    else { if (whole) launch_pages<2, true>(s, c, r, a, g, wgs); else launch_pages<2, false>(s, c, r, a, g, wgs); }
+    if (!many) break;
+  }
 }
 
 }  // namespace mdi

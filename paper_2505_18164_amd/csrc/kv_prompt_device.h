@@ -51,6 +51,15 @@ __device__ __forceinline__ KvBlocks kv_blocks(const KvSight& w, int at, int end)
 
 
 
+// What a row at distance `up_to` behind the first of 32 keys sees of them, a bit a key; `stay` of them are among the first positions.
+__device__ __forceinline__ uint32_t lowest(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t seen_keys(int up_to, int window, int stay) { return lowest(up_to + 1) & (~lowest(up_to - window + 1) | lowest(stay)); }
+// A score, or -inf where bit `key` says so.
+__device__ __forceinline__ float masked(float s, uint32_t seen, int key) {
+  const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, key, 1);
+  return __uint_as_float((__float_as_uint(s) & all) | (0xFF800000u & ~all));
+}
+
 // What a workgroup's rows are, and the blocks they see.
 struct PromptRows {
   BlockPlace at;

@@ -29,9 +29,9 @@ __device__ __forceinline__ void dma4(uint32_t lds, const char* const* p) {
 }
 
 // A workgroup is four wavefronts: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
-template <int HD, int NG, bool kWhole, bool kMany>
+template <int NG, bool kWhole, bool kMany>
 __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
-  constexpr int WQ = 4 / NG, BQ = 64 * WQ, GT = 64 * WQ;         // rows of a workgroup - (position, head) pairs -, threads of a group
+  constexpr int HD = 128, WQ = 4 / NG, BQ = 64 * WQ, GT = 64 * WQ;   // rows of a workgroup - (position, head) pairs -, threads of a group
   constexpr int HT = HD / 32, KS = HD / 16, RB = 2 * HD, UN = HD / 8;   // bytes and 16-byte units of a key
   constexpr int BB = BK * RB;                                    // bytes of a block of keys, or of values
   constexpr int KP = 64 / UN, NI = BK / KP / WQ;                 // keys of an instruction that loads, instructions of a wavefront
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   };
   auto key_of = [&](int n) __attribute__((always_inline)) { return (wave * NI + n) * KP + lane / UN; };
   auto unit_of = [&](int key) __attribute__((always_inline)) {
-    return (lane % UN) ^ ((HD == 128 ? (key & 3) << 2 : ((key >> 1) & 1) << 2) | ((key >> 2) & 3));
+    return (lane % UN) ^ (((key & 3) << 2) | ((key >> 2) & 3));
   };
   auto by_of = [](int n) __attribute__((always_inline)) { return 4096 - 1024 * (n & 3); };   // (dma4 adds what is missing)
   unsigned worst = 0;                                            // a page that is not of the cache is looked for at the end, the last one read in its place
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   const uint32_t w_lds = wave * NI * 1024;
 
   const int kk = (lane & 15) >> 2;                               // what this lane reads: as in kv_prompt.hip
-  const uint32_t k_lane = col * RB + 16 * (half ^ ((HD == 128 ? (col & 3) << 2 : ((col >> 1) & 1) << 2) | ((col >> 2) & 3)));
-  const uint32_t v_lane = (4 * half + kk) * RB + 64 * (HD == 128 ? kk : kk >> 1) + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
+  const uint32_t k_lane = col * RB + 16 * (half ^ (((col & 3) << 2) | ((col >> 2) & 3)));
+  const uint32_t v_lane = (4 * half + kk) * RB + 64 * kk + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
   u32x4 kf[KS], vf[2][HT];                                       // operands: keys of a step; values of its first and second 16 keys
   bf16x8 qf[2][KS];
   auto read_key = [&](uint32_t K, int ks) __attribute__((always_inline)) { kf[ks] = read_lds(K ^ (32 * ks)); };
@@ -191,14 +191,12 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
     if (!whole) {                                                // some of these keys are not for some of the rows
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int up_to = k0 < 0 ? -1 : pos[u] - k0 - 4 * half, from = up_to - a.sight.window, stay = a.sight.sinks - k0 - 4 * half;
+        const uint32_t seen = k0 < 0 ? 0u : seen_keys(pos[u] - k0, a.sight.window, a.sight.sinks - k0) >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = 8 * (e >> 2) + (e & 3);
-          sc[u][e] = key <= up_to && (key > from || key < stay) ? sc[u][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) sc[u][e] = masked(sc[u][e], seen, 8 * (e >> 2) + (e & 3));
       }
     }
+    asm volatile("" : "+v"(sc[0]), "+v"(sc[1]));                 // (not in the accumulation registers)
     float sum[2] = {0.f, 0.f}, next = fmaf(sc[0][0], scale, -m[0]), w0 = 0.f, w1 = 0.f;
     auto pack = [&](int n) __attribute__((always_inline)) {      // weights n - 2 and n - 1
       const int u = (n - 2) >> 4, e = (n - 2) & 15;
@@ -406,12 +404,12 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
 template <int NG> constexpr size_t wide_lds() { return (size_t)NG * 5 * BK * 256; }
 template <int NG, bool kWhole, bool kMany>
 bool allow_one() {                                               // 64 KiB is what a kernel gets by default
-  return hipFuncSetAttribute((const void*)k_kv_prompt_wide<128, NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds<NG>()) == hipSuccess;
+  return hipFuncSetAttribute((const void*)k_kv_prompt_wide<NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds<NG>()) == hipSuccess;
 }
 template <int NG, bool kWhole>
 void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs, bool many) {
-  if (many) hipLaunchKernelGGL((k_kv_prompt_wide<128, NG, kWhole, true>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
-  else hipLaunchKernelGGL((k_kv_prompt_wide<128, NG, kWhole, false>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
+  if (many) hipLaunchKernelGGL((k_kv_prompt_wide<NG, kWhole, true>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
+  else hipLaunchKernelGGL((k_kv_prompt_wide<NG, kWhole, false>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
 }
 
 }  // namespace
