@@ -49,21 +49,24 @@ template <int N> __device__ __forceinline__ void store(float* p, const float* x)
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvAppend a, int l_sh, int pieces) {
   __shared__ __attribute__((aligned(16))) float turn[kBlock / 64][2][128];   // cosines, sines
+  __shared__ __attribute__((aligned(16))) float gains[2][2][256];            // of queries and keys: gains, biases
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), L = 1 << l_sh;
   const unsigned item = blockIdx.x * (kBlock / 64) + wave;
   const int row = (int)(item / (unsigned)pieces), piece = (int)(item - (unsigned)row * (unsigned)pieces);
-  if (row >= r.n_rows) return;
+  const bool norms = a.q_g || a.k_g;
+  if (row >= r.n_rows && !norms) return;
 
   const int j = lane & (L - 1), half = a.rot >> 1, heads = a.H + 2 * c.K;
   const bool turns = V * j < half;
-  const int ch0 = turns ? V * j : 2 * V * j, ch1 = turns ? half + V * j : ch0 + V;   // (half is a multiple of V: lanes past it hold what is not rotated)
+  // (half is a multiple of V: lanes past it hold what is not rotated, in two parts as well, so that neighbours are next to each other)
+  const int ch0 = turns ? V * j : half + V * j, ch1 = ch0 + (turns ? half : (c.h - a.rot) >> 1);
   const int hr0 = (piece * kUnits << (6 - l_sh)) + (lane >> l_sh), step = 64 >> l_sh;
   float x[kUnits][2 * V];
   bool live[kUnits];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     const int hr = hr0 + u * step, kv = hr - a.H;
-    live[u] = hr < heads && ch1 < c.h;
+    live[u] = row < r.n_rows && hr < heads && 2 * V * j < c.h;
     if (!live[u]) {
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) x[u][i] = 0.f;
@@ -73,6 +76,17 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
                         : (const T*)(kv < c.K ? a.k : a.v) + ((long)row * a.kv_row + (long)(kv < c.K ? kv : kv - c.K) * a.kv_head);
     load<V>(p + ch0, x[u]);
     load<V>(p + ch1, x[u] + V);
+  }
+
+  if (norms) {                                                   // (behind the rows' loads: read once a workgroup)
+    for (int i = threadIdx.x; i < c.h; i += kBlock) {
+      gains[0][0][i] = a.q_g ? a.q_g[i] : 0.f;
+      gains[0][1][i] = a.q_b ? a.q_b[i] : 0.f;
+      gains[1][0][i] = a.k_g ? a.k_g[i] : 0.f;
+      gains[1][1][i] = a.k_b ? a.k_b[i] : 0.f;
+    }
+    __syncthreads();
+    if (row >= r.n_rows) return;
   }
 
   // Where the row goes.
@@ -100,9 +114,7 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     const int hr = hr0 + u * step, kv = hr - a.H;
-    const float* const g = kv < 0 ? a.q_g : a.k_g;
-    const float* const b = kv < 0 ? a.q_b : a.k_b;
-    if (a.q_g || a.k_g) {                                        // (all lanes: the sums go over neighbours)
+    if (norms) {                                                 // (all lanes: the sums go over neighbours)
       float mean = 0.f, sum = 0.f;
       if (!a.rms) {
 #pragma unroll
@@ -112,12 +124,18 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) { const float d = x[u][i] - mean; sum = live[u] ? fmaf(d, d, sum) : 0.f; }
       const float by = 1.f / sqrtf(group_sum(sum, L) / c.h + a.eps);
-      if (live[u] && kv < c.K && g)
+      if (live[u] && (kv < 0 ? a.q_g != nullptr : kv < c.K && a.k_g)) {
+        const float* const g = gains[kv < 0 ? 0 : 1][0];
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) {
+        for (int i = 0; i < 2 * V; i += 4) {
           const int ch = i < V ? ch0 + i : ch1 + i - V;
-          x[u][i] = fmaf((x[u][i] - mean) * by, g[ch], b ? b[ch] : 0.f);
+          const float4 gain = *reinterpret_cast<const float4*>(g + ch), bias = *reinterpret_cast<const float4*>(g + 256 + ch);
+          x[u][i] = fmaf((x[u][i] - mean) * by, gain.x, bias.x);
+          x[u][i + 1] = fmaf((x[u][i + 1] - mean) * by, gain.y, bias.y);
+          x[u][i + 2] = fmaf((x[u][i + 2] - mean) * by, gain.z, bias.z);
+          x[u][i + 3] = fmaf((x[u][i + 3] - mean) * by, gain.w, bias.w);
         }
+      }
     }
     if (!live[u]) continue;
     if (kv < c.K && turns)
@@ -147,9 +165,9 @@ void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppend& a)
 }  // namespace
 
 void launch_kv_append(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppend& a) {
-  const bool eight = c.h % 16 == 0 && a.rot % 16 == 0;           // sixteen channels a lane, else eight
+  const bool eight = c.h % 16 == 0 && a.rot % 16 == 0;           // 16 bytes a load: sixteen channels a lane, of fp32 eight; else 8 bytes
   if (c.dtype == MDI_BF16) { if (eight) launch<bf16_t, 8>(s, c, r, a); else launch<bf16_t, 4>(s, c, r, a); }
-  else { if (eight) launch<float, 8>(s, c, r, a); else launch<float, 4>(s, c, r, a); }
+  else launch<float, 4>(s, c, r, a);
 }
 
 }  // namespace mdi

@@ -111,8 +111,9 @@ def lib():
         L.mdi_kv8_attn.argtypes = [kv8, rows, vp, u64, u32, C.c_float, vp, u64, vp, C.c_size_t, vp]
         L.mdi_kv8_attn_bytes.argtypes = [kv8, rows, u32, C.POINTER(C.c_size_t)]
         kv, prep = C.POINTER(MdiKv), C.POINTER(MdiQkPrep)
-        L.mdi_kv_append.argtypes = [kv, rows, prep, vp, vp, u64, u64, vp, u64, u64, u32, vp, u64, vp]
-        L.mdi_kv_attn.argtypes = [kv, rows, vp, u64, u32, C.c_float, u32, u32, vp, u64, vp, C.c_size_t, vp]
+        # (whole numbers as void pointers, which are passed alike: ctypes takes half the time over them)
+        L.mdi_kv_append.argtypes = [kv, rows, prep] + [vp] * 11
+        L.mdi_kv_attn.argtypes = [kv, rows, vp, vp, vp, C.c_float] + [vp] * 7
         L.mdi_kv_attn_bytes.argtypes = [kv, rows, u32, u32, u32, C.POINTER(C.c_size_t)]
         for name in EXPORTS:
             if name not in ("mdi_partition_destroy", "mdi_strerror"):
@@ -398,6 +399,7 @@ class Partition:
 
 # the current stream of a GPU as a number: torch's own way to it where there is one (a Stream object costs 2 us a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 _KV8_TYPES = {torch.bfloat16: MDI_BF16, torch.float32: MDI_F32}
@@ -422,7 +424,7 @@ class _PagedCache:
     def _call(self, what, *args):
         """A C entry point, on the current stream of the cache's GPU, with that GPU current."""
         index = self.device.index
-        if index == torch.cuda.current_device():
+        if index == _current_gpu():
             st = getattr(lib(), what)(*args, _raw_stream(index))
         else:
             with torch.cuda.device(index):
@@ -554,7 +556,7 @@ class KvCache(_PagedCache):
             raise ValueError("data [pages, kv heads, 2, page tokens, head_dim], tables [samples, pages]")
         if data.dtype not in _KV8_TYPES:
             raise ValueError("data: bfloat16 or float32")
-        self.device, self.dtype = data.device, data.dtype
+        self.device, self.dtype, self._index = data.device, data.dtype, data.get_device()
         self._tensor(data, data.dtype, "data")
         self._tensor(tables, torch.int32, "tables")
         if err is not None:
@@ -584,30 +586,36 @@ class KvCache(_PagedCache):
         keep = (q_gain, q_bias, k_gain, k_bias, freq)
         return QkPrep(keep, MdiQkPrep(*[_ptr(t) for t in keep], eps, _NORMS[norm], rot), self.device)
 
+    def _away(self, t):
+        """Is tensor t somewhere else than the cache?"""
+        i = t.get_device()
+        return i != self._index or (i < 0 and t.device != self.device)
+
     def _heads(self, x, heads, rows, what):
         """Address, row stride and head stride of x [rows, heads, head_dim]."""
         shape, stride = x.shape, x.stride()
-        if shape != (rows.n_rows, heads, self.h) or stride[2] != 1 or x.dtype != self.dtype or x.device != self.device:
+        if shape != (rows, heads, self.h) or stride[2] != 1 or x.dtype != self.dtype or self._away(x):
             raise ValueError(f"append: {what} {self.dtype} [rows, {heads} heads, {self.h}] on {self.device}, channels next to each other")
-        return x.data_ptr(), stride[0] if shape[0] > 1 else heads * self.h, stride[1] if heads > 1 else self.h
+        return x.data_ptr(), stride[0] if rows > 1 else heads * self.h, stride[1] if heads > 1 else self.h
 
     def append(self, rows, k, v, q=None, prep=None, q_out=None):
         """Rows k, v [rows, kv heads, head_dim] into the cache and q [rows, heads, head_dim] into q_out (any row and head stride, the
         cache's type), keys and queries through `prep` on the way (see prep(); None: as they are).  Returns q_out, a new tensor
         by default; it may be q itself."""
-        if rows.device != self.device or (prep is not None and prep.device != self.device):
-            raise ValueError(f"append: rows and prep on {self.device}")
-        kp, k_row, k_head = self._heads(k, self.K, rows, "k")
-        vp, v_row, v_head = self._heads(v, self.K, rows, "v")
-        if (k_row, k_head) != (v_row, v_head):
+        device, n = self.device, rows.n_rows
+        if (rows.device is not device and rows.device != device) or (prep is not None and prep.device is not device and prep.device != device):
+            raise ValueError(f"append: rows and prep on {device}")
+        kp, k_row, k_head = self._heads(k, self.K, n, "k")
+        vp, v_row, v_head = self._heads(v, self.K, n, "v")
+        if k_row != v_row or k_head != v_head:
             raise ValueError("append: k and v laid out alike")
         qp, q_row, q_head, heads, op, out_row = None, 0, 0, 0, None, 0
         if q is not None:
             heads = q.shape[1] if q.dim() == 3 else 0
-            qp, q_row, q_head = self._heads(q, heads, rows, "q")
+            qp, q_row, q_head = self._heads(q, heads, n, "q")
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            op, out_row, out_head = self._heads(q_out, heads, rows, "q_out")
+            op, out_row, out_head = self._heads(q_out, heads, n, "q_out")
             if out_head != self.h:
                 raise ValueError("append: heads of q_out next to each other")
         elif q_out is not None:
@@ -629,18 +637,18 @@ class KvCache(_PagedCache):
         workspace() (None: taken from the allocator for this call)."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        shape, qs, os, h = q.shape, q.stride(), out.stride(), self.h
-        if (len(shape) != 3 or shape[0] != rows.n_rows or shape[2] != h or out.shape != shape or q.dtype != self.dtype or out.dtype != self.dtype
-                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or q.device != self.device or out.device != self.device
-                or rows.device != self.device):
-            raise ValueError(f"attn: q and out {self.dtype} [rows, heads, {h}] on {self.device}, heads next to each other")
+        shape, qs, os, h, device, dtype = q.shape, q.stride(), out.stride(), self.h, self.device, self.dtype
+        if (len(shape) != 3 or shape[0] != rows.n_rows or shape[2] != h or out.shape != shape or q.dtype != dtype or out.dtype != dtype
+                or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or self._away(q) or self._away(out)
+                or (rows.device is not device and rows.device != device)):
+            raise ValueError(f"attn: q and out {dtype} [rows, heads, {h}] on {device}, heads next to each other")
         if not (0 <= window < 1 << 32 and 0 <= sinks < 1 << 32):
             raise ValueError("window, sinks: beyond 32 bits")
         heads = shape[1]
         if workspace is None:
             workspace = self.workspace(rows, heads, window, sinks)
-        elif workspace.device != self.device or not workspace.is_contiguous():
-            raise ValueError(f"attn: a contiguous workspace on {self.device}")
+        elif self._away(workspace) or not workspace.is_contiguous():
+            raise ValueError(f"attn: a contiguous workspace on {device}")
         alone = shape[0] < 2                                     # a lone row has no neighbours, whatever its stride says
         self._call("mdi_kv_attn", self._ref, rows._ref, q.data_ptr(), heads * h if alone else qs[0], heads, h ** -0.5 if scale is None else scale,
                    window, sinks, out.data_ptr(), heads * h if alone else os[0], None if workspace is None else workspace.data_ptr(),
