@@ -8,8 +8,6 @@
 namespace mdi {
 namespace {
 
-constexpr int kUnits = 4;                                        // head rows a lane takes one after the other
-
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -43,10 +41,10 @@ template <int N> __device__ __forceinline__ void store(float* p, const float* x)
   for (int n = 0; n < N; n += 4) *reinterpret_cast<float4*>(p + n) = make_float4(x[n], x[n + 1], x[n + 2], x[n + 3]);
 }
 
-// A wavefront takes the head rows - queries, then keys, then values - of one row of the call, 64 / L at a time and kUnits times.  A
+// A wavefront takes the head rows - queries, then keys, then values - of one row of the call, 64 / L at a time and U times.  A
 // lane holds 2 V channels of one: V that are rotated and their V partners, so that no other lane is needed, or 2 V that are not.  The
 // angles are the same for all heads: each is worked out by one lane and read by the others from LDS.
-template <typename T, int V>
+template <typename T, int V, int U>
 __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvAppend a, int l_sh, int pieces) {
   __shared__ __attribute__((aligned(16))) float turn[kBlock / 64][2][128];   // cosines, sines
   __shared__ __attribute__((aligned(16))) float gains[2][2][256];            // of queries and keys: gains, biases
@@ -60,11 +58,11 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
   const bool turns = V * j < half;
   // (half is a multiple of V: lanes past it hold what is not rotated, in two parts as well, so that neighbours are next to each other)
   const int ch0 = turns ? V * j : half + V * j, ch1 = ch0 + (turns ? half : (c.h - a.rot) >> 1);
-  const int hr0 = (piece * kUnits << (6 - l_sh)) + (lane >> l_sh), step = 64 >> l_sh;
-  float x[kUnits][2 * V];
-  bool live[kUnits];
+  const int hr0 = (piece * U << (6 - l_sh)) + (lane >> l_sh), step = 64 >> l_sh;
+  float x[U][2 * V];
+  bool live[U];
 #pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int hr = hr0 + u * step, kv = hr - a.H;
     live[u] = row < r.n_rows && hr < heads && 2 * V * j < c.h;
     if (!live[u]) {
@@ -112,7 +110,7 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
   for (int i = 0; i < V; ++i) { cs[i] = turns ? turn[wave][0][V * j + i] : 1.f; sn[i] = turns ? turn[wave][1][V * j + i] : 0.f; }
 
 #pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int hr = hr0 + u * step, kv = hr - a.H;
     if (norms) {                                                 // (all lanes: the sums go over neighbours)
       float mean = 0.f, sum = 0.f;
@@ -153,13 +151,22 @@ __global__ __launch_bounds__(kBlock) void k_kv_append(KvCache c, KvRows r, KvApp
   }
 }
 
+template <typename T, int V, int U>
+void launch_units(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppend& a, int l_sh) {
+  const int per = U * (64 >> l_sh), pieces = (a.H + 2 * c.K + per - 1) / per;
+  const dim3 grid((unsigned)(((long)r.n_rows * pieces + kBlock / 64 - 1) / (kBlock / 64)));
+  hipLaunchKernelGGL((k_kv_append<T, V, U>), grid, dim3(kBlock), 0, s, c, r, a, l_sh, pieces);
+}
+// Units of a wavefront: of 4, 3 and 2 the one that leaves the fewest of them without a head, of equals the larger.
 template <typename T, int V>
 void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppend& a) {
   int l_sh = 0;
   while ((2 * V << l_sh) < c.h) ++l_sh;
-  const int per = kUnits * (64 >> l_sh), pieces = (a.H + 2 * c.K + per - 1) / per;
-  const dim3 grid((unsigned)(((long)r.n_rows * pieces + kBlock / 64 - 1) / (kBlock / 64)));
-  hipLaunchKernelGGL((k_kv_append<T, V>), grid, dim3(kBlock), 0, s, c, r, a, l_sh, pieces);
+  const int need = (a.H + 2 * c.K + (64 >> l_sh) - 1) >> (6 - l_sh);       // units of a row
+  auto idle = [&](int u) { return (need + u - 1) / u * u - need; };
+  if (idle(4) <= idle(3) && idle(4) <= idle(2)) launch_units<T, V, 4>(s, c, r, a, l_sh);
+  else if (idle(3) <= idle(2)) launch_units<T, V, 3>(s, c, r, a, l_sh);
+  else launch_units<T, V, 2>(s, c, r, a, l_sh);
 }
 
 }  // namespace
