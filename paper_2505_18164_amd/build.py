@@ -14,13 +14,13 @@ LIB = os.path.join(HERE, "libmdi.so")
 SOURCES = ["mdi_api.hip", "decode.hip", "prefill.hip", "gemm_bf16.hip", "gemm_f32.hip", "step_w4.hip", "step_w4_f32.hip",
            "step_w8.hip", "step_w8_f32.hip", "step_batch_ln.hip", "step_batch_rms.hip", "step_batch_ln_w4.hip", "step_batch_rms_w4.hip", "heads.hip", "attn_prefill.hip",
            "kv8_api.hip", "kv8_rows.hip", "kv8_attn.hip", "kv8_decode.hip", "kv8_prompt.hip",
-           "kv8_visit.hip", "kv_api.hip", "kv_append.hip", "kv_attn.hip", "kv_decode.hip", "kv_prompt.hip", "kv_prompt_wide.hip"]
+           "kv8_visit.hip", "kv_api.hip", "kv_append.hip", "kv_attn.hip", "kv_any.hip", "kv_decode.hip", "kv_prompt.hip", "kv_prompt_wide.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wall", "-Wno-unused-function"]
 
 # results of matrix instructions in the registers that vector instructions use, where the source does not say otherwise
-FILE_FLAGS = {"kv_prompt_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+FILE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("kv_prompt_wide.hip", "kv_any.hip")}
 
 
 def _hipcc():

@@ -1,56 +1,10 @@
-// Attention over the cache in the storage type: the simple form, for any head and type, and the launch that adds the pieces of rows
-// which were divided.
+// Attention over the cache in the storage type: which kernel serves a call, and the launch that adds the pieces of rows that were divided.
 #include <algorithm>
 
 #include "kv_device.h"
 
 namespace mdi {
 namespace {
-
-// One workgroup per row, head and piece of what the row sees, its wavefronts' sums folded at the end.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_kv_attn(KvCache c, KvRows r, KvAttn a, int L) {
-  __shared__ float sm[4][8 * 32 + 2];
-  const int row = blockIdx.x / a.H, head = blockIdx.x - row * a.H, kv = head / (a.H / c.K), piece = blockIdx.y;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = c.h;
-  const Kv8View v = kv8_view(c, r, row);
-  if (v.sample < 0) return;
-  T* out = (T*)a.out + ((long)row * a.out_stride + (long)head * h);
-  const int t = v.seen ? kv8_table_row(c, r, v.sample) : -1, item = row * a.H + head;
-  if (t < 0) {
-    if (piece) return;
-    for (int e = threadIdx.x; e < h; e += kBlock) Storage<T>::put(out + e, 0.f);
-    if (a.plan.splits > 1 && threadIdx.x == 0) kv_part_counts(a, c, r)[item] = 1;
-    return;
-  }
-  const int32_t* table = c.tables + (long)t * c.table_stride;
-  const KvSpan span = kv_span(a.sight, v.seen);
-  const int n = span.places(), lo = piece * a.plan.chunk, hi = min(n, lo + a.plan.chunk), pieces = (n + a.plan.chunk - 1) / a.plan.chunk;
-  if (lo >= hi) return;
-  const int ch = 8 * (lane & (L - 1)), sub = lane / L, tpw = 64 / L;
-  const bool live = ch < h;
-  float q[8] = {};
-  if (live) KvType<T>::load8((const T*)a.q + ((long)row * a.q_stride + (long)head * h + ch), q);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) q[j] *= a.scale;
-  const KvSums mine = kv_attend<T>(c, table, kv, span, q, L, ch, live, lo + wave * tpw, 4 * tpw, hi);
-  if (sub == 0) {
-    if (live)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sm[wave][ch + j] = mine.o[j];
-    if (lane == 0) { sm[wave][h] = mine.m; sm[wave][h + 1] = mine.l; }
-  }
-  __syncthreads();
-  float to = kKvNone;
-  for (int w = 0; w < 4; ++w) to = fmaxf(to, sm[w][h]);
-  for (int e = threadIdx.x; e < h; e += kBlock) {
-    float sum = 0.f, ls = 0.f;
-    for (int w = 0; w < 4; ++w) { const float f = exp2f(sm[w][h] - to); sum += sm[w][e] * f; ls += sm[w][h + 1] * f; }
-    if (pieces == 1) Storage<T>::put(out + e, sum / ls);
-    else { kv_part_sums(a, c, item, piece)[e] = sum; if (e == 0) *kv_part_marks(a, c, r, item, piece) = make_float2(to, ls); }
-  }
-  if (piece == 0 && a.plan.splits > 1 && threadIdx.x == 0) kv_part_counts(a, c, r)[item] = pieces;
-}
 
 // Up to 64 pieces of every row and head, always in the same order: a wavefront each, 64 / (h / 4) pieces at a time, a float4 a lane.
 template <typename T>
@@ -137,32 +91,23 @@ __global__ __launch_bounds__(kBlock) void k_kv_join(KvCache c, KvRows r, KvAttn 
 }
 
 template <typename T>
-void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  int L = 1;
-  while (8 * L < c.h) L *= 2;
+void launch_join(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   const unsigned items = (unsigned)(r.n_rows * a.H);
-  if (kv_decode_supported(c, r)) launch_kv_decode(s, c, r, a);
-  else if (kv_prompt_supported(c, r)) launch_kv_prompt(s, c, r, a);
-  else hipLaunchKernelGGL((k_kv_attn<T>), dim3(items, a.plan.splits), dim3(kBlock), 0, s, c, r, a, L);
-  if (a.plan.splits > 1 && a.plan.splits <= 64) hipLaunchKernelGGL((k_kv_join_few<T>), dim3((items + kBlock / 64 - 1) / (kBlock / 64)), dim3(kBlock), 0, s, c, r, a);
-  else if (a.plan.splits > 1) hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
+  if (a.plan.splits <= 64) hipLaunchKernelGGL((k_kv_join_few<T>), dim3((items + kBlock / 64 - 1) / (kBlock / 64)), dim3(kBlock), 0, s, c, r, a);
+  else hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
 }
 
 }  // namespace
 
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  if (kv_decode_supported(c, r)) return kv_decode_plan(c, r, H, w);
-  if (kv_prompt_supported(c, r)) return kv_prompt_plan(c, r, H, w);
-  const int most = kv_most_seen(w, r.max_ctx);
-  const int want = (int)std::max<long>(1, std::min<long>(64, 1024 / ((long)r.n_rows * H)));
-  KvPlan p{};
-  p.chunk = std::max(256, ((most + want - 1) / want + 63) / 64 * 64);
-  p.splits = (most + p.chunk - 1) / p.chunk;
-  return p;
+  return kv_decode_supported(c, r) ? kv_decode_plan(c, r, H, w) : kv_prompt_supported(c, r) ? kv_prompt_plan(c, r, H, w) : kv_any_plan(c, r, H, w);
 }
 
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  if (c.dtype == MDI_BF16) launch<bf16_t>(s, c, r, a); else launch<float>(s, c, r, a);
+  if (kv_decode_supported(c, r)) launch_kv_decode(s, c, r, a);
+  else if (kv_prompt_supported(c, r)) launch_kv_prompt(s, c, r, a);
+  else launch_kv_any(s, c, r, a);
+  if (a.plan.splits > 1) { if (c.dtype == MDI_BF16) launch_join<bf16_t>(s, c, r, a); else launch_join<float>(s, c, r, a); }
 }
 
 }  // namespace mdi

@@ -52,6 +52,9 @@ bool kv_prompt_supported(const KvCache& c, const KvRows& r);
 bool kv_allow_lds();
 KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
+// The others, also on the matrix cores (kv_any.hip).
+KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
+void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 
