@@ -1,14 +1,20 @@
 // Attention over the cache in the storage type on the matrix cores, for what the other two kernels do not serve: fp32, and bf16 heads of
 // other than 64 or 128 channels; single tokens and packed rows.
 //
-// A wavefront takes sixteen rows of (position, query head) of a kv head, or S times as many, and passes over the keys they see,
-// sixteen at a time (bf16: two times sixteen), straight from the pages into registers.  Both products are computed transposed, as in
-// kv_decode.hip: S^T = K Q^T leaves scores of keys 4 g + r (g = lane / 16) of row lane % 16 in a lane, which is what O^T = V^T P^T
-// takes as its second operand - for fp32 v_mfma_f32_16x16x4_f32, whose products and sums are fp32's, register by register; for bf16
-// v_mfma_f32_16x16x32_bf16 with a weight as two operands, its upper digits and what they leave.  Channels and keys may be named in any
-// order that both operands share, so a lane reads 16 bytes of a key and 16 channels' worth of a value at a time.
-// The keys of the next step are asked for when those of this one are multiplied, the values when the scores are, so that either has half
-// a step to arrive, without other registers.  Heads are padded to HD channels, the padding is neither read nor written.
+// A workgroup takes sixteen rows of (position, query head) of a kv head, or two times sixteen, and its four wavefronts a quarter each of
+// the keys they see, sixteen at a time (bf16: two times sixteen), straight from the pages into registers; their sums are added
+// through the LDS.  Both products are computed transposed, as in kv_decode.hip: S^T = K Q^T leaves scores of keys 4 g + r (g = lane / 16)
+// of row lane % 16 in a lane, which is what O^T = V^T P^T takes as its second operand - for fp32 v_mfma_f32_16x16x4_f32, whose
+// products and sums are fp32's, register by register; for bf16 v_mfma_f32_16x16x32_bf16 with a weight as two operands, its upper digits
+// and what they leave.  Channels and keys may be named in any order that both operands share, so a lane reads 16 bytes of a key and
+// 16 channels' worth of a value at a time.  The keys of the next step are asked for when those of this one are multiplied,
+// the values when the step begins.  Heads are padded to HD channels, the padding is neither read nor written.
+//
+// 5 ragged fp32 prompts, 2462 rows of 16 heads of 64 with a window of 300: 49 to 52 us, of which the matrix instructions are 18 (at 154
+// TFLOP/s).  A step of a wavefront takes 1.35 times its matrix instructions' time, and 20 us go before the first: the chain from
+// the samples' starts over page numbers and addresses to the first keys, twice, as each compute unit is given five workgroups and
+// holds three.  A wavefront for every sixteen rows (and no sums to add) took 57, 32 rows of it 60, VALU products 240 to 263.  16 tokens
+// behind 3000 of the 7B shape in fp32: 263 us, 6.0 TB/s.
 #include <algorithm>
 #include <cmath>
 
@@ -40,17 +46,19 @@ template <int HD> struct Query<bf16_t, HD> { u32x4 q[HD / 32]; };
 
 struct AnyGeo { int n_blocks, sets, g_sh, from; };
 
-// What a wavefront's rows see, 64 positions a block: as in kv_prompt_device.h.
-struct AnyBlocks { int sinks, n_sinks, first, from, end, n; };
-__device__ __forceinline__ AnyBlocks any_blocks(const KvSight& w, int at, int end) {
-  AnyBlocks b;
+// What the rows of a wavefront see, at positions at .. end - 1: the first sinks and from .. end - 1, counted in steps of T positions without
+// the steps between: place c is position c of the first `apart`, then c + shift (as KvSpan of one row).  64 places are a block.
+struct AnySpan { int sinks, apart, shift, from, end, steps; };
+template <int T>
+__device__ __forceinline__ AnySpan any_span(const KvSight& w, int at, int end) {
+  AnySpan b;
   b.end = end;
   b.from = max(at + 1 - w.window, 0);
   b.sinks = min(w.sinks, b.from);
-  const int s64 = (b.sinks + 63) >> 6, f64 = b.from >> 6;
-  b.n_sinks = s64 < f64 ? s64 : 0;
-  b.first = b.n_sinks || b.sinks == 0 ? f64 << 6 : 0;
-  b.n = b.n_sinks + ((end - b.first + 63) >> 6);
+  const int first = (b.sinks + T - 1) & -T, second = b.from & -T;
+  b.apart = first < second ? first : 0;
+  b.shift = first < second ? second - first : 0;
+  b.steps = (end - b.shift + T - 1) / T;
   return b;
 }
 
@@ -59,8 +67,12 @@ template <typename T, int HD, int S, bool kTokens, bool kMany>
 __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCache c, KvRows r, KvAttn a, AnyGeo geo) {
   typedef Step<T, HD> St;
   constexpr int kKeyStep = 64 / sizeof(T);                       // channels of a key that the four lanes with it read at once
-  constexpr int VB = St::VB, KU = St::KU, NG = St::kGroups, KT = 16 * NG, kTiles = 64 / KT;
-  __shared__ long list[kWaves][2][64];                           // rows of the cache of a block's keys, and of the next one's
+  constexpr int VB = St::VB, KU = St::KU, NG = St::kGroups, KT = 16 * NG, kSteps = 64 / KT;
+  constexpr int VP = VB < 4 ? VB : 4, kRow = 16 * VP + 4;         // channels of a lane's VB that are added at a time
+  __shared__ long list[kWaves][2][64];                           // rows of the cache of 64 places, and of the next ones
+  __shared__ float sums[kWaves][16 * S][kRow];
+  __shared__ float2 marks[kWaves][16 * S];
+  __shared__ int items[16 * S];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4, h = c.h;
   const T* const data = (const T*)c.data;
@@ -69,8 +81,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
   int which, kv, first_pos, last_pos;                            // of the wavefront's rows
   bool none = false;                                             // the sample takes no part
   if constexpr (kTokens) {
-    const int G = a.H / c.K, groups = kv8_groups(c, a.H), unit = blockIdx.x * kWaves + wave, sample = unit / (c.K * groups), rest = unit - sample * (c.K * groups);
-    if (sample >= r.n) return;
+    const int G = a.H / c.K, groups = kv8_groups(c, a.H), unit = blockIdx.x, sample = unit / (c.K * groups), rest = unit - sample * (c.K * groups);
     kv = rest / groups;
     const int head0 = kv * G + 16 * (rest - kv * groups), heads = min(16, kv * G + G - head0);
     const int seen = __builtin_amdgcn_readfirstlane(kv8_seen(c, r, sample));
@@ -79,12 +90,11 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
     first_pos = last_pos = seen - 1;
     sample_row[0] = sample; head[0] = head0 + min(col, heads - 1); pos[0] = seen - 1; live[0] = col < heads;
   } else {
-    const int x = kMany ? geo.from + blockIdx.x : blockIdx.x, block = x / geo.sets, set = x - block * geo.sets, g_sh = geo.g_sh, bp = 16 * S * kWaves >> g_sh;
+    const int x = kMany ? geo.from + blockIdx.x : blockIdx.x, block = x / geo.sets, set = x - block * geo.sets, g_sh = geo.g_sh, bp = 16 * S >> g_sh;
     const BlockPlace at = place_of<kMany>(r, block, bp);
     if (at.sample < 0) return;
     // (a sample's longest rows first)
-    const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp + (16 * S * wave >> g_sh), head0 = set << g_sh, end = min(q0 + (16 * S >> g_sh), at.rows);
-    if (q0 >= at.rows) return;
+    const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp, head0 = set << g_sh, end = min(q0 + bp, at.rows);
     kv = head0 / (a.H / c.K);
     which = kv8_checked_row(c, at.table);
     none = at.pos < 0 || which < 0;
@@ -104,7 +114,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
   }
   auto item_of = [&](int u) { return sample_row[u] * a.H + head[u]; };
   if (none) {
-    if (blockIdx.y == 0)
+    if (blockIdx.y == 0 && wave == 0)
 #pragma unroll
       for (int u = 0; u < S; ++u) {
         if (!live[u]) continue;
@@ -115,9 +125,11 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
     return;
   }
   const int32_t* const table = c.tables + (long)which * c.table_stride;
-  const AnyBlocks kb = any_blocks(a.sight, first_pos, last_pos + 1);
-  const int b_lo = blockIdx.y * a.plan.chunk, b_hi = (int)min((long)kb.n, (long)b_lo + a.plan.chunk), pieces = (kb.n + a.plan.chunk - 1) / a.plan.chunk;
-  if (b_lo >= b_hi) return;
+  const AnySpan kb = any_span<KT>(a.sight, first_pos, last_pos + 1);
+  const int blocks = (kb.steps + kSteps - 1) / kSteps, pieces = (blocks + a.plan.chunk - 1) / a.plan.chunk;
+  const int p_lo = kSteps * blockIdx.y * a.plan.chunk, p_hi = (int)min((long)kb.steps, (long)p_lo + kSteps * (long)a.plan.chunk);   // of the piece
+  if (p_lo >= p_hi) return;
+  const int lo = p_lo + (int)((long)(p_hi - p_lo) * wave / kWaves), hi = p_lo + (int)((long)(p_hi - p_lo) * (wave + 1) / kWaves);   // of the wavefront
 
   // queries: channels 16 s + 4 g + 0..3 (bf16: 32 s + 8 g + 0..7), as the keys'
   Query<T, HD> q[S];
@@ -140,11 +152,11 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
     for (int b = 0; b < VB; ++b) o[u][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A position that no row of the wavefront sees stands for one near it that some row sees; lane i looks up key i of a block.
-  auto start_of = [&](int b) __attribute__((always_inline)) { return b < kb.n_sinks ? b << 6 : kb.first + ((b - kb.n_sinks) << 6); };
+  // A position that no row of the workgroup sees stands for one near it that some row sees; lane i looks up place i of 64 from step lo on.
+  auto position = [&](int place) __attribute__((always_inline)) { return place + (place >= kb.apart ? kb.shift : 0); };
   auto key_at = [&](int b) __attribute__((always_inline)) {
-    const int k0 = start_of(min(b, b_hi - 1)), p = k0 + lane;
-    return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
+    const int place = KT * lo + 64 * b + lane, p = position(place);
+    return min(p < kb.sinks || p >= kb.from ? p : place < kb.apart ? kb.sinks - 1 : kb.from, kb.end - 1);
   };
   auto page_at = [&](int b) __attribute__((always_inline)) { return table[kv8_page_of(c, key_at(b))]; };
   auto note = [&](int b, int page) __attribute__((always_inline)) { list[wave][b & 1][lane] = kv8_row(c, kv8_checked_page(c, page), kv, key_at(b)) * h; };
@@ -199,17 +211,18 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
       }
   };
 
-  note(b_lo, page_at(b_lo));
-  int page = page_at(b_lo + 1);
+  if (lo < hi) {
+  note(0, page_at(0));
+  int page = page_at(1);
   wrote();
-  ask_keys(b_lo, 0);
-  for (int b = b_lo; b < b_hi; ++b) {
+  ask_keys(0, 0);
+  for (int b = 0; lo + kSteps * b < hi; ++b) {
     note(b + 1, page);
     page = page_at(b + 2);
     wrote();
-    const int k0 = start_of(b);
-    for (int t = 0; t < kTiles; ++t) {
-      const int kt = k0 + KT * t;
+    const int steps = min(kSteps, hi - lo - kSteps * b);
+    for (int t = 0; t < steps; ++t) {
+      const int kt = position(KT * lo + 64 * b + KT * t);
       ask_values(b, t);
       __builtin_amdgcn_sched_barrier(0);
       if (h != HD)
@@ -241,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
         }
       __builtin_amdgcn_sched_barrier(0);
       // (behind the last step's keys nothing that is used)
-      ask_keys(t + 1 < kTiles ? b : b + 1, t + 1 < kTiles ? t + 1 : 0);
+      ask_keys(t + 1 < steps ? b : b + 1, t + 1 < steps ? t + 1 : 0);
       __builtin_amdgcn_sched_barrier(0);
       float weight[S][4 * NG];
       const bool whole = kt + KT - 1 <= first_pos && (kt > last_pos - a.sight.window || kt + KT <= a.sight.sinks);   // all keys are for all rows
@@ -321,6 +334,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
     }
   }
 
+  }
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
   // are computed once more, each by itself.  (Weights that are no numbers are what they should be.)
   float odd = 0.f;
@@ -336,76 +350,99 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
       for (int j = 0; j < 4; ++j) odd = fmaf(o[u][v][j], 0.f, odd);
     spoiled |= !(odd == 0.f) && l[u] - l[u] == 0.f;
   }
-  if (__builtin_expect(__any(spoiled), 0)) {
+  if (wave == 0 && g == 0)
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      items[16 * u + col] = live[u] ? item_of(u) : -1;
+      if (live[u] && a.plan.splits > 1 && blockIdx.y == 0) kv_part_counts(a, c, r)[item_of(u)] = pieces;
+    }
+  if (__builtin_expect(__syncthreads_or(spoiled), 0)) {
     int L = 1;
     while (8 * L < h) L *= 2;
-    const int ch = 8 * (lane & (L - 1)), shift = kb.first - 64 * kb.n_sinks;
+    const int ch = 8 * (lane & (L - 1));
+#pragma unroll
     for (int u = 0; u < S; ++u)
-      for (int i = 0; i < 16; ++i) {
-        if (!__shfl((int)(u == 0 ? live[0] : live[S - 1]), i, 64)) continue;
-        const int row1 = __shfl(u == 0 ? sample_row[0] : sample_row[S - 1], i, 64), head1 = __shfl(u == 0 ? head[0] : head[S - 1], i, 64),
-                  end1 = __shfl(u == 0 ? pos[0] : pos[S - 1], i, 64) + 1, from1 = max(end1 - a.sight.window, 0), item1 = row1 * a.H + head1;
-        const KvSpan span{min(a.sight.sinks, from1), 64 * kb.n_sinks, shift, from1, end1};
+      for (int i = wave; i < 16; i += kWaves) {
+        if (!__shfl((int)live[u], i, 64)) continue;
+        const int row1 = __shfl(sample_row[u], i, 64), head1 = __shfl(head[u], i, 64), end1 = __shfl(pos[u], i, 64) + 1, from1 = max(end1 - a.sight.window, 0),
+                  item1 = row1 * a.H + head1;
+        const KvSpan span{min(a.sight.sinks, from1), kb.apart, kb.shift, from1, end1};
         float x[8] = {};
         if (ch < h) KvType<T>::load8((const T*)a.q + (long)row1 * a.q_stride + (long)head1 * h + ch, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= a.scale;
-        const KvSums sums = kv_attend<T>(c, table, kv, span, x, L, ch, ch < h, 64 * b_lo, 64 / L, min(64 * b_hi, end1 - shift));
+        const KvSums one = kv_attend<T>(c, table, kv, span, x, L, ch, ch < h, KT * p_lo, 64 / L, min(KT * p_hi, end1 - kb.shift));
         if (lane >= L || ch >= h) continue;
         T* const out = (T*)a.out + (long)row1 * a.out_stride + (long)head1 * h + ch;
         float* const part = kv_part_sums(a, c, item1, blockIdx.y) + ch;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (pieces == 1) Storage<T>::put(out + e, sums.o[e] / sums.l);
-          else part[e] = sums.o[e];
-        if (lane == 0 && pieces > 1) *kv_part_marks(a, c, r, item1, blockIdx.y) = make_float2(sums.m, sums.l);
-        if (lane == 0 && blockIdx.y == 0 && a.plan.splits > 1) kv_part_counts(a, c, r)[item1] = pieces;
+          if (pieces == 1) Storage<T>::put(out + e, one.o[e] / one.l);
+          else part[e] = one.o[e];
+        if (lane == 0 && pieces > 1) *kv_part_marks(a, c, r, item1, blockIdx.y) = make_float2(one.m, one.l);
       }
     return;
   }
-  // lane (col, g) has channels VB (4 g + j) + v of its column in o[v][j]
+  // Lane (col, g) has channels VB (4 g + j) + v of its rows in o[v][j].  The wavefronts' sums are added, VP of the VB at a time, always in
+  // the same order.
 #pragma unroll
-  for (int u = 0; u < S; ++u) {
-    if (!live[u]) continue;
-    const int item = item_of(u);
-    if (a.plan.splits > 1 && blockIdx.y == 0 && g == 0) kv_part_counts(a, c, r)[item] = pieces;
-    const float inv = 1.f / l[u];
-    T* const out = (T*)a.out + (long)sample_row[u] * a.out_stride + (long)head[u] * h;
-    float* const part = kv_part_sums(a, c, item, blockIdx.y);
+  for (int v0 = 0; v0 < VB; v0 += VP) {
+    if (v0) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int u = 0; u < S; ++u) {
+      if (v0 == 0 && g == 0) marks[wave][16 * u + col] = make_float2(m[u], l[u]);
 #pragma unroll
-      for (int v = 0; v < VB; ++v) {
-        const int ch = VB * (4 * g + j) + v;
-        if (ch >= h) continue;
-        if (pieces == 1) Storage<T>::put(out + ch, o[u][v][j] * inv);
-        else part[ch] = o[u][v][j];
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int v = 0; v < VP; ++v) sums[wave][16 * u + col][VP * (4 * g + j) + v] = o[u][v0 + v][j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      const int row = 16 * u + (threadIdx.x >> 4), ch = VB * (threadIdx.x & 15) + v0, item = items[row];
+      float f[kWaves], to = kKvNone, sum = 0.f, x[VP] = {};
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) to = fmaxf(to, marks[i][row].x);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        f[i] = exp2_raw(marks[i][row].x - to);
+        sum += marks[i][row].y * f[i];
+#pragma unroll
+        for (int v = 0; v < VP; ++v) x[v] = fmaf(sums[i][row][VP * (threadIdx.x & 15) + v], f[i], x[v]);
       }
-    if (pieces > 1 && g == 0) *kv_part_marks(a, c, r, item, blockIdx.y) = make_float2(m[u], l[u]);
+      if (item < 0) continue;
+      if (pieces == 1) {
+        const int at = item / a.H;
+        T* const out = (T*)a.out + (long)at * a.out_stride + (long)(item - at * a.H) * h + ch;
+        const float inv = 1.f / sum;
+#pragma unroll
+        for (int v = 0; v < VP; ++v)
+          if (ch + v < h) Storage<T>::put(out + v, x[v] * inv);
+      } else {
+        float* const part = kv_part_sums(a, c, item, blockIdx.y) + ch;
+#pragma unroll
+        for (int v = 0; v < VP; ++v)
+          if (ch + v < h) part[v] = x[v];
+        if (ch == 0) *kv_part_marks(a, c, r, item, blockIdx.y) = make_float2(to, sum);
+      }
+    }
   }
 }
 
-// Rows of a workgroup: S sets of sixteen for each of four wavefronts; two sets where they fit into the registers of two wavefronts a SIMD.
-template <typename T> constexpr int sets_of(int padded) { return padded * sizeof(T) <= 256 ? 2 : 1; }
 int padded(int h) { return h <= 32 ? 32 : h <= 64 ? 64 : h <= 128 ? 128 : 256; }
+// How many sets of sixteen rows a wavefront may have: two where they fit into the registers of two wavefronts a SIMD.
+template <typename T> constexpr int most_sets(int padded) { return padded * sizeof(T) <= 256 ? 2 : 1; }
+int most_sets(const KvCache& c) { return c.dtype == MDI_BF16 ? most_sets<bf16_t>(padded(c.h)) : most_sets<float>(padded(c.h)); }
 
-int sets_of(const KvCache& c) { return c.dtype == MDI_BF16 ? sets_of<bf16_t>(padded(c.h)) : sets_of<float>(padded(c.h)); }
-
-AnyGeo geo_of(const KvCache& c, const KvRows& r, int H) {
-  const int rows = 16 * sets_of(c) * kWaves, sh = std::min(kv_heads_shift(c, H), 4), bp = rows >> sh;   // (a wavefront's sixteen are a multiple of 2^sh)
+AnyGeo geo_of(const KvCache& c, const KvRows& r, int H, int sets) {
+  const int rows = 16 * sets, sh = std::min(kv_heads_shift(c, H), 4), bp = rows >> sh;   // (a wavefront's sixteen are a multiple of 2^sh)
   return AnyGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
 }
 
 constexpr int kMostWgs = 1 << 22;    // of a launch: it has fewer than 2^32 threads
-template <typename T, int HD>
-void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  constexpr int S = sets_of<T>(HD);
-  if (!r.start) {
-    const long units = (long)r.n * c.K * kv8_groups(c, a.H);     // (below 2^24: n_rows * H is)
-    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)((units + kWaves - 1) / kWaves), a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, AnyGeo{});
-    return;
-  }
-  AnyGeo g = geo_of(c, r, a.H);
+template <typename T, int HD, int S>
+void launch_sets(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  AnyGeo g = geo_of(c, r, a.H, S);
   const int total = g.n_blocks * g.sets;
   if (r.n <= kInOrder) {
     hipLaunchKernelGGL((k_kv_any<T, HD, S, false, false>), dim3(total, a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, g);
@@ -413,6 +450,16 @@ void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn
   }
   for (; g.from < total; g.from += kMostWgs)
     hipLaunchKernelGGL((k_kv_any<T, HD, S, false, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, g);
+}
+template <typename T, int HD>
+void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
+  if (!r.start) {
+    const long units = (long)r.n * c.K * kv8_groups(c, a.H);     // (below 2^24: n_rows * H is)
+    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)units, a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, AnyGeo{});
+    return;
+  }
+  if constexpr (most_sets<T>(HD) == 2) if (a.plan.groups == 2) return launch_sets<T, HD, 2>(s, c, r, a);
+  launch_sets<T, HD, 1>(s, c, r, a);
 }
 template <typename T>
 void launch_type(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
@@ -426,16 +473,18 @@ void launch_type(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
 
 }  // namespace
 
-// Pieces of a row's blocks: so many wavefronts that every SIMD has two, if there are blocks for them; more pieces than that have to be
-// added again.
+// Two sets of sixteen rows a workgroup read the keys and values half as often, one set is twice as many workgroups: two from 512
+// workgroups on (fp32, 12 heads of 64: 1600 rows 47 against 50 us, 800 rows 29 against 22; bf16 heads of 96: 1600 rows 31 against 34, 800
+// rows 18 against 17).  Pieces only while there is no workgroup for every compute unit, of four blocks or more: 16 fp32 tokens behind
+// 3000 of the TinyLlama shape in 1 piece 40 us, in 2 28, in 4 - a workgroup for each - 23, in 16 26; 2633 rows of it in 1 piece 170, in 2 181.
 KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  const int S = r.start ? sets_of(c) : 1, sh = std::min(kv_heads_shift(c, H), 4), bp = 16 * S >> sh;   // positions of a wavefront
-  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;
-  const double waves = r.start ? (double)n * ((rows + bp - 1) / bp) * (H >> sh) : (double)r.n * c.K * kv8_groups(c, H);
-  const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + (r.start ? bp : 1) + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);   // blocks of a wavefront
-  const int want = (int)std::min(64., std::max(1., std::min(most / 2., std::ceil(2048. / waves))));
-  const int chunk = (int)((most + want - 1) / want);
-  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, 0};
+  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n, sh = std::min(kv_heads_shift(c, H), 4);
+  auto wgs_of = [&](int sets) { const int bp = 16 * sets >> sh; return (double)n * ((rows + bp - 1) / bp) * (H >> sh); };
+  const int sets = r.start && most_sets(c) == 2 && wgs_of(2) >= 512. ? 2 : 1;
+  const double wgs = r.start ? wgs_of(sets) : (double)r.n * c.K * kv8_groups(c, H);
+  const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + (r.start ? 16 * sets >> sh : 1) + w.sinks + 4 * 31 + 63) / 64);   // blocks of 64 places
+  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(256. / wgs)))), chunk = (int)((most + want - 1) / want);
+  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, sets};
 }
 
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
