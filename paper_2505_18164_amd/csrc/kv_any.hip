@@ -477,14 +477,20 @@ void launch_type(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
 // workgroups on (fp32, 12 heads of 64: 1600 rows 47 against 50 us, 800 rows 29 against 22; bf16 heads of 96: 1600 rows 31 against 34, 800
 // rows 18 against 17).  Pieces only while there is no workgroup for every compute unit, of four blocks or more: 16 fp32 tokens behind
 // 3000 of the TinyLlama shape in 1 piece 40 us, in 2 28, in 4 - a workgroup for each - 23, in 16 26; 2633 rows of it in 1 piece 170, in 2 181.
-KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
+KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us) {
   const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n, sh = std::min(kv_heads_shift(c, H), 4);
   auto wgs_of = [&](int sets) { const int bp = 16 * sets >> sh; return (double)n * ((rows + bp - 1) / bp) * (H >> sh); };
-  const int sets = r.start && most_sets(c) == 2 && wgs_of(2) >= 512. ? 2 : 1;
+  const int sets = r.start && most_sets(c) == 2 && rows << sh > 16 && wgs_of(2) >= 512. ? 2 : 1;
   const double wgs = r.start ? wgs_of(sets) : (double)r.n * c.K * kv8_groups(c, H);
-  const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + (r.start ? 16 * sets >> sh : 1) + w.sinks + 4 * 31 + 63) / 64);   // blocks of 64 places
-  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(256. / wgs)))), chunk = (int)((most + want - 1) / want);
-  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, sets};
+  const int reach = (int)std::min<long>(r.max_ctx, (long)w.window + (r.start ? 16 * sets >> sh : 1) + w.sinks + 4 * 31);   // places of a workgroup
+  const int most = (reach + 63) / 64;
+  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(256. / wgs)))), chunk = (most + want - 1) / want, splits = (most + chunk - 1) / chunk;
+  // 128 keys of a workgroup's rows take `step` us of a compute unit, a workgroup some more to begin and end
+  const bool wide = c.h > 64;
+  const double seen = std::min<double>(reach, r.max_ctx - 0.5 * std::min(r.max_ctx, rows)), step = sets == 2 ? (wide ? 1.35 : 0.8) : (wide ? 0.9 : 0.5);
+  *us = std::max(3 + std::ceil(reach / (128. * splits)), wgs * (seen / 128 * step + splits * (wide ? 3.5 : 2.2)) / 256);
+  if (splits > 1) *us += 2 + (double)r.n_rows * H * (1 / 2000. + splits * (double)c.h / 4e6);
+  return KvPlan{kKvAny, chunk, splits, 0, sets};
 }
 
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

@@ -32,7 +32,8 @@ inline int kv_most_seen(const KvSight& w, int max_ctx) { return (int)std::min<lo
 // finished where it is computed; of the others every piece leaves its h weighted sums, its reference and its sum of
 // weights, which a second launch adds.  How many pieces a row and head has is left by whoever computes the first one.
 // wgs > 0 (kv_decode.hip): the cut is another, all samples' places in equal shares for so many workgroups, of at least `chunk`.
-struct KvPlan { int chunk, splits, wgs, groups; };   // chunk: places, or (kv_prompt.hip) blocks of 64; groups: kv_prompt.hip's, of wavefronts in a workgroup; kv_any.hip's, of sixteen rows
+enum KvKernel { kKvDecode, kKvPrompt, kKvAny };
+struct KvPlan { KvKernel kernel; int chunk, splits, wgs, groups; };   // chunk: places, or (kv_prompt.hip) blocks of 64; groups: kv_prompt.hip's, of wavefronts in a workgroup; kv_any.hip's, of sixteen rows
 inline size_t kv_part_bytes(const KvPlan& p, const KvCache& c, const KvRows& r, int H) {
   return p.splits > 1 ? (size_t)r.n_rows * H * (p.splits * (size_t)(c.h + 2) + 1) * sizeof(float) : 0;
 }
@@ -50,10 +51,11 @@ void launch_kv_decode(hipStream_t s, const KvCache& c, const KvRows& r, const Kv
 // Packed rows in bf16 with heads of 64 or 128: on the matrix cores (kv_prompt.hip).  kv_allow_lds: before the first launch on the current device.
 bool kv_prompt_supported(const KvCache& c, const KvRows& r);
 bool kv_allow_lds();
-KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
+KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us);
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
-// The others, also on the matrix cores (kv_any.hip).
-KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
+// Any other, also on the matrix cores, and few packed rows (kv_any.hip).  us: what the call should take, without its launches; of
+// single tokens it is not asked for.
+KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us);
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);

@@ -354,12 +354,11 @@ PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int WQ) {
 }
 // Groups of a workgroup and pieces of a row's blocks.  A step of 64 NG keys takes `step` us, a workgroup some more to begin
 // and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are taken for equal.
-struct PromptPlan { int groups, splits; };
+struct PromptPlan { int groups, splits; double us; };
 PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
   const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
   const double heads = (double)r.n_rows * H;
-  PromptPlan best{1, 1};
-  double best_us = 1e30;
+  PromptPlan best{1, 1, 1e30};
   for (int ng = 1; ng <= 2; ++ng) {
     const int sh = kv_heads_shift(c, H), bp = 256 / ng >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, rows) + 64);
     const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.0 : 2.25) : (ng == 1 ? 1.35 : 1.55);
@@ -369,7 +368,7 @@ PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& 
       const double longest = std::ceil(most / (64. * ng * s)), all = items * seen / (64. * ng * 256);
       double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
       if (s > 1) us += 2 + heads / 2000 + heads * s * c.h / 4e6;
-      if (us < best_us) { best_us = us; best = PromptPlan{ng, s}; }
+      if (us < best.us) best = PromptPlan{ng, s, us};
     }
   }
   return best;
@@ -393,13 +392,14 @@ bool kv_allow_lds() {
   return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_one<2, true, false>() && allow_one<2, false, false>() && allow_one<2, true, true>() && allow_one<2, false, true>() && kv_wide_allow_lds(); });
 }
 
-KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
+KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us) {
   const PromptPlan p = prompt_plan(c, r, H, w);
   // blocks that a workgroup of up to `bp` positions may have: of the first ones, and of a window that begins inside one
   const int bp = 256 / p.groups >> kv_heads_shift(c, H);
   const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
   const int chunk = (int)((most + p.splits - 1) / p.splits);
-  return KvPlan{chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
+  *us = p.us;
+  return KvPlan{kKvPrompt, chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
 }
 
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

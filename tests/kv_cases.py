@@ -119,7 +119,8 @@ class Setup:
         self.start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
         self.pos = np.asarray(behind, dtype=np.int32)
         self.max_ctx = max(max(total), 1)
-        self.q = torch.from_numpy(rng.standard_normal((self.rows, H, h)).astype(np.float32)).to(dtype)
+        q = torch.from_numpy(rng.standard_normal((sum(lens) + min(rows_behind, 3), H, h)).astype(np.float32)).to(dtype)
+        self.q = torch.cat([q, torch.zeros((self.rows - q.shape[0], H, h), dtype=dtype)])
 
     def cache(self, err=True):
         self.err = torch.zeros(1, dtype=torch.int32, device="cuda:0") if err else None
