@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
 
   // A row's reference is the largest score of the first keys that it sees.  Where later ones would have weights of more than
   // kFarSum the reference is raised, but not the sums so far: then all is done once more, from the references that the first time
-  // ended with, which nothing exceeds.  (A rescaling would have the sums in registers that vector instructions reach, and copied
+  // ended with, which nothing exceeds as far.  (A rescaling would have the sums in registers that vector instructions reach, and copied
   // there and back around every step.)
   bool once_more = false;
   // Step i = 2 j + t: scores sn of step i + 1 (operands there), weights pn of step i from its scores sc, and the values of step i - 1
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[u][e]);
         top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;       // both lanes of a row raise alike
-        const float to = fmaxf(m[u], top);
+        const float to = top > m[u] + 25.f ? top : m[u];         // (32 weights of up to 2^25 are no more than kFarSum: other rows' references stay)
         once_more |= to > m[u] && m[u] != kKvNone;
         m[u] = to;
         sum[u] = 0.f;
