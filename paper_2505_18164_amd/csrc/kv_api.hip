@@ -1,4 +1,4 @@
-// The entry points of the cache in the storage type (mdi_kv_* of mdi.h): checks on the host, then the launches (two at most).
+// The entry points of the cache in the storage type (mdi_kv_* of mdi.h): checks on the host, then the launches: one or two, of very many samples a few.
 #include <algorithm>
 
 #include "kv_internal.h"

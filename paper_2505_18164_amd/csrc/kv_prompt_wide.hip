@@ -5,7 +5,12 @@
 // second wavefront on the SIMD did, exponentials while the first multiplies, the wavefront does itself: in step i, of 32
 // keys, it multiplies the keys of step i + 1 and the values of step i - 1 and in between weighs the scores of step i, three vector
 // instructions behind every matrix instruction.  Everything of a step is in registers (the operands of the next are read
-// meanwhile), some 400 of them.
+// meanwhile), some 400 of them.  (Weights are rounded to bf16: see kv_prompt.hip.)
+//
+// Prompts of 6000, 2000 and 500 of the 8B shape 347 us, 0.96 PFLOP/s; with a window of 1024 of the 7B shape 213 to 231, where a workgroup
+// passes over 1280 keys for rows that see 1024 each, and begins and ends in 6 us for every 40.  (The products of kv_prompt.hip, with heads
+// of 128: 380 and 215 to 231; in vector instructions 25 ms and 9 ms.)  Of the 347 us the matrix instructions alone take 248 to 260 -
+// with these data; with zeros the whole takes 336 -, with the softmax 314, with the reads of the LDS 331.
 #include <type_traits>
 
 #include "kv_prompt_device.h"
