@@ -144,14 +144,14 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv_decode(KvCache c, KvRows 
       }
     };
     auto use = [&](Tile<HD>& t, int base) __attribute__((always_inline)) {
-      f32x4 s[2];
-      float p[2][4];
+      float s[2][4], p[2][4];                                     // (scalars: hipcc has lost elements of a vector of which one was replaced under a condition)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < KI; ++i) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[u][i]), qf[i], s[u], 0, 0, 0);
-        s[u] *= a.scale;
+        for (int i = 0; i < KI; ++i) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[u][i]), qf[i], x, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[u][j] = x[j] * a.scale;
       }
       const int p0 = span.position(base);                         // (32 places from here on lie next to each other, or the second 16 behind the gap)
       if (!(p0 + 31 < span.sinks || (base >= span.sinks16 && p0 >= span.from && p0 + 31 < span.end))) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv_decode(KvCache c, KvRows 
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (!span.sees(span.position(base + 16 * u) + 4 * g + j)) s[u][j] = -INFINITY;
+            s[u][j] = span.sees(span.position(base + 16 * u) + 4 * g + j) ? s[u][j] : -INFINITY;
       }
       float top = -INFINITY;
 #pragma unroll

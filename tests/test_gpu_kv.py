@@ -200,6 +200,17 @@ def test_one_new_token_against_64_bits(case, sight, dtype):
     cache.check()
 
 
+@pytest.mark.parametrize("sight", SIGHTS, ids=[f"{w}+{s}" for w, s in SIGHTS])
+@pytest.mark.parametrize("H,K,h,pt", [(8, 2, 64, 16), (6, 3, 64, 40), (4, 2, 128, 64), (10, 2, 128, 7)])
+def test_one_new_token_of_what_may_be_a_large_cache(H, K, h, pt, sight):
+    """Tables for so many positions that the cache is read as a large one, with and without a window that makes it a small one after all."""
+    ctx = [1, 17, 300, 0, 64, 1000]
+    s = Setup(H, K, h, pt, [1] * 6, [max(c, 1) - 1 for c in ctx], BF16, *sight, seed=4, spare=150000 // pt)
+    cache = s.cache()
+    s.check(s.attn(cache, s.plan(cache, one_each=True, max_ctx=150000)))
+    cache.check()
+
+
 @pytest.mark.parametrize("dtype", **TYPES)
 @pytest.mark.parametrize("one_each", [False, True], ids=["packed", "tokens"])
 @pytest.mark.parametrize("sight", [(0, 0), (1700, 100)], ids=["all", "window"])
