@@ -212,127 +212,127 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
   };
 
   if (lo < hi) {
-  note(0, page_at(0));
-  int page = page_at(1);
-  wrote();
-  ask_keys(0, 0);
-  for (int b = 0; lo + kSteps * b < hi; ++b) {
-    note(b + 1, page);
-    page = page_at(b + 2);
+    note(0, page_at(0));
+    int page = page_at(1);
     wrote();
-    const int steps = min(kSteps, hi - lo - kSteps * b);
-    for (int t = 0; t < steps; ++t) {
-      const int kt = position(KT * lo + 64 * b + KT * t);
-      ask_values(b, t);
-      __builtin_amdgcn_sched_barrier(0);
-      if (h != HD)
+    ask_keys(0, 0);
+    for (int b = 0; lo + kSteps * b < hi; ++b) {
+      note(b + 1, page);
+      page = page_at(b + 2);
+      wrote();
+      const int steps = min(kSteps, hi - lo - kSteps * b);
+      for (int t = 0; t < steps; ++t) {
+        const int kt = position(KT * lo + 64 * b + KT * t);
+        ask_values(b, t);
+        __builtin_amdgcn_sched_barrier(0);
+        if (h != HD)
 #pragma unroll
-        for (int s = 0; s < KU; ++s)
-          if (kKeyStep * s + kKeyStep / 4 * g >= h)
+          for (int s = 0; s < KU; ++s)
+            if (kKeyStep * s + kKeyStep / 4 * g >= h)
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-              if constexpr (sizeof(T) == 4) st.k[s] = f32x4{}; else st.k[n][s] = u32x4{};
-            }
-      f32x4 s[S][NG];
-#pragma unroll
-      for (int u = 0; u < S; ++u)
-#pragma unroll
-        for (int n = 0; n < NG; ++n) s[u][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < KU; ++i)
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int u = 0; u < S; ++u) s[u][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][e], q[u].q[i][e], s[u][0], 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int n = 0; n < NG; ++n)
-#pragma unroll
-            for (int u = 0; u < S; ++u)
-              s[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, st.k[n][i]), __builtin_bit_cast(bf16x8, q[u].q[i]), s[u][n], 0, 0, 0);
-        }
-      __builtin_amdgcn_sched_barrier(0);
-      // (behind the last step's keys nothing that is used)
-      ask_keys(t + 1 < steps ? b : b + 1, t + 1 < steps ? t + 1 : 0);
-      __builtin_amdgcn_sched_barrier(0);
-      float weight[S][4 * NG];
-      const bool whole = kt + KT - 1 <= first_pos && (kt > last_pos - a.sight.window || kt + KT <= a.sight.sinks);   // all keys are for all rows
-#pragma unroll
-      for (int u = 0; u < S; ++u) {
-        // (from here on scalars: hipcc lost elements of a vector of which one was replaced under a condition)
-        float x[4 * NG], top;
-#pragma unroll
-        for (int i = 0; i < 4 * NG; ++i) x[i] = s[u][i >> 2][i & 3] * a.scale;
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 4 * NG; ++i) {
-            const int key = kt + 16 * (i >> 2) + 4 * g + (i & 3);
-            x[i] = (key <= pos[u]) & ((key > pos[u] - a.sight.window) | (key < a.sight.sinks)) ? x[i] : -INFINITY;
-          }
-        }
-        top = x[0];
-#pragma unroll
-        for (int i = 1; i < 4 * NG; ++i) top = fmaxf(top, x[i]);
-        // Weights are relative to m, which is raised - for all four lanes of a row alike - only when a score exceeds it by
-        // 2^kRaise: the sum is divided out at the end, so any reference near the largest score does.
-        if (__any(top > m[u] + kRaise)) {
-          top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float to = fmaxf(m[u], top), alpha = exp2_raw(m[u] - to);
-          m[u] = to;
-          l[u] *= alpha;
-#pragma unroll
-          for (int v = 0; v < VB; ++v) o[u][v] *= alpha;
-        }
-#pragma unroll
-        for (int i = 0; i < 4 * NG; ++i) {
-          weight[u][i] = exp2_raw(x[i] - m[u]);
-          l[u] += weight[u][i];
-        }
-      }
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int v = 0; v < VB; ++v)
-#pragma unroll
-            for (int u = 0; u < S; ++u) o[u][v] = __builtin_amdgcn_mfma_f32_16x16x4f32(st.v[j][v], weight[u][j], o[u][v], 0, 0, 0);
-      } else {
-        u32x4 hi_w[S];
-        bf16x8 lo_w[S];
+              for (int n = 0; n < NG; ++n) {
+                if constexpr (sizeof(T) == 4) st.k[s] = f32x4{}; else st.k[n][s] = u32x4{};
+              }
+        f32x4 s[S][NG];
 #pragma unroll
         for (int u = 0; u < S; ++u)
 #pragma unroll
-          for (int n = 0; n < NG; ++n)
+          for (int n = 0; n < NG; ++n) s[u][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-              const float w0 = weight[u][4 * n + j], w1 = weight[u][4 * n + j + 1];
-              hi_w[u][2 * n + j / 2] = high_halves(w0, w1);
-              lo_w[u][4 * n + j] = (__bf16)(w0 - __uint_as_float(__float_as_uint(w0) & 0xFFFF0000u));
-              lo_w[u][4 * n + j + 1] = (__bf16)(w1 - __uint_as_float(__float_as_uint(w1) & 0xFFFF0000u));
-            }
+        for (int i = 0; i < KU; ++i)
+          if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int w = 0; w < VB / 2; ++w) {
-          u32x4 f[2];
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                           // keys 4 g + 2 (i % 2), + 1 of group i / 2
-            const uint32_t lo_row = st.v[i >> 1][2 * (i & 1)][w], hi_row = st.v[i >> 1][2 * (i & 1) + 1][w];
-            f[0][i] = __builtin_amdgcn_perm(hi_row, lo_row, 0x05040100u);
-            f[1][i] = __builtin_amdgcn_perm(hi_row, lo_row, 0x07060302u);
+              for (int u = 0; u < S; ++u) s[u][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(st.k[i][e], q[u].q[i][e], s[u][0], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+              for (int u = 0; u < S; ++u)
+                s[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, st.k[n][i]), __builtin_bit_cast(bf16x8, q[u].q[i]), s[u][n], 0, 0, 0);
           }
+        __builtin_amdgcn_sched_barrier(0);
+        // (behind the last step's keys nothing that is used)
+        ask_keys(t + 1 < steps ? b : b + 1, t + 1 < steps ? t + 1 : 0);
+        __builtin_amdgcn_sched_barrier(0);
+        float weight[S][4 * NG];
+        const bool whole = kt + KT - 1 <= first_pos && (kt > last_pos - a.sight.window || kt + KT <= a.sight.sinks);   // all keys are for all rows
+#pragma unroll
+        for (int u = 0; u < S; ++u) {
+          // (from here on scalars: hipcc lost elements of a vector of which one was replaced under a condition)
+          float x[4 * NG], top;
+#pragma unroll
+          for (int i = 0; i < 4 * NG; ++i) x[i] = s[u][i >> 2][i & 3] * a.scale;
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4 * NG; ++i) {
+              const int key = kt + 16 * (i >> 2) + 4 * g + (i & 3);
+              x[i] = (key <= pos[u]) & ((key > pos[u] - a.sight.window) | (key < a.sight.sinks)) ? x[i] : -INFINITY;
+            }
+          }
+          top = x[0];
+#pragma unroll
+          for (int i = 1; i < 4 * NG; ++i) top = fmaxf(top, x[i]);
+          // Weights are relative to m, which is raised - for all four lanes of a row alike - only when a score exceeds it by
+          // 2^kRaise: the sum is divided out at the end, so any reference near the largest score does.
+          if (__any(top > m[u] + kRaise)) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float to = fmaxf(m[u], top), alpha = exp2_raw(m[u] - to);
+            m[u] = to;
+            l[u] *= alpha;
+#pragma unroll
+            for (int v = 0; v < VB; ++v) o[u][v] *= alpha;
+          }
+#pragma unroll
+          for (int i = 0; i < 4 * NG; ++i) {
+            weight[u][i] = exp2_raw(x[i] - m[u]);
+            l[u] += weight[u][i];
+          }
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int v = 0; v < VB; ++v)
+#pragma unroll
+              for (int u = 0; u < S; ++u) o[u][v] = __builtin_amdgcn_mfma_f32_16x16x4f32(st.v[j][v], weight[u][j], o[u][v], 0, 0, 0);
+        } else {
+          u32x4 hi_w[S];
+          bf16x8 lo_w[S];
 #pragma unroll
           for (int u = 0; u < S; ++u)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              f32x4& x = o[u][2 * w + e];
-              x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[e]), __builtin_bit_cast(bf16x8, hi_w[u]), x, 0, 0, 0);
-              x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[e]), lo_w[u], x, 0, 0, 0);
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+              for (int j = 0; j < 4; j += 2) {
+                const float w0 = weight[u][4 * n + j], w1 = weight[u][4 * n + j + 1];
+                hi_w[u][2 * n + j / 2] = high_halves(w0, w1);
+                lo_w[u][4 * n + j] = (__bf16)(w0 - __uint_as_float(__float_as_uint(w0) & 0xFFFF0000u));
+                lo_w[u][4 * n + j + 1] = (__bf16)(w1 - __uint_as_float(__float_as_uint(w1) & 0xFFFF0000u));
+              }
+#pragma unroll
+          for (int w = 0; w < VB / 2; ++w) {
+            u32x4 f[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                           // keys 4 g + 2 (i % 2), + 1 of group i / 2
+              const uint32_t lo_row = st.v[i >> 1][2 * (i & 1)][w], hi_row = st.v[i >> 1][2 * (i & 1) + 1][w];
+              f[0][i] = __builtin_amdgcn_perm(hi_row, lo_row, 0x05040100u);
+              f[1][i] = __builtin_amdgcn_perm(hi_row, lo_row, 0x07060302u);
             }
+#pragma unroll
+            for (int u = 0; u < S; ++u)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                f32x4& x = o[u][2 * w + e];
+                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[e]), __builtin_bit_cast(bf16x8, hi_w[u]), x, 0, 0, 0);
+                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[e]), lo_w[u], x, 0, 0, 0);
+              }
+          }
         }
       }
     }
-  }
 
   }
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows

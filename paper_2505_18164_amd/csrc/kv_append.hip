@@ -5,7 +5,7 @@
 // reduced there: in 32 it would be off by 2^-24 of itself, 0.007 at position 120000.  Everything else is binary32, rounded once.
 //
 // Memory bounds it, every row is read and written once: 8192 rows of the 7B shape with norms and rotation, 403 MB, 92 us, 4.4 TB/s (a large
-// copy reaches 4.9); 3514 rows of TinyLlama in fp32 with norms, 92 MB, 23 to 24 us.  16 rows of the 8B shape take 5.3 us of the
+// copy reaches 4.9); 4514 rows of TinyLlama in fp32 with norms, 92 MB, 23 to 24 us.  16 rows of the 8B shape take 5.3 us of the
 // GPU, most of them the way from a row to its sample, its page and the page's place, and 6.6 of the host.
 #include "kv_device.h"
 
@@ -47,7 +47,7 @@ template <int N> __device__ __forceinline__ void store(float* p, const float* x)
 
 // Results go out through the caches and inputs come in past them; a head's gains and biases are read once a workgroup, into the LDS (from
 // memory by every wavefront: 126 instead of 92 us for the 8192 rows).  fp32 rows are read 16 bytes a lane, lanes next to each
-// other: 32 bytes a lane, lanes 64 bytes apart, took 38 instead of 24 us for the 3514 rows.
+// other: 32 bytes a lane, lanes 64 bytes apart, took 38 instead of 24 us for the 4514 rows.
 //
 // A wavefront takes the head rows - queries, then keys, then values - of one row of the call, 64 / L at a time and U times.  A
 // lane holds 2 V channels of one: V that are rotated and their V partners, so that no other lane is needed, or 2 V that are not.  The
@@ -165,7 +165,7 @@ void launch_units(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppe
   const dim3 grid((unsigned)(((long)r.n_rows * pieces + kBlock / 64 - 1) / (kBlock / 64)));
   hipLaunchKernelGGL((k_kv_append<T, V, U>), grid, dim3(kBlock), 0, s, c, r, a, l_sh, pieces);
 }
-// Units of a wavefront: of 4, 3 and 2 the one that leaves the fewest of them without a head, of equals the larger.  (4 for all: 3514 rows
+// Units of a wavefront: of 4, 3 and 2 the one that leaves the fewest of them without a head, of equals the larger.  (4 for all: 4514 rows
 // of 40 fp32 heads of 64 25.6 instead of 24.4 us, 8192 rows of 48 heads of 128 with norms 53.8 instead of 52.)
 template <typename T, int V>
 void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAppend& a) {

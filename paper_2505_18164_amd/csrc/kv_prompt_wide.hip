@@ -23,13 +23,13 @@ constexpr float kFarSum = 0x1p30f;
 
 // Four times 64 x 16 bytes global -> LDS, the places 1024 bytes apart: an instruction's offset counts for both addresses.
 __device__ __forceinline__ void dma4(uint32_t lds, const char* base, const uint32_t* off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-               "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+               "global_load_lds_dwordx4 %3, %5 offset:0x800\n\tglobal_load_lds_dwordx4 %4, %5 offset:0xc00"
                ::"s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const char* const* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:1024\n\t"
-               "global_load_lds_dwordx4 %3, off offset:2048\n\tglobal_load_lds_dwordx4 %4, off offset:3072"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\tglobal_load_lds_dwordx4 %2, off offset:0x400\n\t"
+               "global_load_lds_dwordx4 %3, off offset:0x800\n\tglobal_load_lds_dwordx4 %4, off offset:0xc00"
                ::"s"(lds), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]) : "m0", "memory");
 }
 
