@@ -53,6 +53,7 @@ mdi_status mdi_kv_append(const mdi_kv* cache, const mdi_kv8_rows* rows, const md
     if (n_head > 4096 || n_head % (uint32_t)c.K || (some && (!q || !q_out)) || !aligned16(q) || !aligned16(q_out)) return MDI_ERR_ARG;
     if (!good_stride(q_row_stride, unit) || !good_stride(q_head_stride, unit) || !good_stride(q_out_stride, unit) || q_out_stride < (uint64_t)n_head * c.h)
       return MDI_ERR_ARG;
+    if (some && q == q_out && ((r.n_rows > 1 && q_row_stride != q_out_stride) || (n_head > 1 && q_head_stride != (uint64_t)c.h))) return MDI_ERR_ARG;
   } else if (q || q_out) {
     return MDI_ERR_ARG;
   }
@@ -98,6 +99,7 @@ mdi_status mdi_kv_attn(const mdi_kv* cache, const mdi_kv8_rows* rows, const void
   const size_t need = kv_part_bytes(plan, c, r, (int)n_head);
   if (need && (!workspace || !aligned16(workspace))) return MDI_ERR_ARG;
   if (need > workspace_bytes) return MDI_ERR_NOMEM;
+  if (q == out) return MDI_ERR_ARG;                              // (queries are read until the last results are written)
   if (!kv_allow_lds()) return MDI_ERR_HIP;
   launch_kv_attn((hipStream_t)hip_stream, c, r, KvAttn{q, (long)q_stride, out, (long)out_stride, (int)n_head, scale2, sight, (float*)workspace, plan});
   return hip_status();

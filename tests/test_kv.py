@@ -108,6 +108,13 @@ def test_workspaces_and_nothing_to_do():
     assert append(None, none, None, k=None, v=None, q=None, out=None, n_head=0) == mdi.MDI_OK
 
 
+def test_results_in_the_place_of_queries():
+    r = rows(n_rows=4)
+    assert attn(cache(), r, q=4096, out=4096) == mdi.MDI_ERR_ARG
+    for kw in (dict(out_row=512), dict(q_head=128, q_row=1024, out_row=1024)):                                 # laid out otherwise
+        assert append(cache(), r, None, q=4096, out=4096, **{**dict(n_head=4, q_row=256, q_head=64, out_row=256), **kw}) == mdi.MDI_ERR_ARG
+
+
 def test_limits_of_a_launch():
     big = dict(table_stride=1 << 16, n_kv_head=32, head_dim=128)
     assert bytes_of(cache(**big), rows(n=2, n_rows=(1 << 19) - 1, max_ctx=64), 32)[0] == mdi.MDI_OK
