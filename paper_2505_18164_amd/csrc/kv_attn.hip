@@ -40,8 +40,7 @@ __global__ __launch_bounds__(kBlock) void k_kv_join_few(KvCache c, KvRows r, KvA
   Storage<T>::put(out, all.x * inv); Storage<T>::put(out + 1, all.y * inv); Storage<T>::put(out + 2, all.z * inv); Storage<T>::put(out + 3, all.w * inv);
 }
 
-// More of them: a workgroup each, 256 / (h / 4) pieces at a time, a float4 a thread.
-template <typename T>
+// More of them (of single tokens in bf16): a workgroup each, 256 / (h / 4) pieces at a time, a float4 a thread.
 __global__ __launch_bounds__(kBlock) void k_kv_join(KvCache c, KvRows r, KvAttn a) {
   __shared__ float weight[kBlock], red[8];
   __shared__ float4 fold[kBlock];
@@ -86,16 +85,17 @@ __global__ __launch_bounds__(kBlock) void k_kv_join(KvCache c, KvRows r, KvAttn 
     const float4 x = fold[i * per + tid];
     acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
   }
-  T* out = (T*)a.out + ((long)row * a.out_stride + (long)(item - row * a.H) * h + ch);
+  bf16_t* out = (bf16_t*)a.out + ((long)row * a.out_stride + (long)(item - row * a.H) * h + ch);
   const float inv = 1.f / l;
-  Storage<T>::put(out, acc.x * inv); Storage<T>::put(out + 1, acc.y * inv); Storage<T>::put(out + 2, acc.z * inv); Storage<T>::put(out + 3, acc.w * inv);
+  Storage<bf16_t>::put(out, acc.x * inv); Storage<bf16_t>::put(out + 1, acc.y * inv); Storage<bf16_t>::put(out + 2, acc.z * inv); Storage<bf16_t>::put(out + 3, acc.w * inv);
 }
 
-template <typename T>
 void launch_join(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   const unsigned items = (unsigned)(r.n_rows * a.H);
-  if (a.plan.splits <= 64) hipLaunchKernelGGL((k_kv_join_few<T>), dim3((items + kBlock / 64 - 1) / (kBlock / 64)), dim3(kBlock), 0, s, c, r, a);
-  else hipLaunchKernelGGL((k_kv_join<T>), dim3(items), dim3(kBlock), 0, s, c, r, a);
+  const dim3 grid((items + kBlock / 64 - 1) / (kBlock / 64)), block(kBlock);
+  if (a.plan.splits > 64) hipLaunchKernelGGL(k_kv_join, dim3(items), block, 0, s, c, r, a);   // (kv_decode.hip's alone may have more than 64)
+  else if (c.dtype == MDI_BF16) hipLaunchKernelGGL((k_kv_join_few<bf16_t>), grid, block, 0, s, c, r, a);
+  else hipLaunchKernelGGL((k_kv_join_few<float>), grid, block, 0, s, c, r, a);
 }
 
 }  // namespace
@@ -117,7 +117,7 @@ void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAt
   if (a.plan.kernel == kKvDecode) launch_kv_decode(s, c, r, a);
   else if (a.plan.kernel == kKvPrompt) launch_kv_prompt(s, c, r, a);
   else launch_kv_any(s, c, r, a);
-  if (a.plan.splits > 1) { if (c.dtype == MDI_BF16) launch_join<bf16_t>(s, c, r, a); else launch_join<float>(s, c, r, a); }
+  if (a.plan.splits > 1) launch_join(s, c, r, a);
 }
 
 }  // namespace mdi

@@ -9,21 +9,11 @@ namespace mdi {
 template <typename T> struct KvType;
 template <> struct KvType<bf16_t> {
   __device__ static __forceinline__ void load8(const bf16_t* p, float (&x)[8]) { Storage<bf16_t>::load(p, x); }
-  __device__ static __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
 };
 template <> struct KvType<float> {
   __device__ static __forceinline__ void load8(const float* p, float (&x)[8]) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-  __device__ static __forceinline__ void store8(float* p, const float (&x)[8]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
   }
 };
 
