@@ -1,7 +1,7 @@
 // Attention over the cache in the storage type on the matrix cores, for what the other two kernels do not serve: fp32, and bf16 heads of
 // other than 64 or 128 channels; single tokens and packed rows.
 //
-// A workgroup takes sixteen rows of (position, query head) of a kv head, or two times sixteen, and its four wavefronts a quarter each of
+// A workgroup takes sixteen rows of (position, query head) of a kv head, or two times sixteen, and its four wavefronts (two) a share each of
 // the keys they see, sixteen at a time (bf16: two times sixteen), straight from the pages into registers; their sums are added
 // through the LDS.  Both products are computed transposed, as in kv_decode.hip: S^T = K Q^T leaves scores of keys 4 g + r (g = lane / 16)
 // of row lane % 16 in a lane, which is what O^T = V^T P^T takes as its second operand - for fp32 v_mfma_f32_16x16x4_f32, whose
@@ -25,7 +25,10 @@
 namespace mdi {
 namespace {
 
-constexpr int kWaves = 4;
+// Wavefronts of a workgroup.  (Of heads of more than 128 channels a SIMD holds one: two workgroups of two are busy when one of four waits: 2633
+// rows of 8 heads of 256 in bf16 111 -> 93 us, in fp32 204 -> 191; the 2462 rows above with 8, 4 and 2: 67, 52, 52, 2633 of TinyLlama's shape 211,
+// 179, 189.)
+constexpr int waves_of(int padded) { return padded > 128 ? 2 : 4; }
 constexpr float kRaise = 8.f;        // how far (in powers of two) a score may exceed its row's reference before that is raised
 
 // The operands of a step.  K: what a lane has of key `col` of each sixteen; V: channels VB col .. + VB - 1 of keys 4 g + 0..3.
@@ -64,10 +67,11 @@ __device__ __forceinline__ AnySpan any_span(const KvSight& w, int at, int end) {
 
 // kTokens: one row a sample, the columns are up to sixteen query heads of a kv head; else the columns are (position, head) pairs.
 template <typename T, int HD, int S, bool kTokens, bool kMany>
-__global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCache c, KvRows r, KvAttn a, AnyGeo geo) {
+__global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(KvCache c, KvRows r, KvAttn a, AnyGeo geo) {
   typedef Step<T, HD> St;
   constexpr int kKeyStep = 64 / sizeof(T);                       // channels of a key that the four lanes with it read at once
   constexpr int VB = St::VB, KU = St::KU, NG = St::kGroups, KT = 16 * NG, kSteps = 64 / KT;
+  constexpr int kWaves = waves_of(HD);
   constexpr int VP = VB < 4 ? VB : 4, kRow = 16 * VP + 4;         // channels of a lane's VB that are added at a time
   __shared__ long list[kWaves][2][64];                           // rows of the cache of 64 places, and of the next ones
   __shared__ float sums[kWaves][16 * S][kRow];
@@ -398,8 +402,8 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 1 : 2) void k_kv_any(KvCach
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < S; ++u) {
-      const int row = 16 * u + (threadIdx.x >> 4), ch = VB * (threadIdx.x & 15) + v0, item = items[row];
+    for (int row = threadIdx.x >> 4; row < 16 * S; row += 4 * kWaves) {
+      const int ch = VB * (threadIdx.x & 15) + v0, item = items[row];
       float f[kWaves], to = kKvNone, sum = 0.f, x[VP] = {};
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) to = fmaxf(to, marks[i][row].x);
@@ -445,17 +449,17 @@ void launch_sets(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
   AnyGeo g = geo_of(c, r, a.H, S);
   const int total = g.n_blocks * g.sets;
   if (r.n <= kInOrder) {
-    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, false>), dim3(total, a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, g);
+    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, false>), dim3(total, a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, g);
     return;
   }
   for (; g.from < total; g.from += kMostWgs)
-    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, g);
+    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, g);
 }
 template <typename T, int HD>
 void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (!r.start) {
     const long units = (long)r.n * c.K * kv8_groups(c, a.H);     // (below 2^24: n_rows * H is)
-    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)units, a.plan.splits), dim3(64 * kWaves), 0, s, c, r, a, AnyGeo{});
+    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)units, a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, AnyGeo{});
     return;
   }
   if constexpr (most_sets<T>(HD) == 2) if (a.plan.groups == 2) return launch_sets<T, HD, 2>(s, c, r, a);
@@ -484,7 +488,7 @@ KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, d
   const double wgs = r.start ? wgs_of(sets) : (double)r.n * c.K * kv8_groups(c, H);
   const int reach = (int)std::min<long>(r.max_ctx, (long)w.window + (r.start ? 16 * sets >> sh : 1) + w.sinks + 4 * 31);   // places of a workgroup
   const int most = (reach + 63) / 64;
-  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(256. / wgs)))), chunk = (most + want - 1) / want, splits = (most + chunk - 1) / chunk;
+  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(1024. / waves_of(padded(c.h)) / wgs)))), chunk = (most + want - 1) / want, splits = (most + chunk - 1) / chunk;
   // 128 keys of a workgroup's rows take `step` us of a compute unit, a workgroup some more to begin and end
   const bool wide = c.h > 64;
   const double seen = std::min<double>(reach, r.max_ctx - 0.5 * std::min(r.max_ctx, rows)), step = sets == 2 ? (wide ? 1.35 : 0.8) : (wide ? 0.9 : 0.5);
