@@ -494,7 +494,7 @@ KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, d
   const double seen = std::min<double>(reach, r.max_ctx - 0.5 * std::min(r.max_ctx, rows)), step = sets == 2 ? (wide ? 1.35 : 0.8) : (wide ? 0.9 : 0.5);
   *us = std::max(3 + std::ceil(reach / (128. * splits)), wgs * (seen / 128 * step + splits * (wide ? 3.5 : 2.2)) / 256);
   if (splits > 1) *us += 2 + (double)r.n_rows * H * (1 / 2000. + splits * (double)c.h / 4e6);
-  return KvPlan{kKvAny, chunk, splits, 0, sets};
+  return KvPlan{kKvAny, chunk, splits, 0, sets, 0};
 }
 
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

@@ -315,10 +315,10 @@ constexpr int kLeast = 2;            // tiles of a share, at least
 // With many units, or short samples, a unit is a workgroup's.  Else the tiles of all units are cut into equal shares.
 KvPlan kv_decode_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
   const int each = c.K * kv8_groups(c, H), most = kv_most_seen(w, r.max_ctx);   // units of a sample
-  if ((long)r.n * each >= 4 * kShares || most <= kLeast * kKv8Tile) return KvPlan{kKvDecode, most, 1, 0, 0};
+  if ((long)r.n * each >= 4 * kShares || most <= kLeast * kKv8Tile) return KvPlan{kKvDecode, most, 1, 0, 0, 0};
   // a unit of t tiles in shares of at least kLeast, and of at least t * each / kShares (it is one of `each` alike)
   const int tiles = (most + kKv8Tile - 1) / kKv8Tile;
-  return KvPlan{kKvDecode, kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares, 0};
+  return KvPlan{kKvDecode, kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares, 0, 0};
 }
 
 void launch_kv_decode(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

@@ -33,7 +33,7 @@ inline int kv_most_seen(const KvSight& w, int max_ctx) { return (int)std::min<lo
 // weights, which a second launch adds.  How many pieces a row and head has is left by whoever computes the first one.
 // wgs > 0 (kv_decode.hip): the cut is another, all samples' places in equal shares for so many workgroups, of at least `chunk`.
 enum KvKernel { kKvDecode, kKvPrompt, kKvAny };
-struct KvPlan { KvKernel kernel; int chunk, splits, wgs, groups; };   // chunk: places, or (kv_prompt.hip) blocks of 64; groups: kv_prompt.hip's, of wavefronts in a workgroup; kv_any.hip's, of sixteen rows
+struct KvPlan { KvKernel kernel; int chunk, splits, wgs, groups, rows; };   // chunk: places, or (kv_prompt.hip) blocks of 64; groups: kv_prompt.hip's, of wavefronts in a workgroup; kv_any.hip's, of sixteen rows; rows: kv_prompt.hip's, of a workgroup
 inline size_t kv_part_bytes(const KvPlan& p, const KvCache& c, const KvRows& r, int H) {
   return p.splits > 1 ? (size_t)r.n_rows * H * (p.splits * (size_t)(c.h + 2) + 1) * sizeof(float) : 0;
 }

@@ -354,30 +354,35 @@ bool allow_one() {                                               // 64 KiB is wh
   return hipFuncSetAttribute((const void*)k_kv_prompt<NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)prompt_lds<NG>()) == hipSuccess;
 }
 
-PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int WQ) {
-  const int sh = kv_heads_shift(c, H), bp = 32 * WQ >> sh;
+PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int rows) {
+  const int sh = kv_heads_shift(c, H), bp = rows >> sh;
   return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
 }
-// Groups of a workgroup and pieces of a row's blocks.  A step of 64 NG keys takes `step` us, a workgroup some more to begin
-// and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are taken for equal.
-// `step` and the rest are fitted to 13 calls with one and two groups and 1 to 16 pieces.  Two groups against one: 1024 rows of the 7B shape
-// 27 and 39 us, 2048 58 and 68, 1500 of TinyLlama 26 and 37, 4000 of it 107 and 98, 6000 of the 8B shape 334 and 302.  4 pieces
-// of 64 rows behind 8000 of the 8B shape, two groups in 1, 2, 4 and 8 pieces: 124, 77, 54 and 67 us.
-struct PromptPlan { int groups, splits; double us; };
+// Rows and groups of a workgroup and pieces of a row's blocks.  A step of 64 keys (of 128, with two groups) takes `step` us, a workgroup
+// some more to begin and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are
+// taken for equal.  `step` and the rest are fitted to 25 calls with one and two groups and 1 to 16 pieces.
+// Two groups against one: 1024 rows of the 7B shape 27 and 39 us, 2048 57 and 65, 1500 of TinyLlama 26 and 37, 4000 of it 107 and 98, 6000 of the
+// 8B shape 337 and 303.  4 pieces of 64 rows behind 8000 of the 8B shape, two groups in 1, 2, 4 and 8 pieces: 124, 77, 54 and 67 us.
+// Heads of 128 also by workgroups of two wavefronts, two at a time on a compute unit: each reads what four read, but begins and ends beside
+// the other, and 128 rows see fewer keys between them.  Against four: 6000 + 2000 + 500 of the 7B shape with windows of 512, 1024 and
+// 2048 147 and 166, 212 and 229, 265 and 278 us, 8 of 1024 130 and 138; of the 8B shape 353 and 347, 2048 of the 7B shape 65 and 65.
+struct PromptPlan { int rows, groups, splits; double us; };
 PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n;   // of a sample
+  const int n = std::max(1, std::min(r.n, r.n_rows)), n_rows = (r.n_rows + n - 1) / n, sh = kv_heads_shift(c, H);   // rows of a sample
   const double heads = (double)r.n_rows * H;
-  PromptPlan best{1, 1, 1e30};
-  for (int ng = 1; ng <= 2; ++ng) {
-    const int sh = kv_heads_shift(c, H), bp = 256 / ng >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, rows) + 64);
-    const double items = (double)n * ((rows + bp - 1) / bp) * (H >> sh), step = c.h == 128 ? (ng == 1 ? 2.0 : 2.25) : (ng == 1 ? 1.35 : 1.55);
-    const double seen = std::min<double>(most, r.max_ctx - 0.5 * std::min(r.max_ctx, rows));   // what a workgroup sees, on average
+  struct Form { int rows, groups, at_once; double step, ends; };  // workgroups of a compute unit; us of a step and of a workgroup's beginning and end
+  const Form forms[] = {{256, 1, 1, c.h == 128 ? 2.0 : 1.35, 6}, {128, 2, 1, c.h == 128 ? 2.25 : 1.55, 7}, {128, 1, 2, 2.2, 4}};
+  PromptPlan best{256, 1, 1, 1e30};
+  for (const Form& f : forms) {
+    if (f.at_once == 2 && c.h != 128) continue;
+    const int bp = f.rows >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, n_rows) + 64);
+    const double items = (double)n * ((n_rows + bp - 1) / bp) * (H >> sh), slots = 256 * f.at_once;
+    const double seen = std::min<double>(most, r.max_ctx - 0.5 * std::min(r.max_ctx, n_rows));   // what a workgroup sees, on average
     for (int s = 1; s <= 32; s *= 2) {
       if (s > 1 && most < 256 * s) break;
-      const double longest = std::ceil(most / (64. * ng * s)), all = items * seen / (64. * ng * 256);
-      double us = std::max(longest * step + 6, all * step + items * s / 256 * (5 + ng));
+      double us = std::max(std::ceil(most / (64. * f.groups * s)) * f.step + 6, items / slots * (seen / (64. * f.groups) * f.step + s * f.ends));
       if (s > 1) us += 2 + heads / 2000 + heads * s * c.h / 4e6;
-      if (us < best.us) best = PromptPlan{ng, s, us};
+      if (us < best.us) best = PromptPlan{f.rows, f.groups, s, us};
     }
   }
   return best;
@@ -404,15 +409,15 @@ bool kv_allow_lds() {
 KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us) {
   const PromptPlan p = prompt_plan(c, r, H, w);
   // blocks that a workgroup of up to `bp` positions may have: of the first ones, and of a window that begins inside one
-  const int bp = 256 / p.groups >> kv_heads_shift(c, H);
+  const int bp = p.rows >> kv_heads_shift(c, H);
   const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
   const int chunk = (int)((most + p.splits - 1) / p.splits);
   *us = p.us;
-  return KvPlan{kKvPrompt, chunk, (int)((most + chunk - 1) / chunk), 0, p.groups};
+  return KvPlan{kKvPrompt, chunk, (int)((most + chunk - 1) / chunk), 0, p.groups, p.rows};
 }
 
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  PromptGeo g = geo_of(c, r, a.H, 8 / a.plan.groups);
+  PromptGeo g = geo_of(c, r, a.H, a.plan.rows);
   const int total = g.n_blocks * g.sets;                         // (at most 2^24 + 2^17)
   const bool many = r.n > kInOrder, whole = c.pt % BK == 0;
   for (; g.from < total; g.from += kMostWgs) {

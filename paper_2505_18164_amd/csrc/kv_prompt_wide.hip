@@ -1,4 +1,4 @@
-// Attention of packed rows over the bf16 cache, heads of 128: 64 rows of (position, query head) a wavefront, one wavefront a SIMD.
+// Attention of packed rows over the bf16 cache, heads of 128: 64 rows of (position, query head) a wavefront, one wavefront a SIMD, two or four a workgroup.
 //
 // The products of kv_prompt.hip read an operand of every matrix instruction from the LDS, 1 KiB in 32 cycles for each of the four SIMDs of
 // a compute unit: all that its LDS delivers.  Here an operand serves two of them, for the wavefront's two sets of 32 rows.  What a
@@ -7,10 +7,11 @@
 // instructions behind every matrix instruction.  Everything of a step is in registers (the operands of the next are read
 // meanwhile), some 400 of them.  (Weights are rounded to bf16: see kv_prompt.hip.)
 //
-// Prompts of 6000, 2000 and 500 of the 8B shape 347 us, 0.96 PFLOP/s; with a window of 1024 of the 7B shape 213 to 231, where a workgroup
-// passes over 1280 keys for rows that see 1024 each, and begins and ends in 6 us for every 40.  (The products of kv_prompt.hip, with heads
-// of 128: 380 and 215 to 231; in vector instructions 25 ms and 9 ms.)  Of the 347 us the matrix instructions alone take 248 to 260 -
-// with these data; with zeros the whole takes 336 -, with the softmax 314, with the reads of the LDS 331.
+// Prompts of 6000, 2000 and 500 of the 8B shape 347 us, 0.96 PFLOP/s; with a window of 1024 of the 7B shape 205 to 213, where a workgroup
+// passes over 1152 keys for rows that see 1024 each.  (The products of kv_prompt.hip, with heads of 128: 380 and 215 to 231; in vector
+// instructions 25 ms and 9 ms.)  Of the 347 us the matrix instructions alone take 248 to 260 - with these data; with zeros the whole takes
+// 336 -, with the softmax 314, with the reads of the LDS 331.  A workgroup begins and ends in some 6 us, most of them its queries, first
+// keys and results on their way.
 #include <type_traits>
 
 #include "kv_prompt_device.h"
@@ -33,10 +34,10 @@ __device__ __forceinline__ void dma4(uint32_t lds, const char* const* p) {
                ::"s"(lds), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]) : "m0", "memory");
 }
 
-// A workgroup is four wavefronts: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
-template <int NG, bool kWhole, bool kMany>
-__global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
-  constexpr int HD = 128, WQ = 4 / NG, BQ = 64 * WQ, GT = 64 * WQ;   // rows of a workgroup - (position, head) pairs -, threads of a group
+// A workgroup is W wavefronts, four or two: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
+template <int W, int NG, bool kWhole, bool kMany>
+__global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows r, KvAttn a, PromptGeo geo) {
+  constexpr int HD = 128, WQ = W / NG, BQ = 64 * WQ, GT = 64 * WQ;   // rows of a workgroup - (position, head) pairs -, threads of a group
   constexpr int HT = HD / 32, KS = HD / 16, RB = 2 * HD, UN = HD / 8;   // bytes and 16-byte units of a key
   constexpr int BB = BK * RB;                                    // bytes of a block of keys, or of values
   constexpr int KP = 64 / UN, NI = BK / KP / WQ;                 // keys of an instruction that loads, instructions of a wavefront
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
   } while (__builtin_expect(again & 1, 0));
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
   if (__builtin_expect(again, 0)) {
-    prompt_again<HD>(c, r, a, mine, BQ, 4);
+    prompt_again<HD>(c, r, a, mine, BQ, W);
     return;
   }
   if constexpr (NG > 1) {
@@ -407,26 +408,32 @@ __global__ __launch_bounds__(256, 1) void k_kv_prompt_wide(KvCache c, KvRows r, 
 }
 
 template <int NG> constexpr size_t wide_lds() { return (size_t)NG * 5 * BK * 256; }
-template <int NG, bool kWhole, bool kMany>
-bool allow_one() {                                               // 64 KiB is what a kernel gets by default
-  return hipFuncSetAttribute((const void*)k_kv_prompt_wide<NG, kWhole, kMany>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds<NG>()) == hipSuccess;
+template <int W, int NG>
+bool allow() {                                                   // 64 KiB is what a kernel gets by default
+  auto one = [](const void* k) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds<NG>()) == hipSuccess; };
+  return one((const void*)k_kv_prompt_wide<W, NG, true, false>) && one((const void*)k_kv_prompt_wide<W, NG, false, false>) &&
+         one((const void*)k_kv_prompt_wide<W, NG, true, true>) && one((const void*)k_kv_prompt_wide<W, NG, false, true>);
 }
-template <int NG, bool kWhole>
+template <int W, int NG>
 void launch(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs, bool many) {
-  if (many) hipLaunchKernelGGL((k_kv_prompt_wide<NG, kWhole, true>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
-  else hipLaunchKernelGGL((k_kv_prompt_wide<NG, kWhole, false>), dim3(wgs, a.plan.splits), dim3(256), wide_lds<NG>(), s, c, r, a, g);
+  const dim3 grid(wgs, a.plan.splits), block(64 * W);
+  const size_t lds = wide_lds<NG>();
+  if (c.pt % BK == 0) {
+    if (many) hipLaunchKernelGGL((k_kv_prompt_wide<W, NG, true, true>), grid, block, lds, s, c, r, a, g);
+    else hipLaunchKernelGGL((k_kv_prompt_wide<W, NG, true, false>), grid, block, lds, s, c, r, a, g);
+  } else {
+    if (many) hipLaunchKernelGGL((k_kv_prompt_wide<W, NG, false, true>), grid, block, lds, s, c, r, a, g);
+    else hipLaunchKernelGGL((k_kv_prompt_wide<W, NG, false, false>), grid, block, lds, s, c, r, a, g);
+  }
 }
 
 }  // namespace
 
-bool kv_wide_allow_lds() {
-  return allow_one<1, true, false>() && allow_one<1, false, false>() && allow_one<1, true, true>() && allow_one<1, false, true>() &&
-         allow_one<2, true, false>() && allow_one<2, false, false>() && allow_one<2, true, true>() && allow_one<2, false, true>();
-}
+bool kv_wide_allow_lds() { return allow<4, 1>() && allow<4, 2>() && allow<2, 1>(); }
 void launch_kv_wide(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a, const PromptGeo& g, int wgs, bool many) {
-  const bool whole = c.pt % BK == 0;
-  if (a.plan.groups == 1) { if (whole) launch<1, true>(s, c, r, a, g, wgs, many); else launch<1, false>(s, c, r, a, g, wgs, many); }
-  else { if (whole) launch<2, true>(s, c, r, a, g, wgs, many); else launch<2, false>(s, c, r, a, g, wgs, many); }
+  if (a.plan.groups == 2) launch<4, 2>(s, c, r, a, g, wgs, many);
+  else if (a.plan.rows == 256) launch<4, 1>(s, c, r, a, g, wgs, many);
+  else launch<2, 1>(s, c, r, a, g, wgs, many);
 }
 
 }  // namespace mdi

@@ -173,12 +173,11 @@ def test_packed_rows_against_64_bits(case, sight, dtype):
 
 
 # Rows of nobody behind the last sample, times heads: so many that the call is taken for a large one, for each of the ways to divide that.
-CROWDS = [30000, 80000]
+CROWDS = {64: [30000, 80000], 128: [30000, 80000, 200000]}
 
 
-@pytest.mark.parametrize("crowd", CROWDS)
 @pytest.mark.parametrize("sight", SIGHTS, ids=[f"{w}+{s}" for w, s in SIGHTS])
-@pytest.mark.parametrize("case", [c for c in ATTN if c[2] in (64, 128)], ids=[i for c, i in zip(ATTN, IDS) if c[2] in (64, 128)])
+@pytest.mark.parametrize("case,crowd", [(c, n) for c in ATTN for n in CROWDS.get(c[2], [])], ids=[f"{i}-of-{n}" for c, i in zip(ATTN, IDS) for n in CROWDS.get(c[2], [])])
 def test_rows_of_a_large_call_against_64_bits(case, sight, crowd):
     s = Setup(*case, BF16, *sight, seed=3, rows_behind=crowd // case[0])
     cache = s.cache()
@@ -248,7 +247,7 @@ def test_pieces_of_prompts_behind_long_contexts(one_each, dtype):
 
 
 @pytest.mark.parametrize("H,K,h,pt,lens,behind,sight", [
-    (32, 4, 128, 64, [100, 64, 80, 90], [3000, 2500, 2900, 2000], (0, 0)), (32, 2, 128, 24, [100, 64, 80, 90], [3000, 2500, 2900, 2000], (1500, 5)),
+    (32, 4, 128, 64, [100, 100], [4900, 4000], (0, 0)), (32, 4, 128, 64, [100, 64, 80, 90], [3000, 2500, 2900, 2000], (0, 0)), (32, 2, 128, 24, [100, 64, 80, 90], [3000, 2500, 2900, 2000], (1500, 5)),
     (32, 4, 64, 24, [130, 100, 90, 130], [3000, 2500, 2500, 2500], (1500, 600)), (32, 4, 64, 64, [130, 100, 1, 130], [3000, 2500, 2500, 0], (0, 0))])
 def test_many_heads_behind_long_contexts(H, K, h, pt, lens, behind, sight):
     s = Setup(H, K, h, pt, lens, behind, BF16, *sight, seed=5, stale=float("inf"), rows_behind=2)
@@ -263,7 +262,7 @@ def test_many_heads_behind_long_contexts(H, K, h, pt, lens, behind, sight):
     cache.check()
 
 
-KINDS = [(64, BF16, 0), (128, BF16, 0), (48, BF16, 0), (64, F32, 0), (128, F32, 0), (48, F32, 0)] + [(h, BF16, c) for h in (64, 128) for c in CROWDS]
+KINDS = [(64, BF16, 0), (128, BF16, 0), (48, BF16, 0), (64, F32, 0), (128, F32, 0), (48, F32, 0)] + [(h, BF16, c) for h in CROWDS for c in CROWDS[h]]
 KIND_IDS = [f"{h}-{'bf16' if d is BF16 else 'f32'}" + (f"-of-{c}" if c else "") for h, d, c in KINDS]
 
 
@@ -380,7 +379,7 @@ def test_what_is_not_of_the_cache_is_reported(h, dtype, crowd):
             torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("h,crowd", [(128, 0), (96, 0), (128, 30000), (128, 80000), (64, 80000)])
+@pytest.mark.parametrize("h,crowd", [(128, 0), (96, 0), (128, 30000), (128, 80000), (128, 200000), (64, 80000)])
 def test_offsets_past_32_bits(h, crowd):
     """The last pages of a pool of 4.5 GiB."""
     K, pt, H = 8, 64, 16
