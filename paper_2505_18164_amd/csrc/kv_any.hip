@@ -1,5 +1,5 @@
-// Attention over the cache in the storage type on the matrix cores, for what the other two kernels do not serve: fp32, and bf16 heads of
-// other than 64 or 128 channels; single tokens and packed rows.
+// Attention over the cache in the storage type on the matrix cores, for what the other kernels do not serve: fp32, and bf16 heads of other
+// than 64 or 128 channels, single tokens and packed rows; and for packed rows that are too few for kv_prompt.hip (kv_plan).
 //
 // A workgroup takes sixteen rows of (position, query head) of a kv head, or two times sixteen, and its four wavefronts (two) a share each of
 // the keys they see, sixteen at a time (bf16: two times sixteen), straight from the pages into registers; their sums are added
@@ -8,7 +8,7 @@
 // products and sums are fp32's, register by register; for bf16 v_mfma_f32_16x16x32_bf16 with a weight as two operands, its upper digits
 // and what they leave.  Channels and keys may be named in any order that both operands share, so a lane reads 16 bytes of a key and
 // 16 channels' worth of a value at a time.  The keys of the next step are asked for when those of this one are multiplied,
-// the values when the step begins.  Heads are padded to HD channels, the padding is neither read nor written.
+// the values when the step begins.  Heads are padded to HD channels with zeros in keys and queries; the padding is not written.
 //
 // 5 ragged fp32 prompts, 2462 rows of 16 heads of 64 with a window of 300: 49 to 52 us, of which the matrix instructions are 18 (at 154
 // TFLOP/s).  A step of a wavefront takes 1.35 times its matrix instructions' time, and 20 us go before the first: the chain from
@@ -49,7 +49,7 @@ template <int HD> struct Query<bf16_t, HD> { u32x4 q[HD / 32]; };
 
 struct AnyGeo { int n_blocks, sets, g_sh, from; };
 
-// What the rows of a wavefront see, at positions at .. end - 1: the first sinks and from .. end - 1, counted in steps of T positions without
+// What the rows of a workgroup see, at positions at .. end - 1: the first sinks and from .. end - 1, counted in steps of T positions without
 // the steps between: place c is position c of the first `apart`, then c + shift (as KvSpan of one row).  64 places are a block.
 struct AnySpan { int sinks, apart, shift, from, end, steps; };
 template <int T>
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(
   const T* const data = (const T*)c.data;
   int sample_row[S], head[S], pos[S];                            // of this lane's column: row of the call, query head, position
   bool live[S];
-  int which, kv, first_pos, last_pos;                            // of the wavefront's rows
+  int which, kv, first_pos, last_pos;                            // of the workgroup's rows
   bool none = false;                                             // the sample takes no part
   if constexpr (kTokens) {
     const int G = a.H / c.K, groups = kv8_groups(c, a.H), unit = blockIdx.x, sample = unit / (c.K * groups), rest = unit - sample * (c.K * groups);
