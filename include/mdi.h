@@ -627,11 +627,10 @@ MDI_API mdi_status mdi_kv_append(const mdi_kv *cache, const mdi_kv8_rows *rows, 
  * Scores, softmax and sums are binary32, and sums of weights times values are divided
  * at the end: the number of positions times the largest magnitude of a value has to be
  * below 2^120, and |scale| times a query's and key's sum of magnitudes of products below 2^120.
- * Products of fp32 are fp32's.  bf16: products take a weight with 16 digits; in calls of
- * many packed rows of 64 or 128 channels it is rounded to bf16, and summed as rounded.
- * (Where a value that a row does not see is not finite, and where, in such calls, a score
- * exceeds the largest of the first 32 keys that its row sees by 17 or more, rows are
- * computed a second time; the former takes tens of times as long.)  Limits, alignment
+ * Products of fp32 are fp32's.  bf16: products take a weight with 16 digits.
+ * (Where a value that a row does not see is not finite, and where, in calls of many packed
+ * rows of 128 channels, a score exceeds the largest of the first 32 keys that its row sees by
+ * 17 or more, rows are computed a second time; the former takes tens of times as long.)  Limits, alignment
  * (strides multiples of 16 bytes; q and out must not overlap), workspace and errors are
  * those of mdi_kv8_attn, its size mdi_kv_attn_bytes'.  Results do not depend on timing.
  */

@@ -100,10 +100,10 @@ void launch_join(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
 
 }  // namespace
 
-// Packed rows in bf16 with heads of 64 or 128 are kv_prompt.hip's (256 rows of position and head to a workgroup) or kv_any.hip's (16 or 32),
-// whichever should take less time by their plans: 24 prompts of 1 to 64 rows of 12 heads of 64 14.0 against 8.3 us, 64 samples of 2 rows
-// behind 500 of the 8B shape 44 against 28, 512 rows of the 7B shape 19.9 against 17.6, but 24 prompts of 40 rows of the 8B shape 13.9
-// against 21, 8 of 333 rows of TinyLlama's 26 against 35.
+// Packed rows in bf16 with heads of 64 or 128 are kv_prompt.hip's (256 or 128 rows of position and head to a workgroup) or kv_any.hip's (16
+// or 32), whichever should take less time by their plans: 64 samples of 2 rows behind 500 of the 8B shape 33 against 26 us, 512 rows of
+// the 7B shape 21.4 against 16.5, 512 of 12 heads of 64 14.9 against 9.5, but 24 prompts of 40 rows of the 8B shape 14.5 against 20.5, 8 of 333
+// rows of TinyLlama's 28 against 33.
 KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
   if (kv_decode_supported(c, r)) return kv_decode_plan(c, r, H, w);
   double any_us, us;

@@ -8,11 +8,10 @@
 // registers, a block ahead, 16 bytes a lane; the 16-byte units of a row are permuted by the row's number (the permutation is
 // applied to the address in memory, the LDS then holds it for free), which spreads both kinds of reads over all banks.
 //
-// Weights are rounded to bf16, as the product takes them, 2^-9 of each at most, and their sum is of the rounded ones: results are off by
-// 0.0020 of their size, 0.0017 of which are their own rounding.  A second product for the digits they lose would be a third more matrix
-// instructions.
-// 8 prompts of 333 rows of TinyLlama 25 us, one of 4000 98, 0.67 PFLOP/s: a step of 64 keys takes 1.35 us, the matrix instructions of it 0.56,
-// exponentials of one wavefront of a SIMD beside the products of the other.
+// A weight is two operands of the second product, sixteen digits of it (PromptWeights), half as many matrix instructions again; as one it would be
+// off by up to 2^-8, and results by 0.0020 of their size instead of the 0.0017 that are their own rounding.
+// 8 prompts of 333 rows of TinyLlama 28 us, one of 4000 127, 0.51 PFLOP/s (weights of one operand: 25 and 98): a step of 64 keys takes
+// 1.7 us, the matrix instructions of it 0.84, exponentials of one wavefront of a SIMD beside the products of the other.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
     return k0 <= last_pos && (k0 + BK - 1 > wave_pos - a.sight.window || k0 < a.sight.sinks);
   };
   f32x16 s[2];
-  u32x4 pf[4] = {};                                              // weights, two a word
+  PromptWeights<4> pf = {};
   // The products of a step: the values of block j - 1 with its weights, the keys of block j with the queries.  Four operands are
   // on their way from the LDS while the four before them are multiplied.
   auto products = [&](int j, auto keys) __attribute__((always_inline)) {
@@ -186,7 +185,11 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         if (n < HT) {
-          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), __builtin_bit_cast(bf16x8, pf[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
+          o[x % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), __builtin_bit_cast(bf16x8, pf.upper[(4 * n + x) / HT]), o[x % HT], 0, 0, 0);
+          if (x % HT == HT - 1)
+#pragma unroll
+            for (int y = x + 1 - HT; y <= x; ++y)
+              o[y % HT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][y]), __builtin_bit_cast(bf16x8, pf.lower[(4 * n + y) / HT]), o[y % HT], 0, 0, 0);
         } else {
           const int k = 2 * (n - HT) + (x >> 1);
           s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[n & 1][x]), qf[k], k ? s[x & 1] : f32x16{}, 0, 0, 0);
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // The weights of block j from its scores, rounded to bf16 as the product takes them; their sum takes them as they are multiplied.
+  // The weights of block j from its scores.
   float alpha = 1.f;
   bool raised = false;
   auto weigh = [&]() __attribute__((always_inline)) {
@@ -206,9 +209,10 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const bf16x2 w = {(__bf16)exp2_raw(fmaf(s[t][e], scale, -m)), (__bf16)exp2_raw(fmaf(s[t][e + 1], scale, -m))};
-          sum = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
-          pf[2 * t + (e >> 3)][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+          const float w0 = exp2_raw(fmaf(s[t][e], scale, -m)), w1 = exp2_raw(fmaf(s[t][e + 1], scale, -m));
+          sum += w0;
+          sum += w1;
+          pf.put(16 * t + e, w0, w1);
         }
     };
     weights();
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   auto soften = [&](int j) __attribute__((always_inline)) {
     if (!sees(j)) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) pf[t] = u32x4{0, 0, 0, 0};
+      for (int t = 0; t < 4; ++t) { pf.upper[t] = u32x4{0, 0, 0, 0}; pf.lower[t] = u32x4{0, 0, 0, 0}; }
       return;
     }
     const int k0 = start_of(block_of(j));
@@ -360,18 +364,19 @@ PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int rows) {
 }
 // Rows and groups of a workgroup and pieces of a row's blocks.  A step of 64 keys (of 128, with two groups) takes `step` us, a workgroup
 // some more to begin and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are
-// taken for equal.  `step` and the rest are fitted to 25 calls with one and two groups and 1 to 16 pieces.
-// Two groups against one: 1024 rows of the 7B shape 27 and 39 us, 2048 57 and 65, 1500 of TinyLlama 26 and 37, 4000 of it 107 and 98, 6000 of the
-// 8B shape 337 and 303.  4 pieces of 64 rows behind 8000 of the 8B shape, two groups in 1, 2, 4 and 8 pieces: 124, 77, 54 and 67 us.
+// taken for equal, all as long as the longest, so `us` is more than such a call takes (6000 + 2000 + 500 of the 8B shape: 485 us, taken for
+// 800), and serves to compare.  `step` and the rest are fitted to 29 calls with one and two groups and 1 to 16 pieces.
+// Two groups against one: 1024 rows of the 7B shape 31 and 48 us, 2048 68 and 85, 1500 of TinyLlama 30 and 47, 4000 of it 137 and 127, 6000 + 2000 +
+// 500 of the 8B shape 522 and 485.  4 pieces of 64 rows behind 8000 of the 8B shape, two groups in 1, 2, 4 and 8 pieces: 152, 92, 68 and 80 us.
 // Heads of 128 also by workgroups of two wavefronts, two at a time on a compute unit: each reads what four read, but begins and ends beside
 // the other, and 128 rows see fewer keys between them.  Against four: 6000 + 2000 + 500 of the 7B shape with windows of 512, 1024 and
-// 2048 147 and 166, 212 and 229, 265 and 278 us, 8 of 1024 130 and 138; of the 8B shape 353 and 347, 2048 of the 7B shape 65 and 65.
+// 2048 185 and 208, 248 and 266, 353 and 365 us, 8 of 1024 148 and 162; of the 8B shape 487 and 485, 2048 of the 7B shape 83 and 85.
 struct PromptPlan { int rows, groups, splits; double us; };
 PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
   const int n = std::max(1, std::min(r.n, r.n_rows)), n_rows = (r.n_rows + n - 1) / n, sh = kv_heads_shift(c, H);   // rows of a sample
   const double heads = (double)r.n_rows * H;
   struct Form { int rows, groups, at_once; double step, ends; };  // workgroups of a compute unit; us of a step and of a workgroup's beginning and end
-  const Form forms[] = {{256, 1, 1, c.h == 128 ? 2.0 : 1.35, 6}, {128, 2, 1, c.h == 128 ? 2.25 : 1.55, 7}, {128, 1, 2, 2.2, 4}};
+  const Form forms[] = {{256, 1, 1, c.h == 128 ? 2.55 : 1.7, 6}, {128, 2, 1, c.h == 128 ? 2.85 : 1.95, 7}, {128, 1, 2, 2.8, 4}};
   PromptPlan best{256, 1, 1, 1e30};
   for (const Form& f : forms) {
     if (f.at_once == 2 && c.h != 128) continue;

@@ -17,7 +17,7 @@ typedef __attribute__((address_space(3))) u32x4* lds_u32x4;
 
 constexpr int BK = 64;               // keys of a step
 // Weights are counted from a reference of their row, the largest score of the first block that the row sees; it is raised only
-// when a block's weights sum to more than this: weights of any size keep their digits in bf16 and in the sums, which are divided
+// when a block's weights sum to more than this: weights of any size keep their digits in their operands and in the sums, which are divided
 // out at the end.  So no maximum is looked for where nothing is raised.
 constexpr float kMostSum = 0x1p16f;
 
@@ -59,6 +59,18 @@ __device__ __forceinline__ float masked(float s, uint32_t seen, int key) {
   const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, key, 1);
   return __uint_as_float((__float_as_uint(s) & all) | (0xFF800000u & ~all));
 }
+
+// A lane's weights of 16 N keys as two operands of the second product each: rounded to bf16, and what that leaves, rounded again, which
+// is sixteen digits of a weight.  (One alone would be off by as much as the rounding of the result.)
+template <int N> struct PromptWeights {
+  u32x4 upper[N], lower[N];
+  __device__ __forceinline__ void put(int e, float w0, float w1) {   // weights e and e + 1, e even
+    uint32_t up = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)w0, (__bf16)w1});
+    asm("" : "+v"(up));                                          // (else each half is worked out once more)
+    upper[e >> 3][(e & 7) >> 1] = up;
+    lower[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(w0 - __uint_as_float(up << 16)), (__bf16)(w1 - __uint_as_float(up & 0xFFFF0000u))});
+  }
+};
 
 // What a workgroup's rows are, and the blocks they see.
 struct PromptRows {

@@ -1,18 +1,17 @@
 // Attention of packed rows over the bf16 cache, heads of 128: 64 rows of (position, query head) a wavefront, one wavefront a SIMD, two or four a workgroup.
 //
 // The products of kv_prompt.hip read an operand of every matrix instruction from the LDS, 1 KiB in 32 cycles for each of the four SIMDs of
-// a compute unit: all that its LDS delivers.  Here an operand serves two of them, for the wavefront's two sets of 32 rows.  What a
-// second wavefront on the SIMD did, exponentials while the first multiplies, the wavefront does itself: in step i, of 32
-// keys, it multiplies the keys of step i + 1 and the values of step i - 1 and in between weighs the scores of step i, three vector
-// instructions behind every matrix instruction.  Everything of a step is in registers (the operands of the next are read
-// meanwhile), some 400 of them.  (Weights are rounded to bf16: see kv_prompt.hip.)
+// a compute unit: all that its LDS delivers.  Here an operand serves two of them, for the wavefront's two sets of 32 rows, and values four:
+// a weight is two operands (PromptWeights).  What a second wavefront on the SIMD did, exponentials while the first multiplies, the
+// wavefront does itself: in step i, of 32 keys, it multiplies the keys of step i + 1 and the values of step i - 1 and in between
+// weighs the scores of step i, some five vector instructions behind every matrix instruction.  Everything of a step is in registers
+// (operands are read into them shortly before they are multiplied), some 420 of them.
 //
-// Prompts of 6000, 2000 and 500 of the 8B shape 347 us, 0.96 PFLOP/s; with a window of 1024 of the 7B shape 205 to 213, where a workgroup
-// passes over 1152 keys for rows that see 1024 each.  (The products of kv_prompt.hip, with heads of 128: 380 and 215 to 231; in vector
-// instructions 25 ms and 9 ms.)  Of the 347 us the matrix instructions alone take 248 to 260 - with these data; with zeros the whole takes
-// 336 -, with the softmax 314, with the reads of the LDS 331.  A workgroup begins and ends in some 6 us, most of them its queries, first
-// keys and results on their way.
-#include <type_traits>
+// Matrix instructions bound it: prompts of 6000, 2000 and 500 of the 8B shape take 470 to 485 us, 0.7 PFLOP/s of useful products and 1.05 with those
+// of the weights' lower digits, where a large product of the library reaches 1.21; with a window of 1024 of the 7B shape 250, where
+// a workgroup passes over 1152 keys for rows that see 1024 each.  (Weights of one operand: 351 and 197; in vector instructions 25 ms and 9 ms.)
+// A workgroup begins and ends in some 6 us, most of them its queries, first keys and results on their way.
+#include <utility>
 
 #include "kv_prompt_device.h"
 #include "kv_prompt_wide.h"
@@ -33,6 +32,9 @@ __device__ __forceinline__ void dma4(uint32_t lds, const char* const* p) {
                "global_load_lds_dwordx4 %3, off offset:0x800\n\tglobal_load_lds_dwordx4 %4, off offset:0xc00"
                ::"s"(lds), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]) : "m0", "memory");
 }
+
+// f(0) .. f(N - 1), numbers that the compiler knows: a loop whose body takes this much is not unrolled.
+template <typename F, int... N> __device__ __forceinline__ void each(F&& f, std::integer_sequence<int, N...>) { (f(std::integral_constant<int, N>()), ...); }
 
 // A workgroup is W wavefronts, four or two: NG groups of WQ, which work on the same 64 WQ rows; group g takes the key blocks NG i + g.
 template <int W, int NG, bool kWhole, bool kMany>
@@ -92,7 +94,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   auto step_from = [&](int b) __attribute__((always_inline)) { return max(b - b_lo - grp + NG - 1, 0) / NG; };   // the group's first whose block is b or behind it
   // steps whose block is the wavefront's rows' as a whole; stages whose keys and values all are
   const int all_lo = step_from(first_from(max(last_pos - a.sight.window + 1, 0))), all_hi = step_from(min((wave_pos + 1 - gap) >> 6, b_hi));
-  const int rare_lo = step_from(first_from(kb.from)) + 1, rare_hi = step_from(min((kb.end - gap) >> 6, b_hi));
+  const int rare_lo = step_from(first_from(kb.from)), rare_hi = step_from(min((kb.end - gap) >> 6, b_hi));
   auto visible = [&](int p, int k0) __attribute__((always_inline)) {
     return min(p < kb.sinks || p >= kb.from ? p : k0 < kb.sinks ? kb.sinks - 1 : kb.from, kb.end - 1);
   };
@@ -111,8 +113,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   uint32_t at_off[NI];                                           // of a block whose positions are all seen by some row
 #pragma unroll
   for (int n = 0; n < NI; ++n) at_off[n] = (uint32_t)(key_of(n) * RB + 16 * unit_of(key_of(n)) + by_of(n));
-  const char *k_at[kWhole ? 1 : NI] = {}, *v_at[kWhole ? 1 : NI] = {};   // the stage's keys; its values
-  uint32_t k_off[kWhole ? NI : 1], v_off[kWhole ? NI : 1];
+  const char *k_at[kPages] = {}, *v_at = nullptr;                // the stage's keys (kWhole: and its values)
   const long v_by = (long)c.pt * RB;                             // from a key to its value
   const char* const heads_at = (const char*)c.data + 2 * kv * v_by;
   const uint64_t page_bytes = 2ull * c.K * v_by;
@@ -131,69 +132,90 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
     list[1] = (uint32_t)(k >> 32);
     asm volatile("" : "+v"(list[0]), "+v"(list[1]));
   };
-  // Where stage j is: its keys' addresses, and its values' from the keys of the one before.  (Page numbers are looked at before anything
-  // else is asked for: whoever waits for them waits for that, too.)
+  // Pages that hold blocks as a whole: where stage j is, its keys, and its values from the keys of the stage before.  (Page numbers are
+  // looked at before anything else is asked for: whoever waits for them waits for that, too.)
   auto find = [&](int j, int (&pg)[kPages]) __attribute__((always_inline)) {
     if constexpr (kWhole) {
-      v_at[0] = k_at[0] + v_by;
+      v_at = k_at[0] + v_by;
       if ((j & 63) == 0) {
         fill(j, pg);
         pages(j + 64, pg);
       }
       k_at[0] = (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)list[1], j & 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)list[0], j & 63));
-      if (__builtin_expect(j < rare_lo || j >= rare_hi, 0)) {
-        const int k0 = start_of(block_of(j)), k1 = start_of(block_of(max(j - 1, 0)));
+    }
+  };
+  // Instructions 4 n .. + 3 of stage j; lds: the wavefront's part of the block.  Other pages: the values' before the same of the keys,
+  // whose addresses are the next stage's values'.
+  auto ask_block = [&](uint32_t lds, const char* at, int n, int j, bool rare) __attribute__((always_inline)) {
+    if (__builtin_expect(rare, 0)) {
+      const int k0 = start_of(block_of(j));
+      uint32_t off[4];
 #pragma unroll
-        for (int n = 0; n < NI; ++n) {
-          const int key = key_of(n);
-          k_off[n] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key) + by_of(n));
-          v_off[n] = (uint32_t)((visible(k1 + key, k1) - k1) * RB + 16 * unit_of(key) + by_of(n));
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < NI; ++n) { k_off[n] = at_off[n]; v_off[n] = at_off[n]; }
+      for (int i = 0; i < 4; ++i) {
+        const int key = key_of(4 * n + i);
+        off[i] = (uint32_t)((visible(k0 + key, k0) - k0) * RB + 16 * unit_of(key) + by_of(i));
       }
+      dma4(lds + 4096 * n, at, off);
+    } else {
+      dma4(lds + 4096 * n, at, &at_off[4 * n]);
+    }
+  };
+  auto ask_keys = [&](uint32_t lds, int n, int j, int (&pg)[kPages]) __attribute__((always_inline)) {
+    if constexpr (kWhole) {
+      ask_block(lds, k_at[0], n, j, j < rare_lo || j >= rare_hi);
     } else {
       const int k0 = start_of(block_of(j));
 #pragma unroll
-      for (int n = 0; n < NI; ++n) {
-        const int key = key_of(n);
-        v_at[n] = k_at[n] + v_by;
-        k_at[n] = (const char*)c.data + kv8_row(c, checked(pg[n]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key) + by_of(n) - 4096;
-        asm volatile("" : "+v"(k_at[n]));
+      for (int i = 4 * n; i < 4 * n + 4; ++i) {
+        const int key = key_of(i);
+        k_at[i] = (const char*)c.data + kv8_row(c, checked(pg[i]), kv, visible(k0 + key, k0)) * RB + 16 * unit_of(key) + by_of(i) - 4096;
       }
+      dma4(lds + 4096 * n, &k_at[4 * n]);
     }
   };
-  auto ask_keys = [&](uint32_t lds, int n) __attribute__((always_inline)) {   // instructions 4 n .. + 3; lds: the wavefront's part of the block
-    if constexpr (kWhole) dma4(lds + 4096 * n, k_at[0], &k_off[4 * n]); else dma4(lds + 4096 * n, &k_at[4 * n]);
+  auto ask_values = [&](uint32_t lds, int n, int j) __attribute__((always_inline)) {
+    if constexpr (kWhole) {
+      ask_block(lds, v_at, n, max(j - 1, 0), j <= rare_lo || j > rare_hi);
+    } else {
+      const char* p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = k_at[4 * n + i] + v_by;
+      dma4(lds + 4096 * n, p);
+    }
   };
-  auto ask_values = [&](uint32_t lds, int n) __attribute__((always_inline)) {
-    if constexpr (kWhole) dma4(lds + 4096 * n, v_at[0], &v_off[4 * n]); else dma4(lds + 4096 * n, &v_at[4 * n]);
+  // (behind a wait for all loads: else the first that looks at them waits for what has been asked for since)
+  auto loaded = [&](int (&pg)[kPages]) __attribute__((always_inline)) {
+    if constexpr (!kWhole)
+#pragma unroll
+      for (int n = 0; n < NI; ++n) asm volatile("" : "+v"(pg[n]));
   };
   const uint32_t w_lds = wave * NI * 1024;
 
   const int kk = (lane & 15) >> 2;                               // what this lane reads: as in kv_prompt.hip
   const uint32_t k_lane = col * RB + 16 * (half ^ (((col & 3) << 2) | ((col >> 2) & 3)));
   const uint32_t v_lane = (4 * half + kk) * RB + 64 * kk + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) + 8 * (lane & 1);
-  u32x4 kf[KS], vf[2][HT];                                       // operands: keys of a step; values of its first and second 16 keys
+  u32x4 kf[KS], vf[HT];                                          // operands: keys of a step; values of 16 of its keys
   bf16x8 qf[2][KS];
   auto read_key = [&](uint32_t K, int ks) __attribute__((always_inline)) { kf[ks] = read_lds(K ^ (32 * ks)); };
-  auto read_value = [&](uint32_t V, int pp, int n) __attribute__((always_inline)) {   // n: channel block and half of the operand
+  auto read_value = [&](uint32_t V, int n) __attribute__((always_inline)) {   // n: channel block and half of the operand
     const uint32_t p = V ^ (64 * (n >> 1));
     const u32x2 w = read_transposed(n & 1 ? (p ^ 32) + 8 * RB : p);
-    vf[pp][n >> 1][2 * (n & 1)] = w.x;
-    vf[pp][n >> 1][2 * (n & 1) + 1] = w.y;
+    vf[n >> 1][2 * (n & 1)] = w.x;
+    vf[n >> 1][2 * (n & 1) + 1] = w.y;
   };
 
   // A row's reference is the largest score of the first keys that it sees.  Where later ones would have weights of more than
   // kFarSum the reference is raised, but not the sums so far: then all is done once more, from the references that the first time
   // ended with, which nothing exceeds as far.  (A rescaling would have the sums in registers that vector instructions reach, and copied
   // there and back around every step.)
+  typedef PromptWeights<2> Weights;                               // of a row and 32 keys
+  auto keep = [](Weights& w, int pp) __attribute__((always_inline)) { asm volatile("" : "+a"(w.upper[pp]), "+a"(w.lower[pp])); };   // (as kf and vf)
   bool once_more = false;
   // Step i = 2 j + t: scores sn of step i + 1 (operands there), weights pn of step i from its scores sc, and the values of step i - 1
-  // times its weights pc.  K: where the keys of step i + 2 are; V1: the second 16 values of step i - 1; V0: the first 16 of step i.
-  // ask(n): what is asked for behind matrix instruction n.
-  auto step = [&](bool whole, int k0, f32x16 (&sc)[2], f32x16 (&sn)[2], u32x4 (&pc)[2][2], u32x4 (&pn)[2][2], uint32_t K, uint32_t V1, uint32_t V0, auto&& ask) __attribute__((always_inline)) {
+  // times its weights pc.  K: where the keys of step i + 2 are; V: the values of step i - 1.
+  // ask(n): what is asked for behind matrix instruction n.  Of three of these instructions two have an exponential behind them, the third
+  // divides the two weights into their operands.
+  auto step = [&](bool whole, int k0, f32x16 (&sc)[2], f32x16 (&sn)[2], Weights (&pc)[2], Weights (&pn)[2], uint32_t K, uint32_t V, auto&& ask) __attribute__((always_inline)) {
     if (!whole) {                                                // some of these keys are not for some of the rows
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -203,36 +225,35 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
       }
     }
     asm volatile("" : "+v"(sc[0]), "+v"(sc[1]));                 // (not in the accumulation registers)
-    float sum[2] = {0.f, 0.f}, next = fmaf(sc[0][0], scale, -m[0]), w0 = 0.f, w1 = 0.f;
-    auto pack = [&](int n) __attribute__((always_inline)) {      // weights n - 2 and n - 1
-      const int u = (n - 2) >> 4, e = (n - 2) & 15;
-      const bf16x2 w = {(__bf16)w0, (__bf16)w1};
-      sum[u] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[u], false);
-      pn[u][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
-    };
+    float sum[2] = {0.f, 0.f}, w0 = 0.f, w1 = 0.f;
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int n = 0; n < 32; ++n) {
-      if (n < 2 * KS) {
-        const int ks = n >> 1, u = n & 1;
+    each([&](auto index) __attribute__((always_inline)) {
+      constexpr int n = decltype(index)::value;
+      if constexpr (n < 2 * KS) {
+        constexpr int ks = n >> 1, u = n & 1;
         if (u == 0) asm volatile("" : "+a"(kf[ks]));
         sn[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[ks]), qf[u][ks], ks ? sn[u] : f32x16{}, 0, 0, 0);
       } else {
-        const int q = n - 2 * KS, pp = q / (2 * HT), h = (q >> 1) % HT, u = q & 1;
-        if (u == 0) asm volatile("" : "+a"(vf[pp][h]));
-        o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[pp][h]), __builtin_bit_cast(bf16x8, pc[u][pp]), o[u][h], 0, 0, 0);
+        constexpr int q = n - 2 * KS, pp = q / (4 * HT), h = (q >> 2) % HT, part = (q >> 1) & 1, u = q & 1;
+        if ((q & 3) == 0) asm volatile("" : "+a"(vf[h]));
+        o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[h]), __builtin_bit_cast(bf16x8, part ? pc[u].lower[pp] : pc[u].upper[pp]), o[u][h], 0, 0, 0);
       }
-      if (n < 2 * HT) read_value(V1, 1, n);
-      else if (n >= 4 * HT && n < 4 * HT + KS) read_key(K, n - 4 * HT);
-      else if (n >= 6 * HT) read_value(V0, 0, n - 6 * HT);
-      ask(n);
-      if (n >= 2 && (n & 1) == 0) pack(n);
-      const float w = exp2_raw(next);
-      if (n & 1) w1 = w; else w0 = w;
-      if (n < 31) next = fmaf(sc[(n + 1) >> 4][(n + 1) & 15], scale, -m[(n + 1) >> 4]);
+      // (operands are asked for when their registers are free, and those of the products before are no longer needed)
+      if (n < 2 * HT) read_value(V, n);
+      else if (n >= 2 * KS + 4 && n < 2 * KS + 4 + 4 * HT && n % 4 < 2) read_value(V + 16 * RB, (n - 2 * KS - 4) / 4 * 2 + n % 4);
+      else if (n >= 48 - KS) read_key(K, n - 48 + KS);
+      ask(index);
+      constexpr int u = n / 24, e = 2 * (n % 24 / 3) + n % 3;    // weight e of set u, or the two before
+      if constexpr (n % 3 < 2) {
+        const float w = exp2_raw(fmaf(sc[u][e & 15], scale, -m[u]));
+        sum[u] += w;
+        if (n % 3) w1 = w; else w0 = w;
+      } else {
+        pn[u].put(e - 2, w0, w1);
+        if constexpr (e % 8 == 0) keep(pn[u], e / 8 - 1);
+      }
       __builtin_amdgcn_sched_barrier(0);
-    }
-    pack(32);
+    }, std::make_integer_sequence<int, 48>());
     if (__builtin_expect(__any(!(sum[0] < kFarSum) || !(sum[1] < kFarSum)), 0)) {   // (the first keys that a row sees, too)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -246,9 +267,11 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
         sum[u] = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const bf16x2 w = {(__bf16)exp2_raw(fmaf(sc[u][e], scale, -to)), (__bf16)exp2_raw(fmaf(sc[u][e + 1], scale, -to))};
-          sum[u] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[u], false);
-          pn[u][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, w);
+          const float a0 = exp2_raw(fmaf(sc[u][e], scale, -to)), a1 = exp2_raw(fmaf(sc[u][e + 1], scale, -to));
+          sum[u] += a0;
+          sum[u] += a1;
+          pn[u].put(e, a0, a1);
+          if (e % 8 == 6) keep(pn[u], e / 8);
         }
       }
     }
@@ -285,17 +308,16 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
     if constexpr (!kWhole) pages(1, pg);
     find(0, pg0);
 #pragma unroll
-    for (int n = 0; n < NI / 4; ++n) ask_keys(Kb + w_lds, n);
-    if constexpr (kWhole) find(1, pg0); else find(1, pg);
+    for (int n = 0; n < NI / 4; ++n) ask_keys(Kb + w_lds, n, 0, pg0);
+    find(1, pg0);
 #pragma unroll
-    for (int n = 0; n < NI / 4; ++n) { ask_values(Vb + w_lds, n); ask_keys(Kb + BB + w_lds, n); }
+    for (int n = 0; n < NI / 4; ++n) { ask_values(Vb + w_lds, n, 1); ask_keys(Kb + BB + w_lds, n, 1, kWhole ? pg0 : pg); }
     if constexpr (kWhole) pg[0] = pg0[0]; else pages(2, pg);
   }
   // (the first step has no values yet: its weights are zeros, and so is what they multiply)
   for (int i = tid; i < BB / 16; i += GT) *(lds_u32x4)(uintptr_t)(Vb + 2 * BB + 16 * i) = u32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int h = 0; h < HT; ++h) vf[0][h] = u32x4{0, 0, 0, 0};
   wait_loads();
+  loaded(pg);
   __syncthreads();
 
 #pragma unroll
@@ -307,7 +329,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
       for (int e = 0; e < 16; ++e) o[u][i][e] = 0.f;
   }
   f32x16 s0[2], s1[2];
-  u32x4 w0[2][2] = {}, w1[2][2] = {};
+  Weights w0[2] = {}, w1[2] = {};
   // scores of step 0, and the keys of step 1
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) read_key(Kb + k_lane, ks);
@@ -321,7 +343,6 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   uint32_t v_before = Vb + 2 * BB, v_now = Vb;
   for (int j = 0; j < n_it; ++j) {
     find(j + 2, pg);
-    if constexpr (!kWhole) pages(j + 3, pg);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -330,22 +351,24 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
     const bool whole = j >= all_lo && j < all_hi;
     const int k0 = whole ? 0 : mine_too ? start_of(block_of(j)) : -(1 << 30);
     const uint32_t K = Kb + ((j + 1) & 1) * BB + k_lane, v_next = v_now == Vb + 2 * BB ? Vb : v_now + BB, k_lds = Kb + (j & 1) * BB + w_lds;
-    step(whole, k0, s0, s1, w1, w0, K, v_before + v_lane + 48 * RB, v_now + v_lane, [&](int n) __attribute__((always_inline)) {
-      if (n % 4 == 0 && n / 4 < NI / 2) { if (n & 4) ask_keys(k_lds, n / 8); else ask_values(v_next + w_lds, n / 8); }
+    step(whole, k0, s0, s1, w1, w0, K, v_before + v_lane + 32 * RB, [&](auto index) __attribute__((always_inline)) {
+      constexpr int n = decltype(index)::value;
+      if constexpr (n % 4 == 0 && n / 4 < NI / 2) { if constexpr (n & 4) ask_keys(k_lds, n / 8, j + 2, pg); else ask_values(v_next + w_lds, n / 8, j + 2); }
     });
-    step(whole, k0 + (mine_too ? 32 : 0), s1, s0, w0, w1, K + 32 * RB, v_now + v_lane + 16 * RB, v_now + v_lane + 32 * RB, [](int) {});
+    if constexpr (!kWhole) pages(j + 3, pg);
+    step(whole, k0 + (mine_too ? 32 : 0), s1, s0, w0, w1, K + 32 * RB, v_now + v_lane, [](auto) {});
     v_before = v_now;
     v_now = v_next;
     wait_loads();
+    loaded(pg);
     __syncthreads();
   }
   // the values of the last step
 #pragma unroll
-  for (int n = 0; n < 2 * HT; ++n) read_value(v_before + v_lane + 48 * RB, 1, n);
-#pragma unroll
-  for (int n = 0; n < 4 * HT; ++n) {
-    const int pp = n / (2 * HT), h = (n >> 1) % HT, u = n & 1;
-    o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[pp][h]), __builtin_bit_cast(bf16x8, w1[u][pp]), o[u][h], 0, 0, 0);
+  for (int n = 0; n < 8 * HT; ++n) {
+    const int pp = n / (4 * HT), h = (n >> 2) % HT, part = (n >> 1) & 1, u = n & 1;
+    if ((n & 3) == 0) { read_value(v_before + v_lane + (32 + 16 * pp) * RB, 2 * h); read_value(v_before + v_lane + (32 + 16 * pp) * RB, 2 * h + 1); }
+    o[u][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[h]), __builtin_bit_cast(bf16x8, part ? w1[u].lower[pp] : w1[u].upper[pp]), o[u][h], 0, 0, 0);
   }
   __syncthreads();
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
