@@ -532,8 +532,9 @@ class QkPrep:
     """What happens to query and key heads on their way into a cache (mdi_qk_prep), made by KvCache.prep; keeps its device
     vectors alive."""
 
-    def __init__(self, keep, struct, device):
+    def __init__(self, keep, struct, device, gains_of):
         self._keep, self._c, self.device = keep, struct, device
+        self.gains_of = gains_of                                 # channels of a head that the gains are for; None: there are none
         self._ref = C.byref(struct)
 
 
@@ -584,7 +585,8 @@ class KvCache(_PagedCache):
                 raise ValueError("freq [rot / 2]")
             rot = 2 * freq.shape[0]
         keep = (q_gain, q_bias, k_gain, k_bias, freq)
-        return QkPrep(keep, MdiQkPrep(*[_ptr(t) for t in keep], eps, _NORMS[norm], rot), self.device)
+        gains_of = None if q_gain is None and k_gain is None else self.h
+        return QkPrep(keep, MdiQkPrep(*[_ptr(t) for t in keep], eps, _NORMS[norm], rot), self.device, gains_of)
 
     def _away(self, t):
         """Is tensor t somewhere else than the cache?"""
@@ -605,6 +607,8 @@ class KvCache(_PagedCache):
         device, n = self.device, rows.n_rows
         if (rows.device is not device and rows.device != device) or (prep is not None and prep.device is not device and prep.device != device):
             raise ValueError(f"append: rows and prep on {device}")
+        if prep is not None and prep.gains_of is not None and prep.gains_of != self.h:
+            raise ValueError(f"append: prep for heads of {prep.gains_of}, not of {self.h}")
         kp, k_row, k_head = self._heads(k, self.K, n, "k")
         vp, v_row, v_head = self._heads(v, self.K, n, "v")
         if k_row != v_row or k_head != v_head:

@@ -169,3 +169,15 @@ def test_the_formulas():
     x, _ = heads(np.array([[[1.0, 0, 0, 5]]]), [3], freq=[np.pi / 6])          # a quarter turn of channels 0 and 1
     assert np.allclose(x, [[[0, 1, 0, 5]]])
     assert mdi.rope_freq(8, 16.0, "cpu").tolist() == [1.0, 0.5, 0.25, 0.125]
+
+
+def test_a_preparation_for_heads_of_another_size():
+    """Gains and biases are as long as a head of the cache that the preparation was made by: the call cannot know."""
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    small, large = (mdi.KvCache(z(3, 2, 2, 16, h), z(2, 4, dtype=torch.int32)) for h in (64, 128))
+    for ours, theirs, h in ((large, small, 128), (small, large, 64)):
+        g, rows = z(theirs.h, dtype=torch.float32), ours.rows(z(2, dtype=torch.int32), z(3, dtype=torch.int32), n_rows=4)
+        x, q = z(4, 2, h), z(4, 6, h)
+        for gains in (dict(q_gain=g), dict(k_gain=g, k_bias=g), dict(q_gain=g, k_gain=g, norm="layer")):
+            with pytest.raises(ValueError, match=f"heads of {theirs.h}"):
+                ours.append(rows, x, x, q, theirs.prep(**gains))
