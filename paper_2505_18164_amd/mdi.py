@@ -111,7 +111,7 @@ def lib():
         L.mdi_kv8_attn.argtypes = [kv8, rows, vp, u64, u32, C.c_float, vp, u64, vp, C.c_size_t, vp]
         L.mdi_kv8_attn_bytes.argtypes = [kv8, rows, u32, C.POINTER(C.c_size_t)]
         kv, prep = C.POINTER(MdiKv), C.POINTER(MdiQkPrep)
-        # (whole numbers as void pointers, which are passed alike: ctypes takes half the time over them)
+        # (whole numbers as void pointers, which are passed alike: ctypes takes half the time over them, and cuts them no less)
         L.mdi_kv_append.argtypes = [kv, rows, prep] + [vp] * 11
         L.mdi_kv_attn.argtypes = [kv, rows, vp, vp, vp, C.c_float] + [vp] * 7
         L.mdi_kv_attn_bytes.argtypes = [kv, rows, u32, u32, u32, C.POINTER(C.c_size_t)]
@@ -616,6 +616,8 @@ class KvCache(_PagedCache):
         qp, q_row, q_head, heads, op, out_row = None, 0, 0, 0, None, 0
         if q is not None:
             heads = q.shape[1] if q.dim() == 3 else 0
+            if heads >> 32:
+                raise ValueError("append: heads beyond 32 bits")
             qp, q_row, q_head = self._heads(q, heads, n, "q")
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -629,6 +631,8 @@ class KvCache(_PagedCache):
 
     def workspace(self, rows, n_head, window=0, sinks=0):
         """A workspace for attn calls on these rows (None when none is needed)."""
+        if not (0 <= n_head < 1 << 32 and 0 <= window < 1 << 32 and 0 <= sinks < 1 << 32):   # (the C call would see what ctypes leaves of them)
+            raise ValueError("n_head, window, sinks: beyond 32 bits")
         n = C.c_size_t(0)
         st = lib().mdi_kv_attn_bytes(self._ref, rows._ref, n_head, window, sinks, C.byref(n))
         if st != MDI_OK:
@@ -646,9 +650,9 @@ class KvCache(_PagedCache):
                 or qs[2] != 1 or os[2] != 1 or (shape[1] > 1 and (qs[1] != h or os[1] != h)) or self._away(q) or self._away(out)
                 or (rows.device is not device and rows.device != device)):
             raise ValueError(f"attn: q and out {dtype} [rows, heads, {h}] on {device}, heads next to each other")
-        if not (0 <= window < 1 << 32 and 0 <= sinks < 1 << 32):
-            raise ValueError("window, sinks: beyond 32 bits")
         heads = shape[1]
+        if not (heads < 1 << 32 and 0 <= window < 1 << 32 and 0 <= sinks < 1 << 32):
+            raise ValueError("heads, window, sinks: beyond 32 bits")
         if workspace is None:
             workspace = self.workspace(rows, heads, window, sinks)
         elif self._away(workspace) or not workspace.is_contiguous():

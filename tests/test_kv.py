@@ -181,3 +181,16 @@ def test_a_preparation_for_heads_of_another_size():
         for gains in (dict(q_gain=g), dict(k_gain=g, k_bias=g), dict(q_gain=g, k_gain=g, norm="layer")):
             with pytest.raises(ValueError, match=f"heads of {theirs.h}"):
                 ours.append(rows, x, x, q, theirs.prep(**gains))
+
+
+def test_counts_beyond_32_bits_are_not_cut():
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    cache = mdi.KvCache(z(3, 2, 2, 16, 64), z(2, 1000, dtype=torch.int32))
+    rows = cache.rows(z(2, dtype=torch.int32), z(3, dtype=torch.int32), n_rows=4)
+    for heads, kw in ((4, dict(window=1 << 32)), (4, dict(window=-1)), (4, dict(window=5, sinks=(1 << 32) + 4)), (4, dict(sinks=-1)), ((1 << 32) + 4, {}), (-4, {})):
+        with pytest.raises(ValueError, match="32 bits"):
+            cache.workspace(rows, heads, **kw)
+    many = z(1, 1, 64).expand(4, (1 << 32) + 4, 64)                            # one head in the place of all
+    x = z(4, 2, 64)
+    with pytest.raises(ValueError, match="32 bits"):
+        cache.append(rows, x, x, many)
