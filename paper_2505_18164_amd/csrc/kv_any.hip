@@ -89,8 +89,8 @@ __global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(
     kv = rest / groups;
     const int head0 = kv * G + 16 * (rest - kv * groups), heads = min(16, kv * G + G - head0);
     const int seen = __builtin_amdgcn_readfirstlane(kv8_seen(c, r, sample));
-    which = __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample));
-    none = !seen || which < 0;
+    which = seen ? __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample)) : -1;
+    none = which < 0;
     first_pos = last_pos = seen - 1;
     sample_row[0] = sample; head[0] = head0 + min(col, heads - 1); pos[0] = seen - 1; live[0] = col < heads;
   } else {
@@ -100,8 +100,8 @@ __global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(
     // (a sample's longest rows first)
     const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp, head0 = set << g_sh, end = min(q0 + bp, at.rows);
     kv = head0 / (a.H / c.K);
-    which = kv8_checked_row(c, at.table);
-    none = at.pos < 0 || which < 0;
+    which = at.pos < 0 ? -1 : kv8_checked_row(c, at.table);
+    none = which < 0;
     const long far = (long)at.pos + end;
     if (!none && far > r.max_ctx) kv8_report(c);
     auto pos_of = [&](int row) { return (int)min((long)at.pos + min(row, at.rows - 1), (long)r.max_ctx - 1); };

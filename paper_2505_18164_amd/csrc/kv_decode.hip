@@ -80,12 +80,12 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv_decode(KvCache c, KvRows 
       x0 = x1;
     }
     const int kv = unit / groups, head0 = kv * G + 16 * (unit - kv * groups), heads = min(16, kv * G + G - head0);
-    const int which = __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample));
+    const int which = n_places ? __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample)) : -1;   // (who takes no part may have any table)
     const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
     const KvSpan span = kv_span(a.sight, __builtin_amdgcn_readfirstlane(kv8_seen(c, r, sample)));
     bf16_t* out = (bf16_t*)a.out + (long)sample * a.out_stride + (long)head0 * HD;
-    if (a.plan.splits > 1 && piece <= 0 && threadIdx.x < heads) kv_part_counts(a, c, r)[sample * a.H + head0 + threadIdx.x] = n_places && which >= 0 ? pieces : 1;
-    if (!n_places || which < 0) {
+    if (a.plan.splits > 1 && piece <= 0 && threadIdx.x < heads) kv_part_counts(a, c, r)[sample * a.H + head0 + threadIdx.x] = which >= 0 ? pieces : 1;
+    if (which < 0) {
       if (piece <= 0) for (int e = threadIdx.x; e < heads * HD; e += 64 * kWaves) out[e] = 0;
       continue;
     }

@@ -53,13 +53,13 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   if (at.sample < 0) return;
   const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
   const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
-  const int which = kv8_checked_row(c, at.table), p0 = at.pos;
+  const int p0 = at.pos, which = p0 < 0 ? -1 : kv8_checked_row(c, at.table);
   const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
   const int col = lane & 31, half = lane >> 5, head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
   int row[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) row[u] = q0 + ((64 * wave + 32 * u + col) >> g_sh);
-  if (p0 < 0 || which < 0) {                                     // takes no part
+  if (which < 0) {                                               // takes no part
 #pragma unroll
     for (int u = 0; u < 2; ++u)
       if (blockIdx.y == 0 && grp == 0 && row[u] < at.rows) prompt_zeros<HT>(c, r, a, at, row[u], head);

@@ -541,3 +541,29 @@ def test_many_samples(dtype, crowd):
             t = Setup(4, 2, h, 16, [1] * 700, behind, dtype, *sight, seed=2)
             cache = t.cache()
             t.check(t.attn(cache, t.plan(cache, one_each=True)))
+
+
+@pytest.mark.parametrize("h,dtype,crowd", KINDS, ids=KIND_IDS)
+def test_samples_that_take_no_part_may_have_any_table(h, dtype, crowd):
+    """An idle place of a server's batch: no position, and the table number of a sample that is gone.  Nothing depends on it, so nothing is
+    reported; appended rows and queries of it are left as they are, its results are zeros."""
+    s = Setup(4, 2, h, 16, [20, 3, 40], [0, 40, 700], dtype, seed=1, rows_behind=crowd // 4)
+    pos, table = dev(np.array([0, -1, 700], np.int32)), dev(np.array([0, 10 ** 9, 2], np.int32))
+    cache = s.cache()
+    k = torch.randn((s.rows, 2, h), device=DEV).to(dtype)
+    for behind in (0, 3000):                                      # divided into pieces, too
+        plan = cache.rows(pos, start=dev(s.start), table=table, n_rows=s.rows, max_ctx=min(s.max_ctx + behind, s.tables.shape[1] * 16))
+        out = s.attn(cache, plan)
+        assert (out[20:23] == 0).all()
+        want = s.want()
+        may = bound(*want, h, dtype)
+        rows = np.r_[0:20, 23:63]
+        within(out[rows], want[0][rows], may[rows])
+    tokens = cache.rows(dev(np.array([19, -1, 739], np.int32)), table=table)
+    out = cache.attn(tokens, s.q[[19, 22, 62]].to(DEV))
+    assert (out[1] == 0).all()
+    within(out[[0, 2]], want[0][[19, 62]], may[[19, 62]])
+    q = torch.full((3, 4, h), 5.0, device=DEV).to(dtype)
+    cache.append(tokens, k[:3], k[:3].clone(), q.clone(), cache.prep(freq=mdi.rope_freq(h)), q_out=q)
+    assert (q[1] == 5.0).all()
+    cache.check()
