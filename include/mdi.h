@@ -494,8 +494,8 @@ typedef struct mdi_kv8 {
  * buffers (start[0] = 0, never falling, at most n_rows; a sample may have none);
  * NULL: one row per sample, row i is sample i's (then n_rows = n).  pos: device
  * int32 [n], the position of a sample's first row (its others follow); below 0:
- * the sample takes no part.  table: device int32 [n], the row of mdi_kv8.tables
- * that is the sample's; NULL: row i.  n_rows: rows of the buffers, at most 2^24;
+ * the sample takes no part, whatever its table.  table: device int32 [n], the row of
+ * mdi_kv8.tables that is the sample's; NULL: row i.  n_rows: rows of the buffers, at most 2^24;
  * those from start[n] on belong to nobody and are left as they are.  max_ctx:
  * host's bound of pos + rows over all samples, at most table_stride *
  * page_tokens; it decides how the work is divided and whether what is read keeps a

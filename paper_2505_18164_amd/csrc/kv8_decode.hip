@@ -83,12 +83,12 @@ __global__ __launch_bounds__(64 * kWaves, 3) void k_kv8_decode(Kv8Cache c, Kv8Ro
       x0 = x1;
     }
     const int kv = unit / groups, head0 = kv * G + 16 * (unit - kv * groups), heads = min(16, kv * G + G - head0);
-    const int which = __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample));
+    const int which = seen ? __builtin_amdgcn_readfirstlane(kv8_table_row(c, r, sample)) : -1;   // (who takes no part may have any table)
     const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
     int at0 = kv8_page_of(c, lo);
     const int first = at0 + (int)threadIdx.x < c.table_stride ? table[at0 + threadIdx.x] : 0;
     bf16_t* out = a.out + (long)sample * a.out_stride + (long)head0 * HD;
-    if (!seen || which < 0) {
+    if (which < 0) {
       if (piece <= 0) for (int e = threadIdx.x; e < heads * HD; e += 64 * kWaves) out[e] = 0;
       continue;
     }

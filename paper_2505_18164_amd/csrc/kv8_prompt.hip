@@ -89,13 +89,13 @@ __global__ __launch_bounds__(512, 2) void k_kv8_prompt(Kv8Cache c, Kv8Rows r, Kv
   if (at.sample < 0) return;
   const int g_sh = geo.g_sh, bp = BQ >> g_sh, head0 = set << g_sh, kv = head0 / (a.H / c.K);
   const int q0 = ((at.rows + bp - 1) / bp - 1 - at.block) * bp;  // first row of the sample in this block
-  const int which = kv8_checked_row(c, at.table), p0 = at.pos;
+  const int p0 = at.pos, which = p0 < 0 ? -1 : kv8_checked_row(c, at.table);
   const int32_t* table = c.tables + (long)max(which, 0) * c.table_stride;
   const int col = lane & 31, half = lane >> 5;
   const int row = q0 + ((32 * wave + col) >> g_sh), head = head0 + (col & ((1 << g_sh) - 1));   // (32 is a multiple of 2^g_sh)
   const bool live = row < at.rows;
   bf16_t* out = a.out + (long)(at.first + row) * a.out_stride + (long)head * HD;
-  if (p0 < 0 || which < 0) {                                     // takes no part
+  if (which < 0) {                                               // takes no part
     if (blockIdx.y == 0 && grp == 0 && live)
 #pragma unroll
       for (int i = 0; i < HT; ++i)

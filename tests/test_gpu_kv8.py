@@ -471,3 +471,25 @@ def test_two_calls_at_once():
                 got[i].append(cache.attn(rows, q) if i == 0 else cache.attn(tokens, q[:2]))
     torch.cuda.synchronize()
     assert all(torch.equal(x, alone[i]) for i in range(2) for x in got[i])
+
+
+@pytest.mark.parametrize("h", [64, 128, 40])
+def test_samples_that_take_no_part_may_have_any_table(h):
+    """An idle place of a server's batch names the table of a sample that is gone: nothing depends on it, so nothing is reported."""
+    s = Setup(8, 2, h, 16, [20, 3, 40], [0, 40, 700], seed=1)
+    dev = lambda x: torch.from_numpy(np.array(x, dtype=np.int32)).to("cuda:0")
+    pos, table = dev([0, -1, 700]), dev([0, 10 ** 9, 2])
+    cache = s.cache()
+    want = s.want()
+    for max_ctx in (s.max_ctx, s.tables.shape[1] * 16):
+        out = cache.attn(cache.rows(pos, start=dev(s.start), table=table, n_rows=s.rows, max_ctx=max_ctx), s.q.to("cuda:0"))
+        assert (out[20:23] == 0).all()
+        rows = np.r_[0:20, 23:63]
+        check(out[rows], [w[rows] for w in want], h)
+    tokens = cache.rows(dev([19, -1, 739]), table=table)
+    out = cache.attn(tokens, s.q[[19, 22, 62]].to("cuda:0"))
+    assert (out[1] == 0).all()
+    check(out[[0, 2]], [w[[19, 62]] for w in want], h)
+    k = torch.randn((3, 2, h), device="cuda:0")
+    cache.write(tokens, k, k.clone())
+    cache.check()
