@@ -201,7 +201,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   // The weights of block j from its scores.
   float alpha = 1.f;
   bool raised = false;
-  auto weigh = [&]() __attribute__((always_inline)) {
+  auto weigh = [&](const float (&x)[2][16]) __attribute__((always_inline)) {
     float sum;
     auto weights = [&]() __attribute__((always_inline)) {
       sum = 0.f;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const float w0 = exp2_raw(fmaf(s[t][e], scale, -m)), w1 = exp2_raw(fmaf(s[t][e + 1], scale, -m));
+          const float w0 = exp2_raw(fmaf(x[t][e], scale, -m)), w1 = exp2_raw(fmaf(x[t][e + 1], scale, -m));
           sum += w0;
           sum += w1;
           pf.put(16 * t + e, w0, w1);
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[t][e]);
       top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;         // both lanes of a row raise alike
       const float to = fmaxf(m, top);
       alpha = exp2_raw(m - to);
@@ -239,15 +239,20 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
       return;
     }
     const int k0 = start_of(block_of(j));
+    float x[2][16];                                              // (from here on scalars: hipcc lost elements of a vector of which one was replaced under a condition)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = s[t][e];
     if (k0 + BK - 1 > wave_pos || (k0 <= last_pos - a.sight.window && k0 + BK > a.sight.sinks)) {   // some of these keys are not for some of the rows
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const uint32_t seen = seen_keys(pos - k0 - 32 * t, a.sight.window, a.sight.sinks - k0 - 32 * t) >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = masked(s[t][e], seen, 8 * (e >> 2) + (e & 3));
+        for (int e = 0; e < 16; ++e) x[t][e] = masked(x[t][e], seen, 8 * (e >> 2) + (e & 3));
       }
     }
-    weigh();
+    weigh(x);
   };
 
   // Of the wavefronts of a SIMD, w and w + 4, one multiplies while the other takes exponentials: in a step the early four multiply and

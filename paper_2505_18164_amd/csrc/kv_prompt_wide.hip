@@ -216,15 +216,21 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   // ask(n): what is asked for behind matrix instruction n.  Of three of these instructions two have an exponential behind them, the third
   // divides the two weights into their operands.
   auto step = [&](bool whole, int k0, f32x16 (&sc)[2], f32x16 (&sn)[2], Weights (&pc)[2], Weights (&pn)[2], uint32_t K, uint32_t V, auto&& ask) __attribute__((always_inline)) {
+    float x[2][16];                                              // (from here on scalars: hipcc lost elements of a vector of which one was replaced under a condition)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[u][e] = sc[u][e];
     if (!whole) {                                                // some of these keys are not for some of the rows
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint32_t seen = k0 < 0 ? 0u : seen_keys(pos[u] - k0, a.sight.window, a.sight.sinks - k0) >> (4 * half);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[u][e] = masked(sc[u][e], seen, 8 * (e >> 2) + (e & 3));
+        for (int e = 0; e < 16; ++e) x[u][e] = masked(x[u][e], seen, 8 * (e >> 2) + (e & 3));
       }
     }
-    asm volatile("" : "+v"(sc[0]), "+v"(sc[1]));                 // (not in the accumulation registers)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(x[0][e]), "+v"(x[1][e]));   // (not in the accumulation registers)
     float sum[2] = {0.f, 0.f}, w0 = 0.f, w1 = 0.f;
     __builtin_amdgcn_sched_barrier(0);
     each([&](auto index) __attribute__((always_inline)) {
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
       ask(index);
       constexpr int u = n / 24, e = 2 * (n % 24 / 3) + n % 3;    // weight e of set u, or the two before
       if constexpr (n % 3 < 2) {
-        const float w = exp2_raw(fmaf(sc[u][e & 15], scale, -m[u]));
+        const float w = exp2_raw(fmaf(x[u][e & 15], scale, -m[u]));
         sum[u] += w;
         if (n % 3) w1 = w; else w0 = w;
       } else {
@@ -259,7 +265,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
       for (int u = 0; u < 2; ++u) {
         float top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[u][e]);
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
         top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;       // both lanes of a row raise alike
         const float to = top > m[u] + 25.f ? top : m[u];         // (32 weights of up to 2^25 are no more than kFarSum: other rows' references stay)
         once_more |= to > m[u] && m[u] != kKvNone;
@@ -267,7 +273,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
         sum[u] = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const float a0 = exp2_raw(fmaf(sc[u][e], scale, -to)), a1 = exp2_raw(fmaf(sc[u][e + 1], scale, -to));
+          const float a0 = exp2_raw(fmaf(x[u][e], scale, -to)), a1 = exp2_raw(fmaf(x[u][e + 1], scale, -to));
           sum[u] += a0;
           sum[u] += a1;
           pn[u].put(e, a0, a1);
