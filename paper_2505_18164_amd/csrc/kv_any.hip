@@ -25,10 +25,6 @@
 namespace mdi {
 namespace {
 
-// Wavefronts of a workgroup.  (Of heads of more than 128 channels a SIMD holds one: two workgroups of two are busy when one of four waits: 2633
-// rows of 8 heads of 256 in bf16 111 -> 93 us, in fp32 204 -> 191; the 2462 rows above with 8, 4 and 2: 67, 52, 52, 2633 of TinyLlama's shape 211,
-// 179, 189.)
-constexpr int waves_of(int padded) { return padded > 128 ? 2 : 4; }
 constexpr float kRaise = 8.f;        // how far (in powers of two) a score may exceed its row's reference before that is raised
 
 // The operands of a step.  K: what a lane has of key `col` of each sixteen; V: channels VB col .. + VB - 1 of keys 4 g + 0..3.
@@ -67,11 +63,11 @@ __device__ __forceinline__ AnySpan any_span(const KvSight& w, int at, int end) {
 
 // kTokens: one row a sample, the columns are up to sixteen query heads of a kv head; else the columns are (position, head) pairs.
 template <typename T, int HD, int S, bool kTokens, bool kMany>
-__global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(KvCache c, KvRows r, KvAttn a, AnyGeo geo) {
+__global__ __launch_bounds__(64 * kv_waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(KvCache c, KvRows r, KvAttn a, AnyGeo geo) {
   typedef Step<T, HD> St;
   constexpr int kKeyStep = 64 / sizeof(T);                       // channels of a key that the four lanes with it read at once
   constexpr int VB = St::VB, KU = St::KU, NG = St::kGroups, KT = 16 * NG, kSteps = 64 / KT;
-  constexpr int kWaves = waves_of(HD);
+  constexpr int kWaves = kv_waves_of(HD);
   constexpr int VP = VB < 4 ? VB : 4, kRow = 16 * VP + 4;         // channels of a lane's VB that are added at a time
   __shared__ long list[kWaves][2][64];                           // rows of the cache of 64 places, and of the next ones
   __shared__ float sums[kWaves][16 * S][kRow];
@@ -433,11 +429,6 @@ __global__ __launch_bounds__(64 * waves_of(HD), HD > 128 ? 1 : 2) void k_kv_any(
   }
 }
 
-int padded(int h) { return h <= 32 ? 32 : h <= 64 ? 64 : h <= 128 ? 128 : 256; }
-// How many sets of sixteen rows a wavefront may have: two where they fit into the registers of two wavefronts a SIMD.
-template <typename T> constexpr int most_sets(int padded) { return padded * sizeof(T) <= 256 ? 2 : 1; }
-int most_sets(const KvCache& c) { return c.dtype == MDI_BF16 ? most_sets<bf16_t>(padded(c.h)) : most_sets<float>(padded(c.h)); }
-
 AnyGeo geo_of(const KvCache& c, const KvRows& r, int H, int sets) {
   const int rows = 16 * sets, sh = std::min(kv_heads_shift(c, H), 4), bp = rows >> sh;   // (a wavefront's sixteen are a multiple of 2^sh)
   return AnyGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
@@ -449,25 +440,25 @@ void launch_sets(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
   AnyGeo g = geo_of(c, r, a.H, S);
   const int total = g.n_blocks * g.sets;
   if (r.n <= kInOrder) {
-    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, false>), dim3(total, a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, g);
+    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, false>), dim3(total, a.plan.splits), dim3(64 * kv_waves_of(HD)), 0, s, c, r, a, g);
     return;
   }
   for (; g.from < total; g.from += kMostWgs)
-    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, g);
+    hipLaunchKernelGGL((k_kv_any<T, HD, S, false, true>), dim3(std::min(kMostWgs, total - g.from), a.plan.splits), dim3(64 * kv_waves_of(HD)), 0, s, c, r, a, g);
 }
 template <typename T, int HD>
 void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (!r.start) {
     const long units = (long)r.n * c.K * kv8_groups(c, a.H);     // (below 2^24: n_rows * H is)
-    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)units, a.plan.splits), dim3(64 * waves_of(HD)), 0, s, c, r, a, AnyGeo{});
+    hipLaunchKernelGGL((k_kv_any<T, HD, 1, true, false>), dim3((unsigned)units, a.plan.splits), dim3(64 * kv_waves_of(HD)), 0, s, c, r, a, AnyGeo{});
     return;
   }
-  if constexpr (most_sets<T>(HD) == 2) if (a.plan.groups == 2) return launch_sets<T, HD, 2>(s, c, r, a);
+  if constexpr (kv_most_sets(HD, sizeof(T)) == 2) if (a.plan.groups == 2) return launch_sets<T, HD, 2>(s, c, r, a);
   launch_sets<T, HD, 1>(s, c, r, a);
 }
 template <typename T>
 void launch_type(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  switch (padded(c.h)) {
+  switch (kv_padded(c.h)) {
     case 32: return launch_heads<T, 32>(s, c, r, a);
     case 64: return launch_heads<T, 64>(s, c, r, a);
     case 128: return launch_heads<T, 128>(s, c, r, a);
@@ -476,26 +467,6 @@ void launch_type(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
 }
 
 }  // namespace
-
-// Two sets of sixteen rows a workgroup read the keys and values half as often, one set is twice as many workgroups: two from 512
-// workgroups on (fp32, 12 heads of 64: 1600 rows 47 against 50 us, 800 rows 29 against 22; bf16 heads of 96: 1600 rows 31 against 34, 800
-// rows 18 against 17).  Pieces only while there is no workgroup for every compute unit, of four blocks or more: 16 fp32 tokens behind
-// 3000 of the TinyLlama shape in 1 piece 40 us, in 2 28, in 4 - a workgroup for each - 23, in 16 26; 2633 rows of it in 1 piece 170, in 2 181.
-KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us) {
-  const int n = std::max(1, std::min(r.n, r.n_rows)), rows = (r.n_rows + n - 1) / n, sh = std::min(kv_heads_shift(c, H), 4);
-  auto wgs_of = [&](int sets) { const int bp = 16 * sets >> sh; return (double)n * ((rows + bp - 1) / bp) * (H >> sh); };
-  const int sets = r.start && most_sets(c) == 2 && rows << sh > 16 && wgs_of(2) >= 512. ? 2 : 1;
-  const double wgs = r.start ? wgs_of(sets) : (double)r.n * c.K * kv8_groups(c, H);
-  const int reach = (int)std::min<long>(r.max_ctx, (long)w.window + (r.start ? 16 * sets >> sh : 1) + w.sinks + 4 * 31);   // places of a workgroup
-  const int most = (reach + 63) / 64;
-  const int want = (int)std::min(64., std::max(1., std::min(most / 4., std::ceil(1024. / waves_of(padded(c.h)) / wgs)))), chunk = (most + want - 1) / want, splits = (most + chunk - 1) / chunk;
-  // 128 keys of a workgroup's rows take `step` us of a compute unit, a workgroup some more to begin and end
-  const bool wide = c.h > 64;
-  const double seen = std::min<double>(reach, r.max_ctx - 0.5 * std::min(r.max_ctx, rows)), step = sets == 2 ? (wide ? 1.35 : 0.8) : (wide ? 0.9 : 0.5);
-  *us = std::max(3 + std::ceil(reach / (128. * splits)), wgs * (seen / 128 * step + splits * (wide ? 3.5 : 2.2)) / 256);
-  if (splits > 1) *us += 2 + (double)r.n_rows * H * (1 / 2000. + splits * (double)c.h / 4e6);
-  return KvPlan{kKvAny, chunk, splits, 0, sets, 0};
-}
 
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (c.dtype == MDI_BF16) launch_type<bf16_t>(s, c, r, a); else launch_type<float>(s, c, r, a);

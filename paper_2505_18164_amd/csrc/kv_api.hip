@@ -1,7 +1,7 @@
 // The entry points of the cache in the storage type (mdi_kv_* of mdi.h): checks on the host, then the launches: one or two, of very many samples a few.
 #include <algorithm>
 
-#include "kv_internal.h"
+#include "kv_plan.h"
 
 using namespace mdi;
 

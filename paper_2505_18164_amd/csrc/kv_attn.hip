@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "kv_device.h"
+#include "kv_plan.h"
 
 namespace mdi {
 namespace {
@@ -99,19 +100,6 @@ void launch_join(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn&
 }
 
 }  // namespace
-
-// Packed rows in bf16 with heads of 64 or 128 are kv_prompt.hip's (256 or 128 rows of position and head to a workgroup) or kv_any.hip's (16
-// or 32), whichever should take less time by their plans: 64 samples of 2 rows behind 500 of the 8B shape 33 against 26 us, 512 rows of
-// the 7B shape 21.4 against 16.5, 512 of 12 heads of 64 14.9 against 9.5, but 24 prompts of 40 rows of the 8B shape 14.5 against 20.5, 8 of 333
-// rows of TinyLlama's 28 against 33.
-KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  if (kv_decode_supported(c, r)) return kv_decode_plan(c, r, H, w);
-  double any_us, us;
-  const KvPlan any = kv_any_plan(c, r, H, w, &any_us);
-  if (!kv_prompt_supported(c, r)) return any;
-  const KvPlan prompt = kv_prompt_plan(c, r, H, w, &us);
-  return any_us < us ? any : prompt;
-}
 
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (a.plan.kernel == kKvDecode) launch_kv_decode(s, c, r, a);

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "kv8_device.h"
+#include "kv_plan.h"
 
 namespace mdi {
 
@@ -20,7 +21,6 @@ __device__ __forceinline__ Span kv_rows_of(const Kv8Rows& r, int i) {
 // one 70 / 75, 300 of up to 30 of the 8B shape 107 / 108, 600 of up to 20 of TinyLlama 101 / 78, 2000 of up to 10 of the 8B shape
 // 1101 / 601.  (What is over costs where the chip is just full: 4 pieces of 64 behind 8000 of the 8B shape, 256 workgroups, 60 us, with as
 // many empty ones between them 96.  Two kernels, because in one that has both the long prompts take 427 us instead of 414.)
-constexpr int kInOrder = 384;
 struct BlockPlace { int sample, block, first, rows, pos, table; };
 template <bool kMany> __device__ __forceinline__ BlockPlace place_of(const Kv8Rows& r, int x, int bp) {
   const int lane = threadIdx.x & 63;
@@ -54,14 +54,6 @@ template <bool kMany> __device__ __forceinline__ BlockPlace place_of(const Kv8Ro
     }
   }
   return BlockPlace{-1, 0, 0, 0, 0, 0};
-}
-
-// Query heads of a kv head that a workgroup's rows take together: the largest power of two that divides their number, up to 32.
-inline int kv_heads_shift(const KvPages& c, int H) {
-  const int G = H / c.K;
-  int sh = 0;
-  while (sh < 5 && G % (2 << sh) == 0) ++sh;
-  return sh;
 }
 
 }  // namespace mdi

@@ -17,6 +17,7 @@
 
 #include "kv8_mfma.h"
 #include "kv_device.h"
+#include "kv_plan.h"
 
 namespace mdi {
 namespace {
@@ -299,27 +300,10 @@ void launch_decode(hipStream_t s, const KvCache& c, const KvRows& r, const KvAtt
 }
 template <int HD>
 void launch_heads(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
-  const bool once = (double)r.n * kv_most_seen(a.sight, r.max_ctx) * c.K * 4 * HD > 128e6;
-  if (once) launch_decode<HD, true>(s, c, r, a); else launch_decode<HD, false>(s, c, r, a);
+  if (kv_decode_once(c, r, a.sight)) launch_decode<HD, true>(s, c, r, a); else launch_decode<HD, false>(s, c, r, a);
 }
 
 }  // namespace
-
-bool kv_decode_supported(const KvCache& c, const KvRows& r) { return !r.start && c.dtype == MDI_BF16 && (c.h == 64 || c.h == 128); }
-
-// (384, 512, 768, 1024 shares: the 8 tokens 62.0, 52.9, 53.2, 55.9 us, the one 110.9, 89.6, 89.2, 91.9, 32 of the 7B shape behind 600 73.1,
-// 63.4, 66.3, 63.5)
-constexpr int kShares = 512;
-constexpr int kLeast = 2;            // tiles of a share, at least
-
-// With many units, or short samples, a unit is a workgroup's.  Else the tiles of all units are cut into equal shares.
-KvPlan kv_decode_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  const int each = c.K * kv8_groups(c, H), most = kv_most_seen(w, r.max_ctx);   // units of a sample
-  if ((long)r.n * each >= 4 * kShares || most <= kLeast * kKv8Tile) return KvPlan{kKvDecode, most, 1, 0, 0, 0};
-  // a unit of t tiles in shares of at least kLeast, and of at least t * each / kShares (it is one of `each` alike)
-  const int tiles = (most + kKv8Tile - 1) / kKv8Tile;
-  return KvPlan{kKvDecode, kLeast * kKv8Tile, std::min(tiles / kLeast, (kShares + each - 1) / each) + 2, kShares, 0, 0};
-}
 
 void launch_kv_decode(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {
   if (c.h == 128) launch_heads<128>(s, c, r, a); else launch_heads<64>(s, c, r, a);

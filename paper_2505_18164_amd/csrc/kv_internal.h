@@ -45,19 +45,13 @@ struct KvAttn {
   float* part; KvPlan plan;
 };
 // One new token per sample in bf16 with heads of 64 or 128: on the matrix cores (kv_decode.hip).
-bool kv_decode_supported(const KvCache& c, const KvRows& r);
-KvPlan kv_decode_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
 void launch_kv_decode(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 // Packed rows in bf16 with heads of 64 or 128: on the matrix cores (kv_prompt.hip).  kv_allow_lds: before the first launch on the current device.
-bool kv_prompt_supported(const KvCache& c, const KvRows& r);
 bool kv_allow_lds();
-KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us);
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
-// Any other, also on the matrix cores, and few packed rows (kv_any.hip).  us: what the call should take, without its launches; of
-// single tokens it is not asked for.
-KvPlan kv_any_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us);
+// Any other, also on the matrix cores, and few packed rows (kv_any.hip).
 void launch_kv_any(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
-KvPlan kv_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w);
+// Whichever of them a.plan names (kv_plan.h), and the launch that adds the pieces.
 void launch_kv_attn(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a);
 
 }  // namespace mdi

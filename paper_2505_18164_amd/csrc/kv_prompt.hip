@@ -367,37 +367,6 @@ PromptGeo geo_of(const KvCache& c, const KvRows& r, int H, int rows) {
   const int sh = kv_heads_shift(c, H), bp = rows >> sh;
   return PromptGeo{r.n_rows / bp + std::min(r.n, r.n_rows), H >> sh, sh, 0};
 }
-// Rows and groups of a workgroup and pieces of a row's blocks.  A step of 64 keys (of 128, with two groups) takes `step` us, a workgroup
-// some more to begin and end; what is divided is added by a second launch.  How long the single samples are is on the device: they are
-// taken for equal, all as long as the longest, so `us` is more than such a call takes (6000 + 2000 + 500 of the 8B shape: 485 us, taken for
-// 800), and serves to compare.  `step` and the rest are fitted to 29 calls with one and two groups and 1 to 16 pieces.
-// Two groups against one: 1024 rows of the 7B shape 31 and 48 us, 2048 68 and 85, 1500 of TinyLlama 30 and 47, 4000 of it 137 and 127, 6000 + 2000 +
-// 500 of the 8B shape 522 and 485.  4 pieces of 64 rows behind 8000 of the 8B shape, two groups in 1, 2, 4 and 8 pieces: 152, 92, 68 and 80 us.
-// Heads of 128 also by workgroups of two wavefronts, two at a time on a compute unit: each reads what four read, but begins and ends beside
-// the other, and 128 rows see fewer keys between them.  Against four: 6000 + 2000 + 500 of the 7B shape with windows of 512, 1024 and
-// 2048 185 and 208, 248 and 266, 353 and 365 us, 8 of 1024 148 and 162; of the 8B shape 487 and 485, 2048 of the 7B shape 83 and 85.
-struct PromptPlan { int rows, groups, splits; double us; };
-PromptPlan prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w) {
-  const int n = std::max(1, std::min(r.n, r.n_rows)), n_rows = (r.n_rows + n - 1) / n, sh = kv_heads_shift(c, H);   // rows of a sample
-  const double heads = (double)r.n_rows * H;
-  struct Form { int rows, groups, at_once; double step, ends; };  // workgroups of a compute unit; us of a step and of a workgroup's beginning and end
-  const Form forms[] = {{256, 1, 1, c.h == 128 ? 2.55 : 1.7, 6}, {128, 2, 1, c.h == 128 ? 2.85 : 1.95, 7}, {128, 1, 2, 2.8, 4}};
-  PromptPlan best{256, 1, 1, 1e30};
-  for (const Form& f : forms) {
-    if (f.at_once == 2 && c.h != 128) continue;
-    const int bp = f.rows >> sh, most = (int)std::min<long>(r.max_ctx, (long)w.window + w.sinks + std::min(bp, n_rows) + 64);
-    const double items = (double)n * ((n_rows + bp - 1) / bp) * (H >> sh), slots = 256 * f.at_once;
-    const double seen = std::min<double>(most, r.max_ctx - 0.5 * std::min(r.max_ctx, n_rows));   // what a workgroup sees, on average
-    for (int s = 1; s <= 32; s *= 2) {
-      if (s > 1 && most < 256 * s) break;
-      double us = std::max(std::ceil(most / (64. * f.groups * s)) * f.step + 6, items / slots * (seen / (64. * f.groups) * f.step + s * f.ends));
-      if (s > 1) us += 2 + heads / 2000 + heads * s * c.h / 4e6;
-      if (us < best.us) best = PromptPlan{f.rows, f.groups, s, us};
-    }
-  }
-  return best;
-}
-
 // A launch has fewer than 2^32 threads.  n_rows * H is below 2^24, so the workgroups of up to kInOrder samples, at most 2^24 / 128 for
 // the rows and H for each sample, are far below that; one for each of very many samples and heads may not be, and go out in several.
 constexpr int kMostWgs = 1 << 22;
@@ -409,21 +378,10 @@ void launch_pages(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn
 
 }  // namespace
 
-bool kv_prompt_supported(const KvCache& c, const KvRows& r) { return r.start && c.dtype == MDI_BF16 && (c.h == 64 || c.h == 128); }
 bool kv_allow_lds() {
   static OncePerDevice done;
   int dev = -1;
   return hipGetDevice(&dev) == hipSuccess && done.run(dev, []() { return allow_one<2, true, false>() && allow_one<2, false, false>() && allow_one<2, true, true>() && allow_one<2, false, true>() && kv_wide_allow_lds(); });
-}
-
-KvPlan kv_prompt_plan(const KvCache& c, const KvRows& r, int H, const KvSight& w, double* us) {
-  const PromptPlan p = prompt_plan(c, r, H, w);
-  // blocks that a workgroup of up to `bp` positions may have: of the first ones, and of a window that begins inside one
-  const int bp = p.rows >> kv_heads_shift(c, H);
-  const long most = std::min<long>(((long)r.max_ctx + 63) / 64, ((long)w.window + bp + 62) / 64 + 1 + ((long)w.sinks + 63) / 64);
-  const int chunk = (int)((most + p.splits - 1) / p.splits);
-  *us = p.us;
-  return KvPlan{kKvPrompt, chunk, (int)((most + chunk - 1) / chunk), 0, p.groups, p.rows};
 }
 
 void launch_kv_prompt(hipStream_t s, const KvCache& c, const KvRows& r, const KvAttn& a) {

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from kv_digits import Setup, check_digits
+from kv_forms import ones
 
 bf16 = lambda x: torch.from_numpy(x).to(torch.bfloat16).double().numpy()
 upper = lambda w: (w.astype(np.float32).view(np.uint32) & np.uint32(0xFFFF0000)).view(np.float32).astype(np.float64)
@@ -55,3 +56,18 @@ def test_a_position_too_few_is_told():
             return w, w
         with pytest.raises(AssertionError):
             check_digits(attend(s, without), s)
+
+
+@pytest.mark.parametrize("K,h,ctx", [(2, 24, 2500), (1, 64, 6000), (2, 128, 700)])
+def test_a_position_more_or_less_is_told_from_ones(K, h, ctx):
+    """Weights that are all alike, every position a one in one channel: any position that is missing, or counted twice."""
+    s = Setup(2 * K, K, h, 16, [1], [ctx - 1], torch.bfloat16, seed=3, change=ones(K, h, 64))
+    check_digits(attend(s, lambda w: (w, w)), s)
+    for p in list(range(0, ctx, 97)) + [63, 64, ctx - 1]:
+        for times in (0.0, 2.0):
+            def other(w):
+                w = w.copy()
+                w[:, p] *= times
+                return w, w
+            with pytest.raises(AssertionError):
+                check_digits(attend(s, other), s)
