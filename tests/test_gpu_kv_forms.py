@@ -4,7 +4,8 @@ import torch
 
 import kv_forms as F
 from kv_cases import Setup
-from kv_digits import check_digits
+from kv_digits import PARTS, check_digits, interval
+from paper_2505_18164_amd import mdi
 
 pytestmark = pytest.mark.gpu
 CALLS = [(f, w) for f in F.FORMS for w in (False, True) if not (w and f in F.NO_WINDOW)]
@@ -44,3 +45,44 @@ def test_every_position_counts_once(form, window):
 
     s, out = tried(form, window, change=F.ones(K, h, border))
     check(s, out, form)
+
+
+@pytest.mark.parametrize("dtype,H,K,h,n,rows", [(torch.bfloat16, 16, 16, 64, 300000, 300000), (torch.float32, 16, 8, 32, 550000, 550000), (torch.bfloat16, 16, 16, 128, 1800000, 600000)],
+                         ids=["bf16", "f32", "bf16, 128"])
+def test_more_workgroups_than_a_launch_may_have(dtype, H, K, h, n, rows):
+    """Single rows of so many samples that their workgroups go out in several launches: all of them, against 64 bits by samples alike."""
+    dev, pt, tables, ctx = "cuda:0", 16, 7, 11
+    form = F.form((dtype, K, h, 1, n, rows, ctx, H, 0, 0), pt, F.plans([(dtype, K, h, 1, n, rows, ctx, H, 0, 0)])[0])
+    assert form in F.FORMS and "many" in form
+    g = torch.Generator(device=dev)
+    g.manual_seed(1)
+    make = lambda *s: torch.randn(s, generator=g, device=dev).to(dtype)
+    data = make(tables, K, 2, pt, h)
+    err = torch.zeros(1, dtype=torch.int32, device=dev)
+    cache = mdi.KvCache(data, torch.arange(tables, dtype=torch.int32, device=dev).unsqueeze(1), err)
+    i = torch.arange(n, device=dev)
+    start = torch.div((torch.arange(n + 1, device=dev) * rows), n, rounding_mode="floor").to(torch.int32)     # none or one each
+    pos, table = (i % ctx).to(torch.int32), (i % tables).to(torch.int32)
+    kinds = 5                                                     # different queries, so that rows are of tables * ctx * kinds kinds
+    some = make(kinds, H, h)
+    mine = torch.repeat_interleave(i, (start[1:] - start[:-1]).long())
+    assert mine.shape == (rows,)
+    q = some[mine % kinds]
+    out = cache.attn(cache.rows(pos, start=start, table=table, n_rows=rows, max_ctx=ctx), q)
+    cache.check()
+    want = torch.empty((tables, ctx, kinds, H, h), dtype=torch.float64)
+    off = torch.empty_like(want)
+    host, hq = data.cpu().double().numpy(), some.cpu().double().numpy()
+    for t in range(tables):
+        for p in range(ctx):
+            for j in range(kinds):
+                a, b = interval(hq[j:j + 1], host[t, :, 0, :p + 1].transpose(1, 0, 2), host[t, :, 1, :p + 1].transpose(1, 0, 2), p, h ** -0.5, each=PARTS if dtype == torch.bfloat16 else 0.0)
+                want[t, p, j], off[t, p, j] = torch.from_numpy(a[0]), torch.from_numpy(b[0])
+    at = (mine % tables, mine % ctx, mine % kinds)
+    if dtype == torch.float32:
+        off += 2.0 ** -24 * want.abs()
+    lo, hi = ((want + s * off).to(dtype).to(dev) for s in (-1, 1))
+    for a in range(0, rows, 1 << 16):
+        part = [x[a:a + (1 << 16)] for x in at]
+        got = out[a:a + (1 << 16)]
+        assert bool(((lo[part[0], part[1], part[2]] <= got) & (got <= hi[part[0], part[1], part[2]])).all()), a
