@@ -313,13 +313,14 @@ __global__ __launch_bounds__(512, 2) void k_kv_prompt(KvCache c, KvRows r, KvAtt
   if (worst >= (unsigned)c.n_pages) kv8_report(c);
   l += __shfl_xor(l, 32, 64);
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
-  // are computed once more, each by itself.  (Weights that are no numbers are what they should be.)
+  // are computed once more, each by itself, and where sums are so large that adding the groups' or pieces' might exceed binary32's
+  // range (kTooLarge).  (Weights that are no numbers are what they should be.)
   {
     float odd = 0.f;
 #pragma unroll
     for (int i = 0; i < HT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) odd = fmaf(o[i][e], 0.f, odd);
+      for (int e = 0; e < 16; ++e) odd = fmaf(o[i][e] * kTooLarge, 0.f, odd);
     if (__any(!(odd == 0.f) && l - l == 0.f)) again = 1;
   }
   __syncthreads();

@@ -20,6 +20,9 @@ constexpr int BK = 64;               // keys of a step
 // when a block's weights sum to more than this: weights of any size keep their digits in their operands and in the sums, which are divided
 // out at the end.  So no maximum is looked for where nothing is raised.
 constexpr float kMostSum = 0x1p16f;
+// Weights above the reference make sums larger than values are.  From 2^118 on they are not taken: two groups and 32 pieces of smaller ones stay
+// within the range, and kv_attend's weights are at most 1.
+constexpr float kTooLarge = 0x1p10f;
 
 __device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(uintptr_t)at));

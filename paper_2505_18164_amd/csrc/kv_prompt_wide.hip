@@ -378,7 +378,8 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
   }
   __syncthreads();
   // A value that is not finite spoils the sums of rows that do not see it, too: a zero weight times infinity is no number.  Then all rows
-  // are computed once more, each by itself.  (Weights that are no numbers are what they should be.)
+  // are computed once more, each by itself, and where sums are so large that adding the groups' or pieces' might exceed binary32's
+  // range (kTooLarge).  (Weights that are no numbers are what they should be.)
   int* const flag = (int*)smem;
   if (threadIdx.x == 0) *flag = 0;
   __syncthreads();
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_kv_prompt_wide(KvCache c, KvRows 
 #pragma unroll
     for (int i = 0; i < HT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) odd = fmaf(o[u][i][e], 0.f, odd);
+      for (int e = 0; e < 16; ++e) odd = fmaf(o[u][i][e] * kTooLarge, 0.f, odd);
     if (__any(!(odd == 0.f) && l[u] - l[u] == 0.f)) atomicOr(flag, 2);
   }
   if (__any(once_more)) atomicOr(flag, 1);

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from kv_cases import HALF, Setup, attention, bound, dev, heads, within
+from kv_forms import plans
 from paper_2505_18164_amd import mdi
 
 pytestmark = pytest.mark.gpu
@@ -567,3 +568,28 @@ def test_samples_that_take_no_part_may_have_any_table(h, dtype, crowd):
     cache.append(tokens, k[:3], k[:3].clone(), q.clone(), cache.prep(freq=mdi.rope_freq(h)), q_out=q)
     assert (q[1] == 5.0).all()
     cache.check()
+
+
+@pytest.mark.parametrize("H,K,h,pt,lens,behind,rise,value", [
+    (32, 4, 128, 64, [100, 100], [4900, 4000], 11.0, 1.5 * 2.0 ** 100), (32, 4, 128, 64, [100, 64, 80, 90], [3000, 2500, 2900, 2000], 11.0, 1.5 * 2.0 ** 100),
+    (32, 2, 128, 24, [100, 64, 80, 90], [3000, 2500, 2900, 2000], 11.0, 1.5 * 2.0 ** 100), (16, 16, 128, 64, [64], [4000], 11.0, 1.5 * 2.0 ** 100), (8, 8, 128, 64, [1000], [3100], 11.0, 1.5 * 2.0 ** 100),
+    (32, 4, 64, 24, [130, 100, 90, 130], [3000, 2500, 2500, 2500], 7.0, 1.5 * 2.0 ** 106), (32, 4, 64, 64, [130, 100, 1, 130], [3000, 2500, 2500, 0], 7.0, 1.5 * 2.0 ** 106),
+    (32, 4, 64, 64, [1000], [3100], 7.0, 1.5 * 2.0 ** 106), (4, 2, 96, 16, [30], [4000], 5.0, 1.5 * 2.0 ** 106)])
+def test_sums_that_are_finite_until_they_are_added(H, K, h, pt, lens, behind, rise, value):
+    """Values near the largest that the call takes, behind first keys whose scores are lower: weights are counted from those, and groups' and
+    pieces' sums, each within binary32's range, would exceed it when they are added."""
+    for crowd in (0, 30000, 80000):
+        rows, ctx = sum(lens) + crowd // H, max(a + b for a, b in zip(lens, behind))
+        piece = plans([(BF16, K, h, 1, len(lens), rows, ctx, H, 0, 0)])[0][1]
+
+        def change(_, x):
+            x[0] = 0
+            x[0, :, :, 0] = np.where(np.arange(x.shape[1]) // 64 % piece < 2, 0, rise)[:, None]   # (the first two blocks of every piece)
+            x[1] = value
+        s = Setup(H, K, h, pt, lens, behind, BF16, seed=5, change=change, rows_behind=crowd // H)
+        s.q = torch.zeros_like(s.q)
+        s.q[:, :, 0] = 1
+        cache = s.cache()
+        out = s.attn(cache, s.plan(cache), scale=1.0)
+        assert (out[:s.start[-1]] == torch.tensor(value).to(BF16).item()).all()
+        cache.check()
