@@ -626,7 +626,7 @@ MDI_API mdi_status mdi_kv_append(const mdi_kv *cache, const mdi_kv8_rows *rows, 
  * page holds at positions that a row does not see (infinities and NaN included).
  * Scores, softmax and sums are binary32, and sums of weights times values are divided
  * at the end: the number of positions times the largest magnitude of a value has to be
- * below 2^120, and |scale| times a query's and key's sum of magnitudes of products below 2^120.
+ * below 2^120, and so have a query's and key's sum of magnitudes of products and |scale| times it.
  * Products of fp32 are fp32's.  bf16: products take a weight with 16 digits.
  * (Where a value that a row does not see is not finite, and where, in calls of many packed
  * rows of 128 channels, a score exceeds the largest of the first 32 keys that its row sees by
