@@ -1,10 +1,11 @@
 """Every form of the kernels of the cache in the storage type against 64 bits: digits, and every position counted once."""
+import numpy as np
 import pytest
 import torch
 
 import kv_forms as F
-from kv_cases import Setup
-from kv_digits import PARTS, check_digits, interval
+from kv_cases import Setup, bound, dev, sees, within
+from kv_digits import PARTS, check_digits, interval, limits
 from paper_2505_18164_amd import mdi
 
 pytestmark = pytest.mark.gpu
@@ -45,6 +46,61 @@ def test_every_position_counts_once(form, window):
 
     s, out = tried(form, window, change=F.ones(K, h, border))
     check(s, out, form)
+
+
+@pytest.mark.parametrize("form,window", [c for c in CALLS if "once" not in c[0]], ids=[f + (", window" if w else "") for f, w in CALLS if "once" not in f])
+def test_a_value_that_is_not_finite_reaches_only_who_sees_it(form, window):
+    """An infinite value amid every sample's new rows, and one before them that a window may have left behind: who sees neither is
+    what it is without them (they are computed again), and so are the other channels and kv heads of who does."""
+    what, max_ctx, one_each = F.calls()[form, window]
+    last, before = [b + t // 2 for b, t in zip(what["behind"], what["lens"])], [b // 3 for b in what["behind"]]
+
+    def spoiled(i, x):
+        if x.shape[1]:
+            x[1, min(last[i], x.shape[1] - 1), 0, 3] = np.inf
+            x[1, min(before[i], x.shape[1] - 1), 0, 5] = -np.inf
+    s, out = tried(form, window, change=spoiled)
+    got = out.float().cpu().double().numpy()[:s.start[-1]]
+    clean = Setup(**what, seed=7)
+    if s.dtype == torch.bfloat16:
+        lo, hi = limits(clean)
+    else:
+        want = clean.want()
+        may = bound(*want, s.h, s.dtype)
+        lo, hi = want[0] - may, want[0] + may
+    for i, T in enumerate(s.lens):
+        if T:
+            rows, seen = slice(s.start[i], s.start[i] + T), sees(T, s.behind[i], s.behind[i] + T, s.window, s.sinks)
+            for at, ch, value in ((min(last[i], seen.shape[1] - 1), 3, np.inf), (min(before[i], seen.shape[1] - 1), 5, -np.inf)):
+                lo[rows, :s.H // s.K, ch] = np.where(seen[:, at, None], value, lo[rows, :s.H // s.K, ch])
+                hi[rows, :s.H // s.K, ch] = np.where(seen[:, at, None], value, hi[rows, :s.H // s.K, ch])
+    fine = (lo <= got) & (got <= hi)
+    assert fine.all(), (form, (~fine).sum(), [int(x) for x in np.argwhere(~fine)[0]], got[tuple(np.argwhere(~fine)[0])])
+
+
+@pytest.mark.parametrize("form,window", [c for c in CALLS if c[0].startswith("any") or "whole" in c[0]][::2] + [c for c in CALLS if "of many" in c[0]],
+                         ids=lambda x: x if isinstance(x, str) else "window" if x else "all")
+def test_samples_between_that_take_no_part(form, window):
+    """Every third sample is idle, whatever its table: zeros for its rows, the others' as they are without it."""
+    what, max_ctx, one_each = F.calls()[form, window]
+    s = Setup(**what, seed=8)
+    idle = range(1, len(s.lens), 3)
+    s.pos[list(idle)] = -1
+    table = np.arange(len(s.lens))
+    table[list(idle)] = 10 ** 9
+    cache = s.cache()
+    out = s.attn(cache, s.plan(cache, one_each=one_each, max_ctx=max_ctx, table=dev(table.astype(np.int32))))
+    cache.check()
+    rows = np.zeros(out.shape[0], bool)
+    for i in idle:
+        rows[s.start[i]:s.start[i + 1]] = True
+    assert (out[dev(rows)] == 0).all()
+    if s.dtype == torch.bfloat16:
+        check_digits(out, s, what=form, skip=idle)
+    else:
+        want = s.want()
+        seen = np.flatnonzero(~rows[:want[0].shape[0]])
+        within(out[dev(seen)], want[0][seen], bound(*want, s.h, s.dtype)[seen], form)
 
 
 @pytest.mark.parametrize("dtype,H,K,h,n,rows", [(torch.bfloat16, 16, 16, 64, 300000, 300000), (torch.float32, 16, 8, 32, 550000, 550000), (torch.bfloat16, 16, 16, 128, 1800000, 600000)],
