@@ -628,9 +628,12 @@ MDI_API mdi_status mdi_kv_append(const mdi_kv *cache, const mdi_kv8_rows *rows, 
  * at the end: the number of positions times the largest magnitude of a value has to be
  * below 2^120, and so have a query's and key's sum of magnitudes of products and |scale| times it.
  * Products of fp32 are fp32's.  bf16: products take a weight with 16 digits.
- * (Where a value that a row does not see is not finite, and where, in calls of many packed
- * rows of 128 channels, a score exceeds the largest of the first 32 keys that its row sees by
- * 17 or more, rows are computed a second time; the former takes tens of times as long.)  Limits, alignment
+ * (Where a value that a row does not see is not finite, or sums of weights times values
+ * come near the end of binary32's range, rows are computed a second time, which takes tens
+ * of times as long.  In calls of many packed rows of 128 channels they are too, which takes
+ * up to twice as long, where a score exceeds the largest of the first 32 keys that its row
+ * sees by 17 or more.)  First positions that stay keep the angles that they were appended
+ * with.  Limits, alignment
  * (strides multiples of 16 bytes; q and out must not overlap), workspace and errors are
  * those of mdi_kv8_attn, its size mdi_kv_attn_bytes'.  Results do not depend on timing.
  */

@@ -1,5 +1,5 @@
 // Attention over the cache in the storage type on the matrix cores, for what the other kernels do not serve: fp32, and bf16 heads of other
-// than 64 or 128 channels, single tokens and packed rows; and for packed rows that are too few for kv_prompt.hip (kv_plan).
+// than 64 or 128 channels, single tokens and packed rows; and for packed rows that are too few for kv_prompt.hip (kv_plan.h).
 //
 // A workgroup takes sixteen rows of (position, query head) of a kv head, or two times sixteen, and its four wavefronts (two) a share each of
 // the keys they see, sixteen at a time (bf16: two times sixteen), straight from the pages into registers; their sums are added

@@ -1,8 +1,8 @@
 // Attention of packed rows - prompts, or the next pieces of prompts, of several samples - over the bf16 cache, on the matrix cores: heads
-// of 64, and the plan for these and for heads of 128 (kv_prompt_wide.hip).  Few rows are kv_any.hip's.
+// of 64, and the launches of these and of heads of 128 (kv_prompt_wide.hip).  Few rows are kv_any.hip's.
 //
-// A workgroup takes 32 rows of (position, query head) for each of its wavefronts, the heads of one kv head side by side, and passes
-// over the keys they see 64 at a time (KvBlocks).  A wavefront computes S^T = K Q^T with v_mfma_f32_32x32x16_bf16, weighs the scores
+// A workgroup is one group of eight wavefronts or two of four; a group's wavefronts take 32 rows of (position, query head) each, the heads of
+// one kv head side by side, and pass over the keys they see 64 at a time (KvBlocks), two groups over every other 64 of the same rows' keys.  A wavefront computes S^T = K Q^T with v_mfma_f32_32x32x16_bf16, weighs the scores
 // against a reference of its row, and adds O^T += V^T P^T: the scores of a query lie in the lane, and in the order, in which the second
 // product takes weights, so they never leave the registers.  Keys and values travel from the pages to the LDS without passing
 // registers, a block ahead, 16 bytes a lane; the 16-byte units of a row are permuted by the row's number (the permutation is
